@@ -440,6 +440,98 @@ cci_status cci_linear_dense_tc_static(const void *X, cci_dtype dtype, int64_t N,
                                       int K, float *Y, uint32_t *dev_status, cci_stream_t stream);
 
 /*
+ * ---- The layers around a pruned projection: norms and what a head answers ----
+ * (The paper has no counterpart: a language model's feed-forward sub-layer needs them
+ * beside its projections.)  Row strides ld* are in elements, at least the row's length.
+ */
+
+/*
+ * cci_layer_norm -- y[n][c] = (x[n][c] - mean[n]) * rstd[n] * weight[c] + bias[c] for
+ * N rows of D, mean the row's mean, rstd = 1 / sqrt(var + eps) with var the mean
+ * square of the differences from it (all sums fp32; y rounded once).
+ *
+ *   x          device, N rows of D of dtype, row stride ldx
+ *   weight, bias device fp32 [D] or NULL (1 and 0)
+ *   y          device [N][D] of dtype (written)
+ *   mean, rstd device fp32 [N] (written; the backward pass reads them)
+ * N = 0 is valid and enqueues nothing.  eps must be >= 0 (CCI_ERR_VALUE; NaN too).
+ * Errors: CCI_ERR_NULL, CCI_ERR_SHAPE (D < 1, ldx < D), CCI_ERR_DTYPE,
+ *         CCI_ERR_ALIGN, CCI_ERR_VALUE, CCI_ERR_CUDA.
+ */
+cci_status cci_layer_norm(const void *x, cci_dtype dtype, int64_t N, int64_t D, int64_t ldx, const float *weight,
+                          const float *bias, float eps, void *y, float *mean, float *rstd, cci_stream_t stream);
+
+/*
+ * cci_layer_norm_backward -- the gradients of cci_layer_norm, with g = dy * weight and
+ * xh = (x - mean) * rstd:
+ *   dx      = rstd * (g - mean over c of g - xh * mean over c of g * xh)
+ *   dweight[c] = sum over n of dy * xh,  dbias[c] = sum over n of dy
+ * The sums over n are added in a fixed order: the same call gives the same bits.
+ *
+ *   dy         device, N rows of D of dtype, row stride lddy;  x as in the forward call
+ *   mean, rstd as cci_layer_norm wrote them
+ *   weight     as in the forward call (NULL: 1)
+ *   dx         device [N][D] of dtype (written)
+ *   dweight, dbias device fp32 [D] (written; zeros for N = 0), each may be NULL
+ *   workspace  device, 16-byte aligned, cci_layer_norm_workspace_size(N, D) bytes (which
+ *              depends on the current device's number of SMs); overwritten
+ * Errors: as cci_layer_norm; CCI_ERR_WORKSPACE.
+ */
+size_t cci_layer_norm_workspace_size(int64_t N, int64_t D);
+cci_status cci_layer_norm_backward(const void *dy, int64_t lddy, const void *x, int64_t ldx, cci_dtype dtype,
+                                   int64_t N, int64_t D, const float *mean, const float *rstd, const float *weight,
+                                   void *dx, float *dweight, float *dbias, void *workspace, size_t workspace_bytes,
+                                   cci_stream_t stream);
+
+/*
+ * cci_token_logprobs -- for N rows of V logits x, each with a token t:
+ *   logp[n]    = x[t] - log sum exp(x)
+ *   entropy[n] = - sum over v of p_v log p_v, p the row's softmax
+ *   top_logp[n][j], top_idx[n][j]   the `top` largest logits' log probabilities and
+ *                indices, largest first, ties by increasing index
+ *   stats[n]   = (m, log sum exp(x - m)), m the row's maximum (the gradient needs them)
+ * Masked logits (-inf) have probability 0 and add nothing to the entropy.  A row of -inf
+ * alone gives logp -inf, entropy 0, top_logp -inf and stats (-inf, 0).  NaN or +inf in a
+ * row makes its logp and entropy NaN; NaN logits are never listed (places that no number
+ * fills: index -1, NaN).  A token equal to `ignore_index` gives logp 0; any other token
+ * outside [0, V) sets CCI_ERR_INDEX in dev_status and gives NaN.
+ *
+ *   logits     device, N rows of V of dtype, row stride ldx
+ *   tokens     device int64 [N]
+ *   logp, entropy device fp32 [N]; stats fp32 [N][2] (written)
+ *   top        0 .. min(V, CCI_MAX_TOP); top_logp fp32, top_idx int32 [N][top] (written;
+ *              may be NULL for top = 0)
+ *   dev_status device uint32 or NULL
+ * N = 0 is valid and enqueues nothing.
+ * Errors: CCI_ERR_NULL, CCI_ERR_SHAPE (V < 1 or >= 2^31, N >= 2^31, ldx < V, top out of
+ *         range), CCI_ERR_DTYPE, CCI_ERR_ALIGN, CCI_ERR_CUDA.
+ */
+#define CCI_MAX_TOP 32
+cci_status cci_token_logprobs(const void *logits, cci_dtype dtype, int64_t N, int64_t V, int64_t ldx,
+                              const int64_t *tokens, int64_t ignore_index, int top, float *logp, float *entropy,
+                              float *stats, float *top_logp, int32_t *top_idx, uint32_t *dev_status,
+                              cci_stream_t stream);
+
+/*
+ * cci_token_logprobs_backward -- the gradient of logp and entropy to the logits:
+ *   dlogits[n][v] = dlogp[n] * (1[v = t] - p_v) - dentropy[n] * p_v * (log p_v + entropy[n])
+ * Rows of -inf alone, and for the first term rows whose token is `ignore_index`, get 0.
+ *
+ *   logits, tokens as in the forward call; stats, entropy as it wrote them
+ *   dlogp      device fp32 [N] or NULL (0; tokens may be NULL then)
+ *   dentropy   device fp32 [N] or NULL (0; entropy may be NULL then)
+ *   dlogits    device, N rows of V of dtype, row stride lddx (written; may be the logits
+ *              themselves, with the same stride).  Rows at the same offset from a 16-byte boundary
+ *              as the logits' rows are written in whole vectors
+ *   dev_status as in the forward call: a token outside [0, V) counts as left out
+ * Errors: as cci_token_logprobs; CCI_ERR_SHAPE also for lddx < V.
+ */
+cci_status cci_token_logprobs_backward(const void *logits, cci_dtype dtype, int64_t N, int64_t V, int64_t ldx,
+                                       const float *stats, const int64_t *tokens, int64_t ignore_index,
+                                       const float *dlogp, const float *entropy, const float *dentropy,
+                                       void *dlogits, int64_t lddx, uint32_t *dev_status, cci_stream_t stream);
+
+/*
  * cci_kernel_name -- the name of the kernel family that cci_linear_ws /
  * cci_conv2d_ws would run for a layer with these sizes (R = Cin for a product,
  * Cin*KH*KW for a convolution, taken to have strides <= 2) when every pointer is

@@ -68,6 +68,13 @@ SIGNATURES = {
     "cci_dense_planes": (_I32, [_P, _I32, _I64, _I64, _P, ctypes.c_size_t, _P]),
     "cci_dense_conv2d_tc": (_I32, [_P, _I32, _I64, _I64, _I64, _I64, _P, _I64, _I32, _I32, _I32, _I32,
                                    _I32, _I32, _P, _U32P, _P]),
+    "cci_layer_norm": (_I32, [_P, _I32, _I64, _I64, _I64, _P, _P, ctypes.c_float, _P, _P, _P, _P]),
+    "cci_layer_norm_workspace_size": (ctypes.c_size_t, [_I64, _I64]),
+    "cci_layer_norm_backward": (_I32, [_P, _I64, _P, _I64, _I32, _I64, _I64, _P, _P, _P, _P, _P, _P, _P,
+                                       ctypes.c_size_t, _P]),
+    "cci_token_logprobs": (_I32, [_P, _I32, _I64, _I64, _I64, _P, _I64, _I32, _P, _P, _P, _P, _P, _U32P, _P]),
+    "cci_token_logprobs_backward": (_I32, [_P, _I32, _I64, _I64, _I64, _P, _P, _I64, _P, _P, _P, _P, _I64, _U32P,
+                                           _P]),
     "cci_kernel_name": (ctypes.c_char_p, [_I32, _I64, _I64, _I64, _I32, _I32, _I32]),
     "cci_status_string": (ctypes.c_char_p, [_I32]),
     "cci_decode_device_status": (_I32, [ctypes.c_uint32]),
@@ -470,6 +477,140 @@ def dense_conv2d_tc(X: torch.Tensor, Wd: torch.Tensor, Cout: int, KH: int, KW: i
                                      status.data_ptr() if status is not None else None, _stream(X.device)),
            "cci_dense_conv2d_tc")
     return Y
+
+
+# ---------------------------------------------------------------------------
+# the layers around a pruned projection
+# ---------------------------------------------------------------------------
+
+def _cuda_rows(t: torch.Tensor, name: str) -> int:
+    """Row stride of a CUDA matrix whose rows are contiguous."""
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a CUDA tensor")
+    if t.dim() != 2:
+        raise ValueError(f"{name} must be a matrix")
+    rows, cols = t.shape
+    if cols > 1 and t.stride(1) != 1:
+        raise ValueError(f"{name} must have contiguous rows")
+    ld = t.stride(0) if rows > 1 else cols
+    if ld < cols:
+        raise ValueError(f"{name} must not have overlapping rows")
+    return ld
+
+
+def _cuda_vec(t: Optional[torch.Tensor], n: int, name: str, dtype: torch.dtype = torch.float32) -> Optional[int]:
+    """Address of a contiguous CUDA vector of n elements (None: NULL)."""
+    if t is None:
+        return None
+    _cuda_contig(t, name)
+    if t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}")
+    if t.numel() != n:
+        raise ValueError(f"{name} must have {n} elements")
+    return t.data_ptr()
+
+
+def layer_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None, *,
+               eps: float = 1e-5, out: Optional[torch.Tensor] = None):
+    """(y, mean, rstd) of the rows of x[N][D] (``cci_layer_norm``): y in x's dtype, the
+    fp32 mean and 1 / sqrt(var + eps) of each row for the backward pass.  ``weight`` and ``bias``
+    are fp32 [D]; x may have a row stride."""
+    ld = _cuda_rows(x, "x")
+    N, D = x.shape
+    y = out if out is not None else torch.empty((N, D), dtype=x.dtype, device=x.device)
+    if out is not None:
+        _like(out, (N, D), x.dtype, "out")
+    stats = torch.empty((2, N), dtype=torch.float32, device=x.device)
+    mean, rstd = stats.unbind(0)
+    _check(lib().cci_layer_norm(x.data_ptr(), _dtype_code(x), N, D, ld, _cuda_vec(weight, D, "weight"),
+                                _cuda_vec(bias, D, "bias"), eps, y.data_ptr(), mean.data_ptr(), rstd.data_ptr(),
+                                _stream(x.device)), "cci_layer_norm")
+    return y, mean, rstd
+
+
+def layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, mean: torch.Tensor, rstd: torch.Tensor,
+                        weight: Optional[torch.Tensor] = None, *, out: Optional[torch.Tensor] = None,
+                        workspace: Optional[torch.Tensor] = None):
+    """(dx, dweight, dbias) of ``layer_norm`` (``cci_layer_norm_backward``): dx in x's dtype,
+    the parameters' gradients fp32 [D], whether or not the forward call had them."""
+    ldx, lddy = _cuda_rows(x, "x"), _cuda_rows(dy, "dy")
+    N, D = x.shape
+    if dy.shape != x.shape or dy.dtype != x.dtype:
+        raise ValueError("dy must have x's shape and dtype")
+    dx = out if out is not None else torch.empty((N, D), dtype=x.dtype, device=x.device)
+    if out is not None:
+        _like(out, (N, D), x.dtype, "out")
+    params = torch.empty((2, D), dtype=torch.float32, device=x.device)
+    dw, db = params.unbind(0)
+    if workspace is None:
+        workspace = _workspace(_norm_bytes(N, D, x.device.index), x.device)
+    wp, wb = _ws(workspace)
+    _check(lib().cci_layer_norm_backward(dy.data_ptr(), lddy, x.data_ptr(), ldx, _dtype_code(x), N, D,
+                                         _cuda_vec(mean, N, "mean"), _cuda_vec(rstd, N, "rstd"),
+                                         _cuda_vec(weight, D, "weight"), dx.data_ptr(), dw.data_ptr(), db.data_ptr(),
+                                         wp, wb, _stream(x.device)), "cci_layer_norm_backward")
+    return dx, dw, db
+
+
+def token_logprobs(logits: torch.Tensor, tokens: torch.Tensor, *, top: int = 0, ignore_index: int = -100,
+                   status: Optional[torch.Tensor] = None):
+    """(logp, entropy, stats, top_logp, top_idx) of the rows of logits[N][V] and one token (int64) each
+    (``cci_token_logprobs``): the token's log probability (0 for ``ignore_index``), the row's entropy,
+    (maximum, log of the sum of exp(x - maximum)) for the backward pass, and the ``top`` (at most 32)
+    most probable tokens' log probabilities and indices, ties to the lower index (None for top = 0).
+    The logits may have a row stride."""
+    ld = _cuda_rows(logits, "logits")
+    N, V = logits.shape
+    f = torch.empty((4 + top, N), dtype=torch.float32, device=logits.device).view(-1)
+    logp, entropy, stats = f[:N], f[N:2 * N], f[2 * N:4 * N].view(N, 2)
+    top_logp = f[4 * N:].view(N, top) if top else None
+    top_idx = torch.empty((N, top), dtype=torch.int32, device=logits.device) if top else None
+    _check(lib().cci_token_logprobs(logits.data_ptr(), _dtype_code(logits), N, V, ld,
+                                    _cuda_vec(tokens, N, "tokens", torch.int64), ignore_index, top, logp.data_ptr(),
+                                    entropy.data_ptr(), stats.data_ptr(), top_logp.data_ptr() if top else None,
+                                    top_idx.data_ptr() if top else None,
+                                    status.data_ptr() if status is not None else None, _stream(logits.device)),
+           "cci_token_logprobs")
+    return logp, entropy, stats, top_logp, top_idx
+
+
+def token_logprobs_backward(logits: torch.Tensor, tokens: Optional[torch.Tensor], stats: torch.Tensor, *,
+                            dlogp: Optional[torch.Tensor] = None, entropy: Optional[torch.Tensor] = None,
+                            dentropy: Optional[torch.Tensor] = None, ignore_index: int = -100,
+                            out: Optional[torch.Tensor] = None,
+                            status: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """The gradient of ``token_logprobs`` to the logits, in their dtype (``cci_token_logprobs_backward``):
+    of logp weighted by ``dlogp`` and of the entropy weighted by ``dentropy`` (which needs ``entropy``, as
+    the forward call returned it).  It has the logits' row stride unless ``out`` is given; ``out`` may be
+    the logits."""
+    ld = _cuda_rows(logits, "logits")
+    N, V = logits.shape
+    if out is None:
+        out = torch.empty((N, ld), dtype=logits.dtype, device=logits.device)[:, :V]
+        ldd = ld
+    else:
+        ldd = _cuda_rows(out, "out")
+        if out.shape != logits.shape or out.dtype != logits.dtype:
+            raise ValueError("out must have the logits' shape and dtype")
+    _check(lib().cci_token_logprobs_backward(logits.data_ptr(), _dtype_code(logits), N, V, ld,
+                                             _cuda_vec(stats, 2 * N, "stats"),
+                                             _cuda_vec(tokens, N, "tokens", torch.int64), ignore_index,
+                                             _cuda_vec(dlogp, N, "dlogp"), _cuda_vec(entropy, N, "entropy"),
+                                             _cuda_vec(dentropy, N, "dentropy"), out.data_ptr(), ldd,
+                                             status.data_ptr() if status is not None else None,
+                                             _stream(logits.device)), "cci_token_logprobs_backward")
+    return out
+
+
+def _like(t: torch.Tensor, shape, dtype: torch.dtype, name: str) -> None:
+    _cuda_contig(t, name)
+    if tuple(t.shape) != tuple(shape) or t.dtype != dtype:
+        raise ValueError(f"{name} must be {tuple(shape)} of {dtype}")
+
+
+@functools.lru_cache(maxsize=4096)
+def _norm_bytes(N: int, D: int, device_index: int) -> int:
+    return int(lib().cci_layer_norm_workspace_size(N, D))
 
 
 def kernel_name(dtype: torch.dtype, Cin: int, R: int, Cout: int, G: int, K: int,

@@ -6,6 +6,7 @@
 #include <cstring>
 #include <mutex>
 
+#include "cci_checks.h"
 #include "cci_kernels.h"
 
 namespace cci {
@@ -16,28 +17,6 @@ extern const RegtileEntry kRegtile_bf16_a[];
 extern const RegtileEntry kRegtile_bf16_b[];
 
 namespace {
-
-constexpr int64_t kMaxElems = int64_t(1) << 62;
-
-bool aligned(const void *p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
-
-size_t elem_size(int dtype) { return dtype == CCI_F32 ? 4 : 2; }
-
-bool valid_dtype(int dtype) { return dtype == CCI_F32 || dtype == CCI_BF16; }
-
-// a*b without overflow past kMaxElems (all inputs >= 0)
-bool mul_ok(int64_t a, int64_t b)
-{
-    if (a == 0 || b == 0) return true;
-    return a <= kMaxElems / b;
-}
-
-cci_status check_group(int64_t Cout, int G, int K)
-{
-    if (G < 1 || G > 256 || K < 1 || K > G) return CCI_ERR_GROUP;
-    if (Cout % G != 0) return CCI_ERR_GROUP;
-    return CCI_OK;
-}
 
 // expand = true: the branch-free kernel (D == 0); false: the jump-dispatch kernel
 const RegtileEntry *find_regtile(int dtype, int G, int K, bool expand)
@@ -70,8 +49,6 @@ bool regtile_ptr_ok(const FwdParams &p)
 {
     return aligned(p.X, 16) && aligned(p.values, 16) && aligned(p.idx, 16) && aligned(p.Y, 16);
 }
-
-cci_status to_status(cudaError_t e) { return e == cudaSuccess ? CCI_OK : CCI_ERR_CUDA; }
 
 // workspace of the dense tensor-core family: bf16 dense weights [Cout][R], or
 // for fp32 the two operand planes of the split (cci_common.cuh): plane 0

@@ -54,6 +54,25 @@ bool gemm_pk_shape_ok(const FwdParams &p);
 bool gemm_pk_supported(const FwdParams &p);
 cudaError_t launch_gemm_pk(const FwdParams &p, cudaStream_t stream);
 
+// layer norm (cci_norm.cu); ld*: row strides in elements.  part: the backward pass' workspace
+// of layer_norm_workspace bytes (N >= 1), which the sums of dw and db need
+size_t layer_norm_workspace(int64_t N, int64_t D);
+cudaError_t launch_layer_norm(const void *x, int dtype, int64_t N, int64_t D, int64_t ldx, const float *w,
+                              const float *b, float eps, void *y, float *mean, float *rstd, cudaStream_t stream);
+cudaError_t launch_layer_norm_backward(const void *dy, int64_t lddy, const void *x, int64_t ldx, int dtype, int64_t N,
+                                       int64_t D, const float *mean, const float *rstd, const float *w, void *dx,
+                                       float *dw, float *db, float *part, cudaStream_t stream);
+
+// token log probabilities (cci_logprobs.cu)
+cudaError_t launch_token_logprobs(const void *logits, int dtype, int64_t N, int64_t V, int64_t ldx,
+                                  const int64_t *tokens, int64_t ignore, int top, float *logp, float *entropy,
+                                  float *stats, float *top_logp, int32_t *top_idx, uint32_t *status,
+                                  cudaStream_t stream);
+cudaError_t launch_token_logprobs_backward(const void *logits, int dtype, int64_t N, int64_t V, int64_t ldx,
+                                           const float *stats, const int64_t *tokens, int64_t ignore,
+                                           const float *dlogp, const float *entropy, const float *dentropy, void *dx,
+                                           int64_t lddx, uint32_t *status, cudaStream_t stream);
+
 // One register-tiled instantiation: (dtype, G, K) -> tile shape and launcher.
 struct RegtileEntry {
     int dtype, G, K, MG, T, D;
