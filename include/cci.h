@@ -440,7 +440,7 @@ cci_status cci_linear_dense_tc_static(const void *X, cci_dtype dtype, int64_t N,
                                       int K, float *Y, uint32_t *dev_status, cci_stream_t stream);
 
 /*
- * ---- The layers around a pruned projection: norms and what a head answers ----
+ * ---- The layers around a pruned projection: norms, the gated block, what a head answers ----
  * (The paper has no counterpart: a language model's feed-forward sub-layer needs them
  * beside its projections.)  Row strides ld* are in elements, at least the row's length.
  */
@@ -530,6 +530,83 @@ cci_status cci_token_logprobs_backward(const void *logits, cci_dtype dtype, int6
                                        const float *stats, const int64_t *tokens, int64_t ignore_index,
                                        const float *dlogp, const float *entropy, const float *dentropy,
                                        void *dlogits, int64_t lddx, uint32_t *dev_status, cci_stream_t stream);
+
+/*
+ * cci_gated_linear -- the gated feed-forward block's two projections, activation and
+ * product in one kernel, for N tokens of D features and F hidden channels:
+ *   g = X Wg^T,  u = X Wu^T,  H[n][f] = act(g[n][f]) * u[n][f]
+ * with fp32 accumulators and one rounding, to the type of H.  bf16: products of the exact
+ * values on the tensor cores.  fp32: every operand as three bf16 planes, the six products
+ * of planes down to 2^-18 of the whole (what is left out is below 2^-25 |x||w| a term; an
+ * infinite input gives NaN where its products of planes do).
+ *
+ *   X          device [N][D] of dtype
+ *   Wg, Wu     device [F][D] of dtype (pruned weights: their dense form, as cci_td_mask
+ *              writes it; or cci_gated_linear_packed)
+ *   H          device [N][F] of dtype (written)
+ *   g, u       device fp32 [N][F] (written, for cci_gated_linear_backward), or both NULL
+ *   workspace  device, 16-byte aligned, cci_gated_workspace_size(CCI_GATED_FORWARD, ...)
+ *              bytes (0 for bf16, which needs none); overwritten
+ *   dev_status device uint32 or NULL (CCI_ERR_TIMEOUT)
+ * D and F are multiples of 8; every matrix is 16-byte aligned.  N = 0 is valid and enqueues
+ * nothing.
+ * Errors: CCI_ERR_NULL (also one of g and u alone), CCI_ERR_SHAPE (N < 0, D or F < 1, sizes
+ *         of 2^30 or more), CCI_ERR_UNSUPPORTED (D % 8, F % 8), CCI_ERR_DTYPE,
+ *         CCI_ERR_VALUE (act is not a cci_activation), CCI_ERR_ALIGN, CCI_ERR_WORKSPACE,
+ *         CCI_ERR_CUDA.
+ */
+typedef enum cci_activation {
+    CCI_ACT_SILU = 0,      /* g / (1 + exp(-g)) */
+    CCI_ACT_GELU = 1,      /* g * Phi(g), by the error function */
+    CCI_ACT_GELU_TANH = 2, /* g / 2 * (1 + tanh(sqrt(2 / pi) * (g + 0.044715 g^3))) */
+    CCI_ACT_RELU = 3,      /* max(g, 0); NaN stays */
+    CCI_ACT_SIGMOID = 4    /* 1 / (1 + exp(-g)) */
+} cci_activation;
+
+typedef enum cci_gated_call {
+    CCI_GATED_FORWARD = 0,
+    CCI_GATED_PACKED = 1,
+    CCI_GATED_BACKWARD = 2
+} cci_gated_call;
+
+/* bytes of workspace of a call (0: none needed, or invalid sizes) */
+size_t cci_gated_workspace_size(cci_gated_call call, cci_dtype dtype, int64_t N, int64_t D, int64_t F);
+
+cci_status cci_gated_linear(const void *X, cci_dtype dtype, int64_t N, int64_t D, const void *Wg, const void *Wu,
+                            int64_t F, cci_activation act, void *H, float *g, float *u, uint32_t *dev_status,
+                            void *workspace, size_t workspace_bytes, cci_stream_t stream);
+
+/*
+ * cci_gated_linear_packed -- cci_gated_linear with both weight matrices in the packed format
+ * of cci_pack (Cout = F, R = D, the same G and K): any G and K of that format.  The weights
+ * are expanded into the workspace (CCI_GATED_PACKED) and multiplied there, so pruned
+ * positions take part as zeros (an infinite x gives NaN).  An index set that is not strictly
+ * increasing or has an index >= G sets CCI_ERR_INDEX in dev_status.
+ * Errors: as cci_gated_linear; CCI_ERR_GROUP.
+ */
+cci_status cci_gated_linear_packed(const void *X, cci_dtype dtype, int64_t N, int64_t D, const void *gate_values,
+                                   const uint8_t *gate_idx, const void *up_values, const uint8_t *up_idx, int64_t F,
+                                   int G, int K, cci_activation act, void *H, uint32_t *dev_status, void *workspace,
+                                   size_t workspace_bytes, cci_stream_t stream);
+
+/*
+ * cci_gated_linear_backward -- the gradients of cci_gated_linear from that of H:
+ *   dg = dH * u * act'(g),  du = dH * act(g)      (act' of ReLU at 0 is 0)
+ *   dX = dg Wg + du Wu,  dWg = dg^T X,  dWu = du^T X
+ * dg and du are rounded to bf16 for the products (fp32: split into planes, as every operand);
+ * sums are fp32 in a fixed order, each gradient rounded once to dtype.
+ *
+ *   dH         device [N][F] of dtype;  X, Wg, Wu as in the forward call
+ *   g, u       as the forward call wrote them
+ *   dX         device [N][D] of dtype (written), or NULL
+ *   dWg, dWu   device [F][D] of dtype (written; zeros for N = 0), or both NULL
+ *   workspace  cci_gated_workspace_size(CCI_GATED_BACKWARD, ...) bytes
+ * Errors: as cci_gated_linear.
+ */
+cci_status cci_gated_linear_backward(const void *dH, const void *X, cci_dtype dtype, int64_t N, int64_t D,
+                                     const void *Wg, const void *Wu, int64_t F, cci_activation act, const float *g,
+                                     const float *u, void *dX, void *dWg, void *dWu, uint32_t *dev_status,
+                                     void *workspace, size_t workspace_bytes, cci_stream_t stream);
 
 /*
  * cci_kernel_name -- the name of the kernel family that cci_linear_ws /

@@ -25,6 +25,8 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "_build", "libcci.so")
 
 F32, BF16 = 0, 1
+ACTIVATIONS = {"silu": 0, "gelu": 1, "gelu_tanh": 2, "relu": 3, "sigmoid": 4}
+GATED_FORWARD, GATED_PACKED, GATED_BACKWARD = 0, 1, 2
 ALGO_AUTO, ALGO_GENERIC, ALGO_REGTILE, ALGO_DENSE_TC, ALGO_EXPAND, ALGO_DENSE_TC_WS = 0, 1, 2, 3, 4, 5
 
 STATUS_NAMES = {
@@ -75,6 +77,13 @@ SIGNATURES = {
     "cci_token_logprobs": (_I32, [_P, _I32, _I64, _I64, _I64, _P, _I64, _I32, _P, _P, _P, _P, _P, _U32P, _P]),
     "cci_token_logprobs_backward": (_I32, [_P, _I32, _I64, _I64, _I64, _P, _P, _I64, _P, _P, _P, _P, _I64, _U32P,
                                            _P]),
+    "cci_gated_workspace_size": (ctypes.c_size_t, [_I32, _I32, _I64, _I64, _I64]),
+    "cci_gated_linear": (_I32, [_P, _I32, _I64, _I64, _P, _P, _I64, _I32, _P, _P, _P, _U32P, _P, ctypes.c_size_t,
+                                _P]),
+    "cci_gated_linear_packed": (_I32, [_P, _I32, _I64, _I64, _P, _P, _P, _P, _I64, _I32, _I32, _I32, _P, _U32P, _P,
+                                       ctypes.c_size_t, _P]),
+    "cci_gated_linear_backward": (_I32, [_P, _P, _I32, _I64, _I64, _P, _P, _I64, _I32, _P, _P, _P, _P, _P, _U32P, _P,
+                                         ctypes.c_size_t, _P]),
     "cci_kernel_name": (ctypes.c_char_p, [_I32, _I64, _I64, _I64, _I32, _I32, _I32]),
     "cci_status_string": (ctypes.c_char_p, [_I32]),
     "cci_decode_device_status": (_I32, [ctypes.c_uint32]),
@@ -600,6 +609,107 @@ def token_logprobs_backward(logits: torch.Tensor, tokens: Optional[torch.Tensor]
                                              status.data_ptr() if status is not None else None,
                                              _stream(logits.device)), "cci_token_logprobs_backward")
     return out
+
+
+def _act_code(act: str) -> int:
+    code = ACTIVATIONS.get(act)
+    if code is None:
+        raise ValueError(f"unknown activation {act!r}: one of {', '.join(ACTIVATIONS)}")
+    return code
+
+
+def gated_workspace(call: int, dtype: torch.dtype, N: int, D: int, F: int, device) -> Optional[torch.Tensor]:
+    """The workspace of a gated block's call (``GATED_FORWARD``, ``GATED_PACKED`` or ``GATED_BACKWARD``), from
+    PyTorch memory: None when it needs none."""
+    return _workspace(_gated_bytes(call, F32 if dtype == torch.float32 else BF16, N, D, F), device)
+
+
+@functools.lru_cache(maxsize=4096)
+def _gated_bytes(call: int, dtype: int, N: int, D: int, F: int) -> int:
+    return int(lib().cci_gated_workspace_size(call, dtype, N, D, F))
+
+
+def gated_linear(X: torch.Tensor, Wg: torch.Tensor, Wu: torch.Tensor, *, act: str = "silu", save: bool = False,
+                 out: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None,
+                 workspace: Optional[torch.Tensor] = None):
+    """H[N][F] = act(X Wg^T) * (X Wu^T) in X's dtype (``cci_gated_linear``): both projections of a gated
+    feed-forward block, the activation (a key of ``ACTIVATIONS``) and the product in one kernel.
+    X [N][D], Wg and Wu dense [F][D]; D and F multiples of 8.  ``save``: returns (H, g, u) with the fp32
+    pre-activations for ``gated_linear_backward``."""
+    _cuda_contig(X, "X")
+    N, D = X.shape
+    F = Wg.shape[0]
+    _like(Wg, (F, D), X.dtype, "Wg")
+    _like(Wu, (F, D), X.dtype, "Wu")
+    code = _dtype_code(X)
+    if out is not None:
+        _like(out, (N, F), X.dtype, "out")
+    H = out if out is not None else torch.empty((N, F), dtype=X.dtype, device=X.device)
+    g = torch.empty((N, F), dtype=torch.float32, device=X.device) if save else None
+    u = torch.empty((N, F), dtype=torch.float32, device=X.device) if save else None
+    if workspace is None:
+        workspace = _workspace(_gated_bytes(GATED_FORWARD, code, N, D, F), X.device)
+    wp, wb = _ws(workspace)
+    _check(lib().cci_gated_linear(X.data_ptr(), code, N, D, Wg.data_ptr(), Wu.data_ptr(), F, _act_code(act),
+                                  H.data_ptr(), g.data_ptr() if save else None, u.data_ptr() if save else None,
+                                  status.data_ptr() if status is not None else None, wp, wb, _stream(X.device)),
+           "cci_gated_linear")
+    return (H, g, u) if save else H
+
+
+def gated_linear_packed(X: torch.Tensor, gate: Tuple[torch.Tensor, torch.Tensor],
+                        up: Tuple[torch.Tensor, torch.Tensor], F: int, G: int, K: int, *, act: str = "silu",
+                        out: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None,
+                        workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """``gated_linear`` with packed weights: ``gate`` and ``up`` are the (values, idx) pairs of ``pack``
+    for [F][D] weights, both with (G, K) (``cci_gated_linear_packed``)."""
+    _cuda_contig(X, "X")
+    N, D = X.shape
+    if G < 1 or F % G:
+        raise CCIError(3, "gated_linear_packed")
+    for (v, i), name in ((gate, "gate"), (up, "up")):
+        _like(v, (F // G, D, K), X.dtype, name + " values")
+        _like(i, (F // G, D, K), torch.uint8, name + " idx")
+    code = _dtype_code(X)
+    if out is not None:
+        _like(out, (N, F), X.dtype, "out")
+    H = out if out is not None else torch.empty((N, F), dtype=X.dtype, device=X.device)
+    if workspace is None:
+        workspace = _workspace(_gated_bytes(GATED_PACKED, code, N, D, F), X.device)
+    wp, wb = _ws(workspace)
+    _check(lib().cci_gated_linear_packed(X.data_ptr(), code, N, D, gate[0].data_ptr(), gate[1].data_ptr(),
+                                         up[0].data_ptr(), up[1].data_ptr(), F, G, K, _act_code(act), H.data_ptr(),
+                                         status.data_ptr() if status is not None else None, wp, wb,
+                                         _stream(X.device)), "cci_gated_linear_packed")
+    return H
+
+
+def gated_linear_backward(dH: torch.Tensor, X: torch.Tensor, Wg: torch.Tensor, Wu: torch.Tensor, g: torch.Tensor,
+                          u: torch.Tensor, *, act: str = "silu", need_dx: bool = True, need_dw: bool = True,
+                          status: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None):
+    """(dX, dWg, dWu) of ``gated_linear`` (``cci_gated_linear_backward``) from the gradient of H and the saved
+    g and u, each in X's dtype; None for those not asked for (``need_dx``, ``need_dw``)."""
+    _cuda_contig(X, "X")
+    N, D = X.shape
+    F = Wg.shape[0]
+    _like(dH, (N, F), X.dtype, "dH")
+    _like(Wg, (F, D), X.dtype, "Wg")
+    _like(Wu, (F, D), X.dtype, "Wu")
+    _like(g, (N, F), torch.float32, "g")
+    _like(u, (N, F), torch.float32, "u")
+    code = _dtype_code(X)
+    dX = torch.empty_like(X) if need_dx else None
+    dWg, dWu = (torch.empty_like(Wg), torch.empty_like(Wu)) if need_dw else (None, None)
+    if workspace is None:
+        workspace = _workspace(_gated_bytes(GATED_BACKWARD, code, N, D, F), X.device)
+    wp, wb = _ws(workspace)
+    _check(lib().cci_gated_linear_backward(dH.data_ptr(), X.data_ptr(), code, N, D, Wg.data_ptr(), Wu.data_ptr(), F,
+                                           _act_code(act), g.data_ptr(), u.data_ptr(),
+                                           dX.data_ptr() if need_dx else None, dWg.data_ptr() if need_dw else None,
+                                           dWu.data_ptr() if need_dw else None,
+                                           status.data_ptr() if status is not None else None, wp, wb,
+                                           _stream(X.device)), "cci_gated_linear_backward")
+    return dX, dWg, dWu
 
 
 def _like(t: torch.Tensor, shape, dtype: torch.dtype, name: str) -> None:

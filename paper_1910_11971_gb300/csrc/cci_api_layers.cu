@@ -96,3 +96,126 @@ cci_status cci_token_logprobs_backward(const void *logits, cci_dtype dtype, int6
 }
 
 }  // extern "C"
+
+namespace {
+
+// sizes and pointers that every call of the gated block has
+cci_status check_gated(int dtype, int64_t N, int64_t D, int64_t F, int act, const void *X, const void *Wg,
+                       const void *Wu, const void *workspace, size_t bytes, int call)
+{
+    constexpr int64_t lim = int64_t(1) << 30;  // tile coordinates are 32-bit
+    if (!valid_dtype(dtype)) return CCI_ERR_DTYPE;
+    if (!Wg || !Wu || (N > 0 && !X)) return CCI_ERR_NULL;
+    if (N < 0 || D < 1 || F < 1 || N >= lim || D >= lim || F >= lim) return CCI_ERR_SHAPE;
+    if (act < CCI_ACT_SILU || act > CCI_ACT_SIGMOID) return CCI_ERR_VALUE;
+    if (D % 8 != 0 || F % 8 != 0) return CCI_ERR_UNSUPPORTED;
+    if (!aligned(X, 16) || !aligned(Wg, 16) || !aligned(Wu, 16)) return CCI_ERR_ALIGN;
+    const size_t need = N > 0 ? gated_workspace(dtype, N, D, F, call) : 0;
+    if (need > 0 && (!workspace || bytes < need || !aligned(workspace, 16))) return CCI_ERR_WORKSPACE;
+    return CCI_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t cci_gated_workspace_size(cci_gated_call call, cci_dtype dtype, int64_t N, int64_t D, int64_t F)
+{
+    constexpr int64_t lim = int64_t(1) << 30;
+    if (!valid_dtype(dtype) || N < 1 || D < 1 || F < 1 || N >= lim || D >= lim || F >= lim) return 0;
+    if (call < CCI_GATED_FORWARD || call > CCI_GATED_BACKWARD) return 0;
+    return gated_workspace(dtype, N, D, F, call);
+}
+
+cci_status cci_gated_linear(const void *X, cci_dtype dtype, int64_t N, int64_t D, const void *Wg, const void *Wu,
+                            int64_t F, cci_activation act, void *H, float *g, float *u, uint32_t *dev_status,
+                            void *workspace, size_t workspace_bytes, cci_stream_t stream)
+{
+    const cci_status st = check_gated(dtype, N, D, F, act, X, Wg, Wu, workspace, workspace_bytes, CCI_GATED_FORWARD);
+    if (st != CCI_OK) return st;
+    if (N > 0 && (!H || !g != !u)) return CCI_ERR_NULL;
+    if (!aligned(H, 16) || !aligned(g, 16) || !aligned(u, 16)) return CCI_ERR_ALIGN;
+    if (N == 0) return CCI_OK;
+    GatedArgs a{};
+    a.X = X;
+    a.dtype = dtype;
+    a.N = N;
+    a.D = D;
+    a.F = F;
+    a.Wg = Wg;
+    a.Wu = Wu;
+    a.act = act;
+    a.H = H;
+    a.g = g;
+    a.u = u;
+    a.status = dev_status;
+    a.workspace = workspace;
+    return to_status(launch_gated(a, as_stream(stream)));
+}
+
+cci_status cci_gated_linear_packed(const void *X, cci_dtype dtype, int64_t N, int64_t D, const void *gate_values,
+                                   const uint8_t *gate_idx, const void *up_values, const uint8_t *up_idx, int64_t F,
+                                   int G, int K, cci_activation act, void *H, uint32_t *dev_status, void *workspace,
+                                   size_t workspace_bytes, cci_stream_t stream)
+{
+    if (!gate_idx || !up_idx) return valid_dtype(dtype) ? CCI_ERR_NULL : CCI_ERR_DTYPE;
+    const cci_status st = check_gated(dtype, N, D, F, act, X, gate_values, up_values, workspace, workspace_bytes,
+                                      CCI_GATED_PACKED);
+    if (st != CCI_OK) return st;
+    const cci_status gr = check_group(F, G, K);
+    if (gr != CCI_OK) return gr;
+    if (N > 0 && !H) return CCI_ERR_NULL;
+    if (!aligned(H, 16)) return CCI_ERR_ALIGN;
+    if (N == 0) return CCI_OK;
+    GatedArgs a{};
+    a.X = X;
+    a.dtype = dtype;
+    a.N = N;
+    a.D = D;
+    a.F = F;
+    a.Wg = gate_values;
+    a.Wu = up_values;
+    a.gate_idx = gate_idx;
+    a.up_idx = up_idx;
+    a.G = G;
+    a.K = K;
+    a.act = act;
+    a.H = H;
+    a.status = dev_status;
+    a.workspace = workspace;
+    return to_status(launch_gated(a, as_stream(stream)));
+}
+
+cci_status cci_gated_linear_backward(const void *dH, const void *X, cci_dtype dtype, int64_t N, int64_t D,
+                                     const void *Wg, const void *Wu, int64_t F, cci_activation act, const float *g,
+                                     const float *u, void *dX, void *dWg, void *dWu, uint32_t *dev_status,
+                                     void *workspace, size_t workspace_bytes, cci_stream_t stream)
+{
+    const cci_status st = check_gated(dtype, N, D, F, act, X, Wg, Wu, workspace, workspace_bytes, CCI_GATED_BACKWARD);
+    if (st != CCI_OK) return st;
+    if (N > 0 && (!dH || !g || !u)) return CCI_ERR_NULL;
+    if (!dWg != !dWu) return CCI_ERR_NULL;
+    if (!aligned(dH, 16) || !aligned(g, 16) || !aligned(u, 16) || !aligned(dX, 16) || !aligned(dWg, 16) ||
+        !aligned(dWu, 16))
+        return CCI_ERR_ALIGN;
+    GatedArgs a{};
+    a.X = X;
+    a.dtype = dtype;
+    a.N = N;
+    a.D = D;
+    a.F = F;
+    a.Wg = Wg;
+    a.Wu = Wu;
+    a.act = act;
+    a.g = const_cast<float *>(g);
+    a.u = const_cast<float *>(u);
+    a.dH = dH;
+    a.dX = dX;
+    a.dWg = dWg;
+    a.dWu = dWu;
+    a.status = dev_status;
+    a.workspace = workspace;
+    return to_status(launch_gated_backward(a, as_stream(stream)));
+}
+
+}  // extern "C"

@@ -1,0 +1,327 @@
+// cci_gated.cu -- the gated feed-forward block: what surrounds its tensor-core products
+// (cci_gated.cuh).
+//
+//   planes    fp32 matrices as three bf16 planes, once per call (memory bound: 4 bytes read and 6
+//             written an element)
+//   expand    both packed weight matrices (values, idx) to dense bf16, or to those planes
+//   slopes    dg = dh u act'(g), du = dh act(g) from the saved fp32 g and u, rounded to bf16 (or split
+//             into planes), the operands of the gradients' products (memory bound: 14 bytes an
+//             element in bf16).  g and u are saved in fp32, not rounded to bf16: with them rounded too
+//             the gradients would carry three roundings to 8 bits where one is unavoidable
+#include "cci_gated.cuh"
+#include "cci_rowops.cuh"
+
+namespace cci {
+namespace gated {
+
+constexpr size_t round256(size_t b) { return (b + 255) / 256 * 256; }
+
+// v as three bf16: each the nearest of what the ones before leave.  A value that does not fit (inf,
+// NaN) is its first plane alone, and one that would round up to inf is cut
+__device__ __forceinline__ void split3(float v, uint32_t (&p)[3])
+{
+    uint32_t b = row::bf16x2(v, 0.f) & 0xffffu;
+    if ((b & 0x7f80u) == 0x7f80u && fabsf(v) <= 3.402823466e38f) b = (__float_as_uint(v) >> 16);
+    p[0] = b;
+    const bool whole = (b & 0x7f80u) != 0x7f80u;
+    const float r1 = whole ? v - __uint_as_float(b << 16) : 0.f;
+    p[1] = row::bf16x2(r1, 0.f) & 0xffffu;
+    const float r2 = r1 - __uint_as_float(p[1] << 16);
+    p[2] = row::bf16x2(r2, 0.f) & 0xffffu;
+}
+
+// eight values to their places in one plane or three, `plane` elements apart
+template <int P>
+__device__ __forceinline__ void store_planes(uint16_t *out, int64_t plane, const float (&v)[8])
+{
+    if constexpr (P == 1) {
+        row::store<uint16_t, 8>(out, v);
+    } else {
+        uint32_t w[3][4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            uint32_t a[3], b[3];
+            split3(v[2 * j], a);
+            split3(v[2 * j + 1], b);
+#pragma unroll
+            for (int q = 0; q < 3; ++q) w[q][j] = a[q] | b[q] << 16;
+        }
+#pragma unroll
+        for (int q = 0; q < 3; ++q)
+            *reinterpret_cast<uint4 *>(out + q * plane) = make_uint4(w[q][0], w[q][1], w[q][2], w[q][3]);
+    }
+}
+
+// up to three matrices in one launch: blockIdx.y is the matrix
+struct PlaneJobs {
+    const float *in[3];
+    uint16_t *out[3];
+    int64_t n[3];  // elements, a multiple of 8
+};
+
+__global__ void __launch_bounds__(256) planes_kernel(PlaneJobs j)
+{
+    const float *in = j.in[blockIdx.y];
+    uint16_t *out = j.out[blockIdx.y];
+    const int64_t n = j.n[blockIdx.y];
+    for (int64_t i = (static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x) * 8; i < n;
+         i += static_cast<int64_t>(gridDim.x) * 2048) {
+        float v[8];
+        row::unpack<float, 8>(row::load_once<float, 8>(in + i), v);
+        store_planes<3>(out + i, n, v);
+    }
+}
+
+// ---- packed weights -> dense, one group of G rows and `cols` columns a block; blockIdx.y: gate, up ----
+struct ExpandJob {
+    const void *values[2];
+    const uint8_t *idx[2];
+    uint16_t *out[2];
+    int64_t F, D;
+    int G, K, cols, col_blocks;
+    uint32_t *status;
+};
+
+template <typename T>
+__global__ void __launch_bounds__(256) expand_kernel(ExpandJob j)
+{
+    extern __shared__ __align__(16) unsigned char tile_raw[];
+    T *tile = reinterpret_cast<T *>(tile_raw);  // [G][cols]
+    const int which = blockIdx.y, G = j.G, K = j.K, cols = j.cols;
+    const int64_t group = blockIdx.x / j.col_blocks, d0 = static_cast<int64_t>(blockIdx.x % j.col_blocks) * cols;
+    const int n = j.D - d0 < cols ? static_cast<int>(j.D - d0) : cols;
+    for (int i = threadIdx.x; i < G * cols * static_cast<int>(sizeof(T)) / 16; i += 256)
+        reinterpret_cast<uint4 *>(tile)[i] = make_uint4(0u, 0u, 0u, 0u);
+    __syncthreads();
+    const int64_t at = (group * j.D + d0) * K;
+    const T *values = static_cast<const T *>(j.values[which]) + at;
+    const uint8_t *idx = j.idx[which] + at;
+    bool bad = false;
+    for (int i = threadIdx.x; i < n * K; i += 256) {
+        const int c = i / K, k = i - c * K, r = idx[i];
+        bad |= r >= G || (k > 0 && r <= idx[i - 1]);
+        if (r < G) tile[r * cols + c] = values[i];
+    }
+    if (bad) report(j.status, CCI_ERR_INDEX);
+    __syncthreads();
+    uint16_t *out = j.out[which] + group * G * j.D + d0;
+    const int words = n / 8;  // D is a multiple of 8
+    for (int i = threadIdx.x; i < G * words; i += 256) {
+        const int r = i / words, c = (i - r * words) * 8;
+        if constexpr (sizeof(T) == 2) {
+            *reinterpret_cast<uint4 *>(out + r * j.D + c) = *reinterpret_cast<const uint4 *>(tile + r * cols + c);
+        } else {
+            float v[8];
+            row::unpack<float, 8>(row::load<float, 8>(reinterpret_cast<const float *>(tile) + r * cols + c), v);
+            store_planes<3>(out + r * j.D + c, j.F * j.D, v);
+        }
+    }
+}
+
+// ---- dg and du ----
+template <typename T, int P>
+__global__ void __launch_bounds__(256)
+    slopes_kernel(const T *dh, const float *g, const float *u, int64_t n, int act, uint16_t *dg, uint16_t *du)
+{
+    for (int64_t i = (static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x) * 8; i < n;
+         i += static_cast<int64_t>(gridDim.x) * 2048) {
+        float h[8], gv[8], uv[8];
+        row::unpack<T, 8>(row::load_once<T, 8>(dh + i), h);
+        row::unpack<float, 8>(row::load_once<float, 8>(g + i), gv);
+        row::unpack<float, 8>(row::load_once<float, 8>(u + i), uv);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            float a;
+            const float s = slope_of(gv[j], act, a);
+            gv[j] = h[j] * uv[j] * s;
+            uv[j] = h[j] * a;
+        }
+        store_planes<P>(dg + i, n, gv);
+        store_planes<P>(du + i, n, uv);
+    }
+}
+
+unsigned grid_of(int64_t n)
+{
+    const int64_t blocks = (n / 8 + 255) / 256, most = static_cast<int64_t>(ws::sm_count()) * 8;
+    return static_cast<unsigned>(blocks < 1 ? 1 : (blocks < most ? blocks : most));
+}
+
+// places in the workspace (bytes from its start; 0 sized where a call does not need one)
+struct Layout {
+    size_t x, wg, wu, dg, du, total;
+};
+
+Layout layout(int dtype, int64_t N, int64_t D, int64_t F, int call)
+{
+    const bool f32 = dtype == CCI_F32;
+    const size_t planes = f32 ? 3 : 1;
+    const bool dense = f32 || call == CCI_GATED_PACKED;  // weights laid out here
+    Layout l{};
+    size_t at = 0;
+    auto take = [&](bool need, int64_t n) {
+        const size_t here = at;
+        if (need) at += round256(static_cast<size_t>(n) * 2 * planes);
+        return here;
+    };
+    l.x = take(f32, N * D);
+    l.wg = take(dense, F * D);
+    l.wu = take(dense, F * D);
+    l.dg = take(call == CCI_GATED_BACKWARD, N * F);
+    l.du = take(call == CCI_GATED_BACKWARD, N * F);
+    l.total = at;
+    return l;
+}
+
+cudaError_t split(const float *const *in, uint16_t *const *out, const int64_t *n, int jobs, cudaStream_t stream)
+{
+    PlaneJobs j{};
+    int64_t most = 0;
+    for (int i = 0; i < jobs; ++i) {
+        j.in[i] = in[i];
+        j.out[i] = out[i];
+        j.n[i] = n[i];
+        most = n[i] > most ? n[i] : most;
+    }
+    planes_kernel<<<dim3(grid_of(most), static_cast<unsigned>(jobs)), 256, 0, stream>>>(j);
+    return cudaGetLastError();
+}
+
+}  // namespace gated
+
+size_t gated_workspace(int dtype, int64_t N, int64_t D, int64_t F, int call)
+{
+    return gated::layout(dtype, N, D, F, call).total;
+}
+
+cudaError_t launch_gated(const GatedArgs &a, cudaStream_t stream)
+{
+    using namespace gated;
+    const bool f32 = a.dtype == CCI_F32, packed = a.gate_idx != nullptr;
+    const Layout l = layout(a.dtype, a.N, a.D, a.F, packed ? CCI_GATED_PACKED : CCI_GATED_FORWARD);
+    char *base = static_cast<char *>(a.workspace);
+    const void *x = a.X, *wg = a.Wg, *wu = a.Wu;
+    if (packed) {
+        ExpandJob j{};
+        j.values[0] = a.Wg;
+        j.values[1] = a.Wu;
+        j.idx[0] = a.gate_idx;
+        j.idx[1] = a.up_idx;
+        j.out[0] = reinterpret_cast<uint16_t *>(base + l.wg);
+        j.out[1] = reinterpret_cast<uint16_t *>(base + l.wu);
+        j.F = a.F;
+        j.D = a.D;
+        j.G = a.G;
+        j.K = a.K;
+        // a tile of at most 32 KB
+        j.cols = a.G <= 32 ? 256 : (a.G <= 64 ? 128 : (a.G <= 128 ? 64 : 32));
+        j.status = a.status;
+        j.col_blocks = static_cast<int>((a.D + j.cols - 1) / j.cols);
+        const int64_t blocks = a.F / a.G * j.col_blocks;
+        if (blocks > 0x7fffffff) return cudaErrorInvalidValue;
+        const dim3 grid(static_cast<unsigned>(blocks), 2);
+        const size_t bytes = static_cast<size_t>(a.G) * j.cols * (f32 ? 4 : 2);
+        if (f32)
+            expand_kernel<float><<<grid, 256, bytes, stream>>>(j);
+        else
+            expand_kernel<uint16_t><<<grid, 256, bytes, stream>>>(j);
+        const cudaError_t e = cudaGetLastError();
+        if (e != cudaSuccess) return e;
+        wg = base + l.wg;
+        wu = base + l.wu;
+    }
+    if (f32) {
+        const float *in[3] = {static_cast<const float *>(a.X), static_cast<const float *>(a.Wg),
+                              static_cast<const float *>(a.Wu)};
+        uint16_t *out[3] = {reinterpret_cast<uint16_t *>(base + l.x), reinterpret_cast<uint16_t *>(base + l.wg),
+                            reinterpret_cast<uint16_t *>(base + l.wu)};
+        const int64_t n[3] = {a.N * a.D, a.F * a.D, a.F * a.D};
+        const cudaError_t e = split(in, out, n, packed ? 1 : 3, stream);
+        if (e != cudaSuccess) return e;
+        x = base + l.x;
+        wg = base + l.wg;
+        wu = base + l.wu;
+    }
+    const int planes = f32 ? 3 : 1;
+    Job j{};
+    j.a[0] = Operand{x, a.N, a.D, planes};
+    j.b[0] = Operand{wg, a.F, a.D, planes};
+    j.b[1] = Operand{wu, a.F, a.D, planes};
+    j.out[0] = a.H;
+    j.save[0] = a.g;
+    j.save[1] = a.u;
+    j.M = a.N;
+    j.N = a.F;
+    j.K = a.D;
+    j.terms = f32 ? 6 : 1;
+    j.act = a.act;
+    j.out_f32 = f32;
+    j.status = a.status;
+    return launch_forward(j, stream);
+}
+
+cudaError_t launch_gated_backward(const GatedArgs &a, cudaStream_t stream)
+{
+    using namespace gated;
+    const bool f32 = a.dtype == CCI_F32;
+    if (a.N == 0) {  // no rows to sum over
+        const size_t bytes = static_cast<size_t>(a.F) * a.D * (f32 ? 4 : 2);
+        cudaError_t e = a.dWg ? cudaMemsetAsync(a.dWg, 0, bytes, stream) : cudaSuccess;
+        if (e == cudaSuccess && a.dWu) e = cudaMemsetAsync(a.dWu, 0, bytes, stream);
+        return e;
+    }
+    const Layout l = layout(a.dtype, a.N, a.D, a.F, CCI_GATED_BACKWARD);
+    char *base = static_cast<char *>(a.workspace);
+    uint16_t *dg = reinterpret_cast<uint16_t *>(base + l.dg), *du = reinterpret_cast<uint16_t *>(base + l.du);
+    const int64_t n = a.N * a.F;
+    if (f32)
+        slopes_kernel<float, 3><<<grid_of(n), 256, 0, stream>>>(static_cast<const float *>(a.dH), a.g, a.u, n, a.act,
+                                                                dg, du);
+    else
+        slopes_kernel<uint16_t, 1><<<grid_of(n), 256, 0, stream>>>(static_cast<const uint16_t *>(a.dH), a.g, a.u, n,
+                                                                   a.act, dg, du);
+    cudaError_t e = cudaGetLastError();
+    if (e != cudaSuccess) return e;
+    const void *x = a.X, *wg = a.Wg, *wu = a.Wu;
+    if (f32) {
+        const float *in[3] = {static_cast<const float *>(a.X), static_cast<const float *>(a.Wg),
+                              static_cast<const float *>(a.Wu)};
+        uint16_t *out[3] = {reinterpret_cast<uint16_t *>(base + l.x), reinterpret_cast<uint16_t *>(base + l.wg),
+                            reinterpret_cast<uint16_t *>(base + l.wu)};
+        const int64_t count[3] = {a.N * a.D, a.F * a.D, a.F * a.D};
+        e = split(in, out, count, 3, stream);
+        if (e != cudaSuccess) return e;
+        x = base + l.x;
+        wg = base + l.wg;
+        wu = base + l.wu;
+    }
+    const int planes = f32 ? 3 : 1;
+    Job j{};
+    j.terms = f32 ? 6 : 1;
+    j.out_f32 = f32;
+    j.status = a.status;
+    j.a[0] = Operand{dg, a.N, a.F, planes};
+    j.a[1] = Operand{du, a.N, a.F, planes};
+    if (a.dX) {
+        j.b[0] = Operand{wg, a.F, a.D, planes};
+        j.b[1] = Operand{wu, a.F, a.D, planes};
+        j.out[0] = a.dX;
+        j.M = a.N;
+        j.N = a.D;
+        j.K = a.F;
+        e = launch_dx(j, stream);
+        if (e != cudaSuccess) return e;
+    }
+    if (a.dWg) {
+        j.b[0] = Operand{x, a.N, a.D, planes};
+        j.out[0] = a.dWg;
+        j.out[1] = a.dWu;
+        j.M = a.F;
+        j.N = a.D;
+        j.K = a.N;
+        e = launch_dw(j, stream);
+    }
+    return e;
+}
+
+}  // namespace cci

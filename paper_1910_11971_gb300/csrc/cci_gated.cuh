@@ -1,0 +1,688 @@
+// cci_gated.cuh -- the tensor-core products of the gated feed-forward block.
+//
+//   forward   g = X Wg^T, u = X Wu^T, h = act(g) * u in one kernel: an output tile holds the gate's
+//             and the up projection's accumulators of the same channels side by side in tensor
+//             memory, and the epilogue joins them.  X [N][D], W [F][D]: both K-major.
+//   dX        dg Wg + du Wu: one reduction over both pairs, 2 F long.  dg, du [N][F] K-major; the
+//             weights' rows run along the output, so they are read MN-major (no transposed copy).
+//   dW        dg^T X and du^T X in one launch, the reduction over the tokens: both operands MN-major.
+//
+// Operands are bf16 with fp32 accumulators (tcgen05.mma kind::f16).  fp32 tensors come as three bf16
+// planes, v = v1 + v2 + v3 with v1 the nearest bf16 of v and so on (each takes 8 bits of the 24): the
+// reduction runs over the six products of planes down to 2^-18 of the whole, the smallest
+// first; what is left out is below 2^-25 |a||b|.  Six bf16 products beat fp32 on the CUDA cores
+// (80 TFLOP/s against 1887 / 6) and keep its accuracy, which one tf32 product would not.
+//
+// Tiles: 256 x 256 over a CTA pair (each CTA holds its 128 rows of A and half of B; the even CTA
+// issues), or 128 x 128 and 128 x 64 on one CTA where there is little to do.  Both operands are copied
+// by TMA into 128-byte-swizzled stages 64 deep; two accumulators in tensor memory, so that one tile's
+// epilogue runs beside the next one's products; a persistent grid walks the tiles eight M tiles at
+// a time, so that what the SMs read at once stays in L2.
+//
+// Roles: warp 0 copies, warp 1 issues the MMAs, warp 2 holds the tensor memory, warps 4-7 write the
+// output through shared memory by TMA, which clips ragged edges.  Every wait is bounded: on expiry
+// the status word gets CCI_ERR_TIMEOUT, the other roles stop, and the block leaves when its copies
+// and products have ended.
+#pragma once
+
+#include "cci_gemm_ws.cuh"
+
+namespace cci {
+namespace gated {
+
+enum Mode { kForward = 0, kDx = 1, kDw = 2 };
+
+// everything a launch needs but its tensor maps
+struct Params {
+    int64_t M, N;        // output rows and columns (forward: N = F)
+    int k_stages;        // 64-deep stages of one reduction
+    int pairs;           // reductions added up: 2 for dX (gate, up), else 1
+    int terms;           // products of planes: 1 (bf16) or 6 (fp32)
+    int a_rows;          // rows of A's box (K-major): 128, or fewer where the matrix has fewer
+    int m_tiles;         // of one output (dW has two)
+    int n_tiles;
+    int tiles;
+    int act;             // cci_activation
+    int out_f32;
+    int save;            // forward: g and u are written too (fp32)
+    uint32_t *status;
+};
+
+// [0] gate, [1] up where an operand or output is one of two
+struct Maps {
+    CUtensorMap a[2], b[2], out[2];
+    CUtensorMap save[2];
+};
+
+template <int CG, int BN>
+struct Cfg {
+    static constexpr int kM = 128;            // rows of a CTA
+    static constexpr int kBRows = BN / CG;    // rows of B that a CTA holds
+    static constexpr int kABytes = kM * 128, kBBytes = kBRows * 128;
+    static constexpr int kStage = kABytes + kBBytes;
+    static constexpr int kOut = kM * 128;     // an output buffer: 128 rows of 128 bytes
+    static constexpr int kOuts = 2;
+    static constexpr int kFit = (static_cast<int>(kMaxSmemPerBlock) - 2048 - kOuts * kOut) / kStage;
+    static constexpr int kStages = kFit < 8 ? kFit : 8;
+    static constexpr int kTmem = 2 * BN;
+    static constexpr int kThreads = 256;
+    static constexpr size_t kSmem = 1024 + static_cast<size_t>(kStages) * kStage + kOuts * kOut + 1024;
+    static_assert(kStage % 1024 == 0 && kStages >= 4 && kSmem <= kMaxSmemPerBlock, "stages");
+    static_assert(kTmem == 128 || kTmem == 256 || kTmem == 512, "tensor memory comes in powers of two");
+};
+
+struct Smem {
+    uint64_t full[8], empty[8];
+    uint64_t acc_full[2], acc_empty[2];
+    uint64_t drain;
+    uint32_t tmem_base;
+    int abort;
+};
+static_assert(sizeof(Smem) <= 1024, "barriers");
+
+// ---- activations, in fp32 ----
+__device__ __forceinline__ float sigmoid(float g) { return 1.f / (1.f + expf(-g)); }
+
+__device__ __forceinline__ float act_of(float g, int act)
+{
+    switch (act) {
+        case CCI_ACT_SILU: return g / (1.f + expf(-g));
+        case CCI_ACT_GELU: return 0.5f * g * erfcf(g * -0.70710678f);
+        case CCI_ACT_GELU_TANH: return g * sigmoid(1.5957691f * (g + 0.044715f * g * g * g));
+        case CCI_ACT_RELU: return g > 0.f ? g : (g != g ? g : 0.f);
+        default: return sigmoid(g);
+    }
+}
+
+// act'(g), act(g) to a
+__device__ __forceinline__ float slope_of(float g, int act, float &a)
+{
+    switch (act) {
+        case CCI_ACT_SILU: {
+            const float p = sigmoid(g);
+            a = act_of(g, act);
+            return p * (1.f + g * (1.f - p));
+        }
+        case CCI_ACT_GELU: {
+            const float c = 0.5f * erfcf(g * -0.70710678f);
+            a = g * c;
+            return c + g * 0.39894228f * expf(-0.5f * g * g);
+        }
+        case CCI_ACT_GELU_TANH: {
+            // 0.5 (1 + tanh(z)) = sigmoid(2 z)
+            const float g2 = g * g, p = sigmoid(1.5957691f * (g + 0.044715f * g2 * g));
+            a = g * p;
+            return p + g * p * (1.f - p) * 1.5957691f * (1.f + 3.f * 0.044715f * g2);
+        }
+        case CCI_ACT_RELU: a = act_of(g, act); return g > 0.f ? 1.f : 0.f;
+        default: {
+            const float p = sigmoid(g);
+            a = p;
+            return p * (1.f - p);
+        }
+    }
+}
+
+// ---- tensor core ----
+// shared-memory descriptor of a tile with the 128-byte swizzle.  K-major: rows of 128 bytes, 8-row
+// atoms of 1024 (stride offset).  MN-major: rows of 64 outputs (128 bytes) for one k, 8 k to an atom
+// (stride offset 1024), the next 64 outputs 64 rows further (leading offset 8192)
+template <bool MN>
+__device__ __forceinline__ uint64_t tile_desc(uint32_t addr)
+{
+    uint64_t d = 0;
+    d |= static_cast<uint64_t>((addr & 0x3ffff) >> 4);
+    d |= static_cast<uint64_t>(MN ? 8192 >> 4 : 1) << 16;
+    d |= static_cast<uint64_t>(1024 >> 4) << 32;
+    d |= static_cast<uint64_t>(1) << 46;
+    d |= static_cast<uint64_t>(2) << 61;
+    return d;
+}
+
+// the four 16-deep products of a 64-deep stage, and the commit that frees the stage (in both CTAs of a
+// pair).  kA, kB: descriptor steps of 16 reduction indices (32 bytes K-major, 16 rows MN-major)
+template <int CG, uint32_t kIdesc, int kA, int kB>
+__device__ __forceinline__ void stage_mma(uint32_t d, uint64_t a, uint64_t b, uint32_t acc, uint32_t bar)
+{
+    if constexpr (CG == 2)
+        asm volatile(
+            "{\n.reg .pred pa, pt;\n.reg .b64 x, y;\n"
+            "setp.ne.b32 pa, %3, 0;\nsetp.eq.b32 pt, 0, 0;\n"
+            "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %4, pa;\n"
+            "add.s64 x, %1, %7;\nadd.s64 y, %2, %8;\n"
+            "tcgen05.mma.cta_group::2.kind::f16 [%0], x, y, %4, pt;\n"
+            "add.s64 x, x, %7;\nadd.s64 y, y, %8;\n"
+            "tcgen05.mma.cta_group::2.kind::f16 [%0], x, y, %4, pt;\n"
+            "add.s64 x, x, %7;\nadd.s64 y, y, %8;\n"
+            "tcgen05.mma.cta_group::2.kind::f16 [%0], x, y, %4, pt;\n"
+            "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%5], %6;\n}\n" ::"r"(d),
+            "l"(a), "l"(b), "r"(acc), "n"(kIdesc), "r"(bar), "h"(static_cast<uint16_t>(3)), "n"(kA), "n"(kB)
+            : "memory");
+    else
+        asm volatile(
+            "{\n.reg .pred pa, pt;\n.reg .b64 x, y;\n"
+            "setp.ne.b32 pa, %3, 0;\nsetp.eq.b32 pt, 0, 0;\n"
+            "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %4, pa;\n"
+            "add.s64 x, %1, %6;\nadd.s64 y, %2, %7;\n"
+            "tcgen05.mma.cta_group::1.kind::f16 [%0], x, y, %4, pt;\n"
+            "add.s64 x, x, %6;\nadd.s64 y, y, %7;\n"
+            "tcgen05.mma.cta_group::1.kind::f16 [%0], x, y, %4, pt;\n"
+            "add.s64 x, x, %6;\nadd.s64 y, y, %7;\n"
+            "tcgen05.mma.cta_group::1.kind::f16 [%0], x, y, %4, pt;\n"
+            "tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%5];\n}\n" ::"r"(d),
+            "l"(a), "l"(b), "r"(acc), "n"(kIdesc), "r"(bar), "n"(kA), "n"(kB)
+            : "memory");
+}
+
+// 3-D tile load (inner element, row, plane); the inner coordinate is a multiple of 64.  CG = 2:
+// completes on the even CTA's barrier (a cluster address)
+template <int CG>
+__device__ __forceinline__ void load_3d(uint32_t dst, const CUtensorMap *map, int c0, int c1, int c2, uint32_t bar)
+{
+    if constexpr (CG == 2)
+        asm volatile(
+            "cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, "
+            "{%2, %3, %4}], [%5];" ::"r"(dst),
+            "l"(reinterpret_cast<uint64_t>(map)), "r"(c0), "r"(c1), "r"(c2), "r"(bar)
+            : "memory");
+    else
+        asm volatile(
+            "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, "
+            "%4}], [%5];" ::"r"(dst),
+            "l"(reinterpret_cast<uint64_t>(map)), "r"(c0), "r"(c1), "r"(c2), "r"(bar)
+            : "memory");
+}
+
+// 32 columns of this warp's TMEM lanes, without waiting for them
+__device__ __forceinline__ void tmem_ld32_begin(uint32_t taddr, uint32_t (&v)[32])
+{
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, "
+        "%15, %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+        : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]),
+          "=r"(v[8]), "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15]),
+          "=r"(v[16]), "=r"(v[17]), "=r"(v[18]), "=r"(v[19]), "=r"(v[20]), "=r"(v[21]), "=r"(v[22]), "=r"(v[23]),
+          "=r"(v[24]), "=r"(v[25]), "=r"(v[26]), "=r"(v[27]), "=r"(v[28]), "=r"(v[29]), "=r"(v[30]), "=r"(v[31])
+        : "r"(taddr));
+}
+
+// products of planes (of A, of B) by term, the smallest first
+__device__ __forceinline__ void term_planes(int term, int terms, int &pa, int &pb)
+{
+    // 0 2, 1 1, 2 0, 0 1, 1 0, 0 0: two bits a term
+    pa = terms == 1 ? 0 : (0x124 >> (2 * term)) & 3;
+    pb = terms == 1 ? 0 : (0x046 >> (2 * term)) & 3;
+}
+
+// tile -> M tile (with which output, for dW) and N tile: eight M tiles at a time
+__device__ __forceinline__ void tile_at(const Params &p, int tile, int mt_all, int &mt, int &nt)
+{
+    const int per = 8 * p.n_tiles, g = tile / per, r = tile - g * per;
+    const int gm = mt_all - 8 * g < 8 ? mt_all - 8 * g : 8;
+    nt = r / gm;
+    mt = 8 * g + r - nt * gm;
+}
+
+// SPLIT (fp32, CG = 1): the tensor core cuts, not rounds, its running sum at every addition, an error
+// that grows with the length of the sum (1.9e-5 of the result at 4096 indices and six terms, measured).
+// So it adds kChunk stages at a time, and the output warps add the chunks in registers, to the nearest.
+constexpr int kChunk = 8;
+
+template <int MODE, int CG, int BN, bool SPLIT>
+__global__ void __launch_bounds__(Cfg<CG, BN>::kThreads, 1)
+    product_kernel(const Params p, const __grid_constant__ Maps maps)
+{
+    using C = Cfg<CG, BN>;
+    constexpr bool kAMn = MODE == kDw, kBMn = MODE != kForward;
+    constexpr int kStages = C::kStages;
+    constexpr int kNOut = MODE == kForward ? BN / 2 : BN;  // output columns of a tile
+    constexpr uint32_t kIdesc = (1u << 4) | (1u << 7) | (1u << 10) | (static_cast<uint32_t>(kAMn) << 15) |
+                                (static_cast<uint32_t>(kBMn) << 16) | (static_cast<uint32_t>(BN >> 3) << 17) |
+                                (static_cast<uint32_t>((C::kM * CG) >> 4) << 24);
+    extern __shared__ __align__(16) unsigned char smem_raw[];
+    const uint32_t raw = tc::smem_u32(smem_raw);
+    const uint32_t base = (raw + 1023u) & ~1023u;
+    const uint32_t outs = base + kStages * C::kStage;
+    Smem *S = reinterpret_cast<Smem *>(smem_raw + (outs - raw) + C::kOuts * C::kOut);
+    volatile int *abort = &S->abort;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const uint32_t rank = CG == 2 ? ws::cluster_rank() : 0u;
+    const int first = static_cast<int>(blockIdx.x) / CG, step = static_cast<int>(gridDim.x) / CG;
+    const int mt_all = MODE == kDw ? 2 * p.m_tiles : p.m_tiles;
+    const int per_tile = p.pairs * p.terms * p.k_stages;  // stages of a tile
+    const int chunk_len = SPLIT ? kChunk : per_tile;
+
+    if (tid == 0) {
+        for (int s = 0; s < kStages; ++s) {
+            tc::mbar_init(&S->full[s], 1);
+            tc::mbar_init(&S->empty[s], 1);
+        }
+        for (int a = 0; a < 2; ++a) {
+            tc::mbar_init(&S->acc_full[a], 1);
+            tc::mbar_init(&S->acc_empty[a], 4 * CG);
+        }
+        tc::mbar_init(&S->drain, 1);
+        S->abort = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 2) {
+        if constexpr (CG == 2) {
+            asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(
+                             tc::smem_u32(&S->tmem_base)),
+                         "r"(C::kTmem)
+                         : "memory");
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+        } else {
+            asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(
+                             tc::smem_u32(&S->tmem_base)),
+                         "r"(C::kTmem)
+                         : "memory");
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+        }
+    }
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    if constexpr (CG == 2) ws::cluster_sync();
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    const uint32_t tmem = S->tmem_base;
+
+    if (warp == 0) {
+        // ---- copies
+        if (tc::elect_one()) {
+            const uint32_t a_bytes = kAMn ? static_cast<uint32_t>(C::kABytes) : static_cast<uint32_t>(p.a_rows) * 128u;
+            const uint32_t bytes = CG * (a_bytes + static_cast<uint32_t>(C::kBBytes));
+            int s = 0, it = 0;
+            uint32_t ph = 1u;  // a fresh barrier's preceding phase counts as complete
+            bool ok = true;
+            for (int tile = first; tile < p.tiles && ok; tile += step) {
+                int mt, nt;
+                tile_at(p, tile, mt_all, mt, nt);
+                int which = 0;  // dW: gate or up
+                if (MODE == kDw && mt >= p.m_tiles) {
+                    which = 1;
+                    mt -= p.m_tiles;
+                }
+                const int m0 = (mt * CG + static_cast<int>(rank)) * C::kM;
+                const int n0 = nt * kNOut;
+                for (int pair = 0; pair < p.pairs && ok; ++pair) {
+                    const CUtensorMap *ma = &maps.a[MODE == kDw ? which : pair];
+                    for (int t = 0; t < p.terms && ok; ++t) {
+                        int pa, pb;
+                        term_planes(t, p.terms, pa, pb);
+                        for (int ks = 0; ks < p.k_stages; ++ks, ++it) {
+                            ok = tc::mbar_wait(&S->empty[s], ph, abort, p.status);
+                            if (!ok) break;
+                            const uint32_t sa = base + s * C::kStage, sb = sa + C::kABytes;
+                            uint32_t bar = tc::smem_u32(&S->full[s]);
+                            if (rank == 0) tc::mbar_arrive_expect_tx(&S->full[s], bytes);
+                            if constexpr (CG == 2) bar = ws::map_to_rank(bar, 0);
+                            const int k0 = ks * 64;
+                            if constexpr (kAMn) {
+#pragma unroll
+                                for (int i = 0; i < C::kM / 64; ++i)
+                                    load_3d<CG>(sa + i * 8192, ma, m0 + 64 * i, k0, pa, bar);
+                            } else {
+                                load_3d<CG>(sa, ma, k0, m0, pa, bar);
+                            }
+                            if constexpr (MODE == kForward) {
+                                if constexpr (CG == 2) {
+                                    // the even CTA holds the gate's rows, the odd one the up projection's
+                                    load_3d<CG>(sb, &maps.b[rank], k0, n0, pb, bar);
+                                } else {
+                                    load_3d<CG>(sb, &maps.b[0], k0, n0, pb, bar);
+                                    load_3d<CG>(sb + C::kBBytes / 2, &maps.b[1], k0, n0, pb, bar);
+                                }
+                            } else {
+                                const CUtensorMap *mb = &maps.b[MODE == kDx ? pair : 0];
+                                const int nb = n0 + static_cast<int>(rank) * C::kBRows;
+#pragma unroll
+                                for (int i = 0; i < C::kBRows / 64; ++i)
+                                    load_3d<CG>(sb + i * 8192, mb, nb + 64 * i, k0, pb, bar);
+                            }
+                            if (++s == kStages) {
+                                s = 0;
+                                ph ^= 1u;
+                            }
+                        }
+                    }
+                }
+            }
+            // no copy is in flight when the block ends, also after an abort: the even CTA's barriers
+            // count those of both
+            if (rank == 0) {
+                int no_abort = 0;
+                for (int d = it > kStages ? it - kStages : 0; d < it; ++d)
+                    tc::mbar_wait(&S->full[d % kStages], (d / kStages) & 1, &no_abort, p.status);
+            }
+        }
+        __syncwarp();
+    } else if (warp == 1 && rank == 0) {
+        // ---- products
+        if (tc::elect_one()) {
+            int s = 0, t = 0;
+            uint32_t ph = 0u;
+            bool ok = true;
+            const uint64_t da0 = tile_desc<kAMn>(base), db0 = tile_desc<kBMn>(base + C::kABytes);
+            const uint32_t empty0 = tc::smem_u32(&S->empty[0]);
+            for (int tile = first; tile < p.tiles && ok; tile += step) {
+                for (int left = per_tile; left > 0 && ok; left -= chunk_len, ++t) {
+                    const int acc = t & 1, n = left < chunk_len ? left : chunk_len;
+                    if (t >= 2) ok = tc::mbar_wait<CG == 2>(&S->acc_empty[acc], ((t >> 1) - 1) & 1, abort, p.status);
+                    if (!ok) break;
+                    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                    const uint32_t d = tmem + static_cast<uint32_t>(acc * BN);
+                    for (int i = 0; i < n; ++i) {
+                        ok = tc::mbar_wait(&S->full[s], ph, abort, p.status);
+                        if (!ok) break;
+                        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                        const uint64_t off = static_cast<uint64_t>(s) * (C::kStage >> 4);
+                        stage_mma<CG, kIdesc, kAMn ? 128 : 2, kBMn ? 128 : 2>(d, da0 + off, db0 + off, i > 0 ? 1u : 0u,
+                                                                              empty0 + 8u * s);
+                        if (++s == kStages) {
+                            s = 0;
+                            ph ^= 1u;
+                        }
+                    }
+                    if (ok) {
+                        if constexpr (CG == 2)
+                            ws::mma_commit_pair(&S->acc_full[acc]);
+                        else
+                            tc::mma_commit(&S->acc_full[acc]);
+                    }
+                }
+            }
+            // every product has ended before the tensor memory is given back
+            if constexpr (CG == 2)
+                ws::mma_commit_pair(&S->drain);
+            else
+                tc::mma_commit(&S->drain);
+            int no_abort = 0;
+            tc::mbar_wait(&S->drain, 0, &no_abort, p.status);
+        }
+        __syncwarp();
+    } else if (warp >= 4) {
+        // ---- output: row `m` of the CTA's 128 per thread
+        const int m = tid - 128;
+        const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
+        const uint32_t acc_empty0 = CG == 2 ? ws::map_to_rank(tc::smem_u32(&S->acc_empty[0]), 0) : 0u;
+        int t = 0, stored = 0;
+        bool ok = true;
+        // the next buffer, once the store that last read it has; a buffer's store to `map` at (c0, r0)
+        auto take = [&]() {
+            const uint32_t buf = outs + static_cast<uint32_t>(stored % C::kOuts) * C::kOut;
+            ++stored;
+            if (m == 0) tc::bulk_wait_read<C::kOuts - 1>();
+            tc::named_sync(1, 128);
+            return buf;
+        };
+        auto give = [&](uint32_t buf, const CUtensorMap *map, int c0, int r0) {
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            tc::named_sync(1, 128);
+            if (m == 0) {
+                tc::tma_store_2d(map, buf, c0, r0);
+                tc::bulk_commit();
+            }
+        };
+        // 128 bytes of every row
+        auto put = [&](const uint32_t (&v)[32], const CUtensorMap *map, int c0, int r0) {
+            const uint32_t buf = take();
+#pragma unroll
+            for (int q = 0; q < 8; ++q)
+                ws::st_shared_v4(buf + ws::sw_chunk(m, q), v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]);
+            give(buf, map, c0, r0);
+        };
+        // 64 bytes of every row (tiles of 32 bf16 columns), rows 64 bytes apart without a swizzle
+        auto put_half = [&](const uint32_t (&v)[32], const CUtensorMap *map, int c0, int r0) {
+            const uint32_t buf = take();
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+                ws::st_shared_v4(buf + static_cast<uint32_t>(m) * 64u + 16u * q, v[4 * q], v[4 * q + 1], v[4 * q + 2],
+                                 v[4 * q + 3]);
+            give(buf, map, c0, r0);
+        };
+        // accumulator t of this CTA: waited for, and given back once read
+        auto acc_wait = [&]() {
+            bool done = tc::mbar_wait(&S->acc_full[t & 1], (t >> 1) & 1, abort, p.status);
+            done = tc::named_and(1, 128, done);
+            __syncwarp();
+            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+            return done;
+        };
+        auto acc_free = [&]() {
+            asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+            __syncwarp();
+            if (lane == 0) {
+                if (CG == 2 && rank != 0)
+                    ws::mbar_arrive_remote(acc_empty0 + static_cast<uint32_t>((t & 1) * sizeof(uint64_t)));
+                else
+                    tc::mbar_arrive(&S->acc_empty[t & 1]);
+            }
+            ++t;
+        };
+        for (int tile = first; tile < p.tiles && ok; tile += step) {
+            int mt, nt;
+            tile_at(p, tile, mt_all, mt, nt);
+            int which = 0;
+            if (MODE == kDw && mt >= p.m_tiles) {
+                which = 1;
+                mt -= p.m_tiles;
+            }
+            const int r0 = (mt * CG + static_cast<int>(rank)) * C::kM, n0 = nt * kNOut;
+            const bool rows = r0 < p.M;  // the odd CTA's rows may all lie past the matrix
+            const int cols = p.N - n0 < kNOut ? static_cast<int>(p.N - n0) : kNOut;
+            uint32_t o[32];
+            // 32 finished columns from c on (forward: v the gate's, u the up projection's)
+            auto output = [&](int c, uint32_t (&v)[32], const uint32_t (&u)[32]) {
+                if constexpr (MODE == kForward) {
+                    if (p.save) {
+                        put(v, &maps.save[0], n0 + c, r0);
+                        put(u, &maps.save[1], n0 + c, r0);
+                    }
+#pragma unroll
+                    for (int j = 0; j < 32; ++j)
+                        v[j] = __float_as_uint(act_of(__uint_as_float(v[j]), p.act) * __uint_as_float(u[j]));
+                }
+                if (p.out_f32) {
+                    put(v, &maps.out[which], n0 + c, r0);
+                } else if constexpr (kNOut == 32) {
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) o[j] = ws::bf16x2_rn(v[2 * j], v[2 * j + 1]);
+                    put_half(o, &maps.out[which], n0 + c, r0);
+                } else if (c & 32) {
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) o[16 + j] = ws::bf16x2_rn(v[2 * j], v[2 * j + 1]);
+                    put(o, &maps.out[which], n0 + c - 32, r0);
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) o[j] = ws::bf16x2_rn(v[2 * j], v[2 * j + 1]);
+                    if (c + 32 >= cols) {
+#pragma unroll
+                        for (int j = 16; j < 32; ++j) o[j] = 0u;
+                        put(o, &maps.out[which], n0 + c, r0);
+                    }
+                }
+            };
+            if constexpr (SPLIT) {
+                uint32_t sum[BN / 32][32];
+#pragma unroll
+                for (int q = 0; q < BN / 32; ++q)
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) sum[q][j] = 0u;
+                for (int left = per_tile; left > 0 && ok; left -= chunk_len) {
+                    ok = acc_wait();
+                    if (!ok) break;
+#pragma unroll
+                    for (int q = 0; q < BN / 32; ++q) {
+                        uint32_t v[32];
+                        tmem_ld32_begin(tmem + lanes + static_cast<uint32_t>((t & 1) * BN + 32 * q), v);
+                        asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+                        for (int j = 0; j < 32; ++j)
+                            sum[q][j] = __float_as_uint(__uint_as_float(sum[q][j]) + __uint_as_float(v[j]));
+                    }
+                    acc_free();
+                }
+                if (!ok) break;
+#pragma unroll
+                for (int q = 0; q < kNOut / 32; ++q)
+                    if (32 * q < cols && rows) output(32 * q, sum[q], sum[(MODE == kForward ? kNOut / 32 : 0) + q]);
+            } else {
+                ok = acc_wait();
+                if (!ok) break;
+                const uint32_t col0 = tmem + lanes + static_cast<uint32_t>((t & 1) * BN);
+                for (int c = 0; c < cols && rows; c += 32) {
+                    uint32_t v[32], u[32];
+                    tmem_ld32_begin(col0 + c, v);
+                    if constexpr (MODE == kForward) tmem_ld32_begin(col0 + kNOut + c, u);
+                    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+                    output(c, v, u);
+                }
+                acc_free();
+            }
+        }
+        if (m == 0) tc::bulk_wait_all();
+    }
+
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    if constexpr (CG == 2) {
+        // the last commit signals this CTA's barrier too: it has arrived before either CTA leaves
+        if (rank != 0 && tid == 0) {
+            int no_abort = 0;
+            tc::mbar_wait(&S->drain, 0, &no_abort, p.status);
+        }
+        __syncwarp();
+        ws::cluster_sync();
+    }
+    if (warp == 2) {
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        if constexpr (CG == 2)
+            asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(C::kTmem) : "memory");
+        else
+            asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(C::kTmem) : "memory");
+    }
+}
+
+// ---------------------------------------------------------------------------
+// host
+// ---------------------------------------------------------------------------
+
+// one operand: a row-major matrix [rows][cols] of bf16 in `planes` planes, one after the other
+struct Operand {
+    const void *data;
+    int64_t rows, cols;
+    int planes;
+};
+
+// copies of 64 (swizzled 128-byte rows) x box_rows
+inline bool operand_map(CUtensorMap *m, const Operand &o, int box_rows)
+{
+    const int64_t dims[3] = {o.cols, o.rows, o.planes};
+    const int64_t strides[2] = {o.cols * 2, o.cols * o.rows * 2};
+    const int box[3] = {64, box_rows, 1};
+    return ws::make_map_strided(m, o.data, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, dims, strides, box);
+}
+
+// stores of `width` columns x 128 rows into [rows][cols]: 128 swizzled bytes a row, or 64 plain ones
+inline bool output_map(CUtensorMap *m, void *data, bool f32, int64_t rows, int64_t cols, int width)
+{
+    const int es = f32 ? 4 : 2;
+    const int64_t dims[2] = {cols, rows}, strides[1] = {cols * es};
+    const int box[2] = {width, 128};
+    return ws::make_map_strided(m, data, f32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2,
+                                dims, strides, box, width * es == 128);
+}
+
+// a launch: `a`, `b` and `out` with two entries where there are two
+struct Job {
+    Operand a[2], b[2];
+    void *out[2];
+    float *save[2];   // forward: g and u, or null
+    int64_t M, N, K;  // rows and columns of an output, length of a reduction
+    int terms, act, out_f32;
+    uint32_t *status;
+};
+
+template <int MODE, int CG, int BN, bool SPLIT>
+cudaError_t launch_tiled(const Job &j, cudaStream_t stream)
+{
+    using C = Cfg<CG, BN>;
+    constexpr int kNOut = MODE == kForward ? BN / 2 : BN;
+    constexpr int two_a = MODE == kForward ? 1 : 2, two_b = MODE == kDw ? 1 : 2, two_out = MODE == kDw ? 2 : 1;
+    Params p{};
+    Maps maps{};
+    p.M = j.M;
+    p.N = j.N;
+    p.k_stages = static_cast<int>((j.K + 63) / 64);
+    p.pairs = MODE == kDx ? 2 : 1;
+    p.terms = j.terms;
+    p.a_rows = j.M < C::kM ? static_cast<int>((j.M + 7) / 8 * 8) : C::kM;
+    p.act = j.act;
+    p.out_f32 = j.out_f32;
+    p.save = j.save[0] != nullptr;
+    p.status = j.status;
+    const int64_t mt = (j.M + CG * C::kM - 1) / (CG * C::kM), nt = (j.N + kNOut - 1) / kNOut;
+    if (mt * two_out * nt > (int64_t(1) << 30)) return cudaErrorInvalidValue;
+    p.m_tiles = static_cast<int>(mt);
+    p.n_tiles = static_cast<int>(nt);
+    p.tiles = static_cast<int>(mt * two_out * nt);
+    for (int i = 0; i < two_a; ++i)
+        if (!operand_map(&maps.a[i], j.a[i], MODE == kDw ? 64 : p.a_rows)) return cudaErrorInvalidValue;
+    for (int i = 0; i < two_b; ++i)
+        if (!operand_map(&maps.b[i], j.b[i], MODE == kForward ? (CG == 2 ? C::kBRows : C::kBRows / 2) : 64))
+            return cudaErrorInvalidValue;
+    const int width = j.out_f32 ? 32 : (kNOut < 64 ? kNOut : 64);
+    for (int i = 0; i < two_out; ++i)
+        if (!output_map(&maps.out[i], j.out[i], j.out_f32, j.M, j.N, width)) return cudaErrorInvalidValue;
+    if (p.save)
+        for (int i = 0; i < 2; ++i)
+            if (!output_map(&maps.save[i], j.save[i], true, j.M, j.N, 32)) return cudaErrorInvalidValue;
+    static SmemAttrCache attr_cache;
+    const cudaError_t attr = smem_attr_once(product_kernel<MODE, CG, BN, SPLIT>, static_cast<int>(C::kSmem), attr_cache);
+    if (attr != cudaSuccess) return attr;
+    const int64_t slots = ws::sm_count() / CG;
+    const unsigned blocks = static_cast<unsigned>((p.tiles < slots ? p.tiles : slots) * CG);
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(blocks);
+    cfg.blockDim = dim3(C::kThreads);
+    cfg.dynamicSmemBytes = C::kSmem;
+    cfg.stream = stream;
+    cudaLaunchAttribute la[1];
+    la[0].id = cudaLaunchAttributeClusterDimension;
+    la[0].val.clusterDim.x = CG;
+    la[0].val.clusterDim.y = 1;
+    la[0].val.clusterDim.z = 1;
+    cfg.attrs = la;
+    cfg.numAttrs = CG == 2 ? 1 : 0;
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, product_kernel<MODE, CG, BN, SPLIT>, p, maps);
+    return e != cudaSuccess ? e : cudaGetLastError();
+}
+
+// the tile whose rounds over the SMs take the fewest tensor-core cycles: a 64-deep stage takes 512 cycles in a
+// 256 x 256 pair tile, 256 in a 128 x 128 one and 192 in a 128 x 64 one, plus about 4000 a round for the
+// first copies and the last output
+template <int MODE>
+cudaError_t launch(const Job &j, cudaStream_t stream)
+{
+    const int64_t sms = ws::sm_count(), outs = MODE == kDw ? 2 : 1;
+    const int64_t stages = (j.K + 63) / 64 * j.terms * (MODE == kDx ? 2 : 1);
+    auto cycles = [&](int64_t rows, int64_t cols, int64_t slots, int64_t stage) {
+        const int64_t n = MODE == kForward ? cols / 2 : cols;
+        const int64_t tiles = (j.M + rows - 1) / rows * outs * ((j.N + n - 1) / n);
+        return (tiles + slots - 1) / slots * (stages * stage + 4000);
+    };
+    const int64_t pair = cycles(256, 256, sms / 2, 512), wide = cycles(128, 128, sms, 256),
+                  narrow = cycles(128, 64, sms, 192);
+    if (j.terms > 1)  // fp32: the output warps hold a tile's sums
+        return wide <= narrow ? launch_tiled<MODE, 1, 128, true>(j, stream) : launch_tiled<MODE, 1, 64, true>(j, stream);
+    if (pair <= wide && pair <= narrow) return launch_tiled<MODE, 2, 256, false>(j, stream);
+    if (wide <= narrow) return launch_tiled<MODE, 1, 128, false>(j, stream);
+    return launch_tiled<MODE, 1, 64, false>(j, stream);
+}
+
+cudaError_t launch_forward(const Job &j, cudaStream_t stream);
+cudaError_t launch_dx(const Job &j, cudaStream_t stream);
+cudaError_t launch_dw(const Job &j, cudaStream_t stream);
+
+}  // namespace gated
+}  // namespace cci

@@ -73,6 +73,27 @@ cudaError_t launch_token_logprobs_backward(const void *logits, int dtype, int64_
                                            const float *dlogp, const float *entropy, const float *dentropy, void *dx,
                                            int64_t lddx, uint32_t *status, cudaStream_t stream);
 
+// gated feed-forward block (cci_gated*.cu).  Wg, Wu: dense [F][D], or with gate_idx the packed
+// values; g, u: the saved pre-activations (forward: written, or null; backward: read); backward: dX, and
+// dWg with dWu, each may be null.  workspace: gated_workspace bytes for the call (a cci_gated_call)
+struct GatedArgs {
+    const void *X;
+    int dtype;
+    int64_t N, D, F;
+    const void *Wg, *Wu;
+    const uint8_t *gate_idx, *up_idx;
+    int G, K, act;
+    void *H;
+    float *g, *u;
+    const void *dH;
+    void *dX, *dWg, *dWu;
+    uint32_t *status;
+    void *workspace;
+};
+size_t gated_workspace(int dtype, int64_t N, int64_t D, int64_t F, int call);
+cudaError_t launch_gated(const GatedArgs &a, cudaStream_t stream);
+cudaError_t launch_gated_backward(const GatedArgs &a, cudaStream_t stream);
+
 // One register-tiled instantiation: (dtype, G, K) -> tile shape and launcher.
 struct RegtileEntry {
     int dtype, G, K, MG, T, D;
