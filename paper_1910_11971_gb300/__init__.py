@@ -526,11 +526,12 @@ def layer_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Opt
     are fp32 [D]; x may have a row stride."""
     ld = _cuda_rows(x, "x")
     N, D = x.shape
-    y = out if out is not None else torch.empty((N, D), dtype=x.dtype, device=x.device)
     if out is not None:
         _like(out, (N, D), x.dtype, "out")
-    stats = torch.empty((2, N), dtype=torch.float32, device=x.device)
-    mean, rstd = stats.unbind(0)
+    y = out if out is not None else torch.empty((N, D), dtype=x.dtype, device=x.device)
+    # small outputs are allocated one by one: views of one allocation cost the host more
+    mean = torch.empty(N, dtype=torch.float32, device=x.device)
+    rstd = torch.empty(N, dtype=torch.float32, device=x.device)
     _check(lib().cci_layer_norm(x.data_ptr(), _dtype_code(x), N, D, ld, _cuda_vec(weight, D, "weight"),
                                 _cuda_vec(bias, D, "bias"), eps, y.data_ptr(), mean.data_ptr(), rstd.data_ptr(),
                                 _stream(x.device)), "cci_layer_norm")
@@ -546,11 +547,11 @@ def layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, mean: torch.Tensor, r
     N, D = x.shape
     if dy.shape != x.shape or dy.dtype != x.dtype:
         raise ValueError("dy must have x's shape and dtype")
-    dx = out if out is not None else torch.empty((N, D), dtype=x.dtype, device=x.device)
     if out is not None:
         _like(out, (N, D), x.dtype, "out")
-    params = torch.empty((2, D), dtype=torch.float32, device=x.device)
-    dw, db = params.unbind(0)
+    dx = out if out is not None else torch.empty((N, D), dtype=x.dtype, device=x.device)
+    dw = torch.empty(D, dtype=torch.float32, device=x.device)
+    db = torch.empty(D, dtype=torch.float32, device=x.device)
     if workspace is None:
         workspace = _workspace(_norm_bytes(N, D, x.device.index), x.device)
     wp, wb = _ws(workspace)
@@ -570,9 +571,10 @@ def token_logprobs(logits: torch.Tensor, tokens: torch.Tensor, *, top: int = 0, 
     The logits may have a row stride."""
     ld = _cuda_rows(logits, "logits")
     N, V = logits.shape
-    f = torch.empty((4 + top, N), dtype=torch.float32, device=logits.device).view(-1)
-    logp, entropy, stats = f[:N], f[N:2 * N], f[2 * N:4 * N].view(N, 2)
-    top_logp = f[4 * N:].view(N, top) if top else None
+    logp = torch.empty(N, dtype=torch.float32, device=logits.device)
+    entropy = torch.empty(N, dtype=torch.float32, device=logits.device)
+    stats = torch.empty((N, 2), dtype=torch.float32, device=logits.device)
+    top_logp = torch.empty((N, top), dtype=torch.float32, device=logits.device) if top else None
     top_idx = torch.empty((N, top), dtype=torch.int32, device=logits.device) if top else None
     _check(lib().cci_token_logprobs(logits.data_ptr(), _dtype_code(logits), N, V, ld,
                                     _cuda_vec(tokens, N, "tokens", torch.int64), ignore_index, top, logp.data_ptr(),
@@ -590,13 +592,16 @@ def token_logprobs_backward(logits: torch.Tensor, tokens: Optional[torch.Tensor]
                             status: Optional[torch.Tensor] = None) -> torch.Tensor:
     """The gradient of ``token_logprobs`` to the logits, in their dtype (``cci_token_logprobs_backward``):
     of logp weighted by ``dlogp`` and of the entropy weighted by ``dentropy`` (which needs ``entropy``, as
-    the forward call returned it).  It has the logits' row stride unless ``out`` is given; ``out`` may be
-    the logits."""
+    the forward call returned it).  Rows padded by up to 64 logits keep their stride in the result, unless
+    ``out`` is given; ``out`` may be the logits."""
     ld = _cuda_rows(logits, "logits")
     N, V = logits.shape
     if out is None:
-        out = torch.empty((N, ld), dtype=logits.dtype, device=logits.device)[:, :V]
-        ldd = ld
+        # a padded row's stride (rows then start on the same 16-byte words), not that of a wide matrix' slice
+        ldd = ld if ld <= V + 64 else V
+        out = torch.empty((N, ldd), dtype=logits.dtype, device=logits.device)
+        if ldd != V:
+            out = out[:, :V]
     else:
         ldd = _cuda_rows(out, "out")
         if out.shape != logits.shape or out.dtype != logits.dtype:
