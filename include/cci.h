@@ -503,7 +503,7 @@ cci_status cci_layer_norm_backward(const void *dy, int64_t lddy, const void *x, 
  *              may be NULL for top = 0)
  *   dev_status device uint32 or NULL
  * N = 0 is valid and enqueues nothing.
- * Errors: CCI_ERR_NULL, CCI_ERR_SHAPE (V < 1 or >= 2^31, N >= 2^31, ldx < V, top out of
+ * Errors: CCI_ERR_NULL, CCI_ERR_SHAPE (V < 1 or > 2^24, N >= 2^31, ldx < V, top out of
  *         range), CCI_ERR_DTYPE, CCI_ERR_ALIGN, CCI_ERR_CUDA.
  */
 #define CCI_MAX_TOP 32

@@ -9,6 +9,7 @@ using namespace cci;
 namespace {
 
 constexpr int64_t kMaxRows = int64_t(1) << 31;
+constexpr int64_t kMaxLogits = int64_t(1) << 24;  // of a row: the alternatives' runs fit shared memory
 
 cudaStream_t as_stream(cci_stream_t s) { return reinterpret_cast<cudaStream_t>(s); }
 
@@ -65,7 +66,7 @@ cci_status cci_token_logprobs(const void *logits, cci_dtype dtype, int64_t N, in
     if (!valid_dtype(dtype)) return CCI_ERR_DTYPE;
     if (N > 0 && (!logits || !tokens || !logp || !entropy || !stats || (top > 0 && (!top_logp || !top_idx))))
         return CCI_ERR_NULL;
-    if (!rows_ok(N, V, ldx) || V >= kMaxRows || N >= kMaxRows || top < 0 || top > CCI_MAX_TOP || top > V)
+    if (!rows_ok(N, V, ldx) || V > kMaxLogits || N >= kMaxRows || top < 0 || top > CCI_MAX_TOP || top > V)
         return CCI_ERR_SHAPE;
     if (!aligned(logits, elem_size(dtype)) || !aligned(tokens, 8) || !aligned(logp, 4) || !aligned(entropy, 4) ||
         !aligned(stats, 4) || !aligned(top_logp, 4) || !aligned(top_idx, 4))
@@ -83,7 +84,7 @@ cci_status cci_token_logprobs_backward(const void *logits, cci_dtype dtype, int6
     if (!valid_dtype(dtype)) return CCI_ERR_DTYPE;
     if (N > 0 && (!logits || !stats || !dlogits || (dlogp && !tokens) || (dentropy && !entropy))) return CCI_ERR_NULL;
     // a block takes 8192 logits of a row
-    if (!rows_ok(N, V, ldx) || !rows_ok(N, V, lddx) || V >= kMaxRows || N >= kMaxRows ||
+    if (!rows_ok(N, V, ldx) || !rows_ok(N, V, lddx) || V > kMaxLogits || N >= kMaxRows ||
         N * ((V + 8191) / 8192) >= kMaxRows)
         return CCI_ERR_SHAPE;
     const size_t es = elem_size(dtype);

@@ -369,14 +369,6 @@ __global__ void __launch_bounds__(1024)
 
 constexpr int64_t kRegisterColumns = 16384;  // widest row that a block holds
 
-int sm_count()
-{
-    int dev = 0, n = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
-        return 1;
-    return n;
-}
-
 int64_t least(int64_t a, int64_t b) { return a < b ? a : b; }
 
 struct Args {
@@ -411,7 +403,7 @@ int64_t backward_blocks(int e, int64_t N, int64_t D)
 {
     if (D > kRegisterColumns) return least(N, 16);
     const int tpr = group_threads(e, D), groups = block_threads(tpr) / tpr;
-    return least((N + groups - 1) / groups, static_cast<int64_t>(sm_count()) * backward_residents(tpr));
+    return least((N + groups - 1) / groups, static_cast<int64_t>(row::sm_count()) * backward_residents(tpr));
 }
 
 // the most parts of any form of a call
@@ -425,7 +417,7 @@ template <typename T, int V, int E, int TPR>
 cudaError_t forward_one(const Args &a)
 {
     constexpr int kT = block_threads(TPR), kGroups = kT / TPR;
-    const int64_t blocks = least((a.N + kGroups - 1) / kGroups, static_cast<int64_t>(sm_count()) * forward_residents(TPR));
+    const int64_t blocks = least((a.N + kGroups - 1) / kGroups, static_cast<int64_t>(row::sm_count()) * forward_residents(TPR));
     norm_kernel<T, V, E, TPR><<<static_cast<unsigned>(blocks), kT, 0, a.stream>>>(
         static_cast<const T *>(a.x), a.ldx, a.N, static_cast<int>(a.D), a.w, a.b, a.eps, static_cast<T *>(a.y), a.mean,
         a.rstd);
@@ -486,7 +478,7 @@ template <typename T>
 cudaError_t forward(const Args &a)
 {
     if (a.D > kRegisterColumns) {
-        norm_long_kernel<T><<<static_cast<unsigned>(least(a.N, 2 * sm_count())), 1024, 0, a.stream>>>(
+        norm_long_kernel<T><<<static_cast<unsigned>(least(a.N, 2 * row::sm_count())), 1024, 0, a.stream>>>(
             static_cast<const T *>(a.x), a.ldx, a.N, a.D, a.w, a.b, a.eps, static_cast<T *>(a.y), a.mean, a.rstd);
         return cudaGetLastError();
     }
@@ -497,7 +489,7 @@ template <typename T>
 cudaError_t backward(const Args &a)
 {
     if (a.D > kRegisterColumns) {
-        norm_long_dx_kernel<T><<<static_cast<unsigned>(least(a.N, 2 * sm_count())), 1024, 0, a.stream>>>(
+        norm_long_dx_kernel<T><<<static_cast<unsigned>(least(a.N, 2 * row::sm_count())), 1024, 0, a.stream>>>(
             static_cast<const T *>(a.dy), a.lddy, static_cast<const T *>(a.x), a.ldx, a.mean_in, a.rstd_in, a.w, a.N,
             a.D, static_cast<T *>(a.y));
         const cudaError_t e = cudaGetLastError();

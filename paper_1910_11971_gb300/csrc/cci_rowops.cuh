@@ -7,6 +7,15 @@
 namespace cci {
 namespace row {
 
+// SMs of the current device (1 when it cannot be asked)
+inline int sm_count()
+{
+    int dev = 0, n = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
+        return 1;
+    return n;
+}
+
 // element types: float, or uint16_t for the bits of a bf16
 __device__ __forceinline__ float to_f32(float v) { return v; }
 __device__ __forceinline__ float to_f32(uint16_t v) { return bf16_bits_to_f32(v); }
