@@ -3,7 +3,8 @@
 //
 //   planes    fp32 matrices as three bf16 planes, once per call (memory bound: 4 bytes read and 6
 //             written an element)
-//   expand    both packed weight matrices (values, idx) to dense bf16, or to those planes
+//   expand    both packed weight matrices (values, idx) to dense bf16, or to those planes; few tokens (cci_gated_few.cu)
+//             read the packed bf16 weights themselves, and dense fp32 ones
 //   slopes    dg = dh u act'(g), du = dh act(g) from the saved fp32 g and u, rounded to bf16 (or split
 //             into planes), the operands of the gradients' products (memory bound: 14 bytes an
 //             element in bf16).  g and u are saved in fp32, not rounded to bf16: with them rounded too
@@ -79,6 +80,7 @@ struct ExpandJob {
     uint16_t *out[2];
     int64_t F, D;
     int G, K, cols, col_blocks;
+    int whole;  // fp32: [F][D] fp32 instead of planes
     uint32_t *status;
 };
 
@@ -113,7 +115,10 @@ __global__ void __launch_bounds__(256) expand_kernel(ExpandJob j)
         } else {
             float v[8];
             row::unpack<float, 8>(row::load<float, 8>(reinterpret_cast<const float *>(tile) + r * cols + c), v);
-            store_planes<3>(out + r * j.D + c, j.F * j.D, v);
+            if (j.whole)
+                row::store<float, 8>(reinterpret_cast<float *>(j.out[which]) + (group * G + r) * j.D + d0 + c, v);
+            else
+                store_planes<3>(out + r * j.D + c, j.F * j.D, v);
         }
     }
 }
@@ -197,7 +202,8 @@ size_t gated_workspace(int dtype, int64_t N, int64_t D, int64_t F, int call)
 cudaError_t launch_gated(const GatedArgs &a, cudaStream_t stream)
 {
     using namespace gated;
-    const bool f32 = a.dtype == CCI_F32, packed = a.gate_idx != nullptr;
+    const bool f32 = a.dtype == CCI_F32, packed = a.gate_idx != nullptr, few = few_tokens(a.dtype, a.N);
+    if (packed ? few_packed(a) : few) return launch_few(a, a.Wg, a.Wu, packed, stream);
     const Layout l = layout(a.dtype, a.N, a.D, a.F, packed ? CCI_GATED_PACKED : CCI_GATED_FORWARD);
     char *base = static_cast<char *>(a.workspace);
     const void *x = a.X, *wg = a.Wg, *wu = a.Wu;
@@ -216,6 +222,7 @@ cudaError_t launch_gated(const GatedArgs &a, cudaStream_t stream)
         // a tile of at most 32 KB
         j.cols = a.G <= 32 ? 256 : (a.G <= 64 ? 128 : (a.G <= 128 ? 64 : 32));
         j.status = a.status;
+        j.whole = few;
         j.col_blocks = static_cast<int>((a.D + j.cols - 1) / j.cols);
         const int64_t blocks = a.F / a.G * j.col_blocks;
         if (blocks > 0x7fffffff) return cudaErrorInvalidValue;
@@ -229,6 +236,7 @@ cudaError_t launch_gated(const GatedArgs &a, cudaStream_t stream)
         if (e != cudaSuccess) return e;
         wg = base + l.wg;
         wu = base + l.wu;
+        if (few) return launch_few(a, wg, wu, false, stream);
     }
     if (f32) {
         const float *in[3] = {static_cast<const float *>(a.X), static_cast<const float *>(a.Wg),
