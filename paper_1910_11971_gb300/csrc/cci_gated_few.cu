@@ -71,12 +71,6 @@ __device__ __forceinline__ void finish(const Args &p, const float *red, int stri
 // eight weights of one row (bf16) as a lane's fragment words
 __device__ __forceinline__ uint4 load_weights(const uint16_t *w) { return row::load_once<uint16_t, 8>(w).w[0]; }
 
-// K kept weights of each of eight indices and their places in the group, as they are packed
-template <int K>
-struct Run {
-    uint32_t v[4 * K], i[2 * K];
-};
-
 // from shared memory; the lanes of a group read the same words
 template <int K>
 __device__ __forceinline__ void load_run(Run<K> &r, const unsigned char *values, const unsigned char *idx)
@@ -92,36 +86,6 @@ __device__ __forceinline__ void load_run(Run<K> &r, const unsigned char *values,
         r.i[2 * q] = i.x;
         r.i[2 * q + 1] = i.y;
     }
-}
-
-// the eight weights of the row with index j (rows: j in every byte): each value whose index is j, else zero
-template <int K>
-__device__ __forceinline__ uint4 pick(const Run<K> &r, uint32_t rows)
-{
-    using ws::pk::prmt;
-    uint32_t m[2 * K];  // bit 7 of a byte: that slot's index is j (indices are below 128)
-#pragma unroll
-    for (int q = 0; q < 2 * K; ++q) m[q] = 0x80808080u - (r.i[q] ^ rows);
-    uint32_t out[4];
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {  // indices 2 e and 2 e + 1
-        if constexpr (K == 1) {
-            out[e] = r.v[e] & prmt(m[e >> 1], 0u, e & 1 ? 0xbbaau : 0x9988u);
-        } else {
-            uint32_t x[2];  // both halves of x[h]: what of index 2 e + h's slots is kept
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                x[h] = 0u;
-#pragma unroll
-                for (int s = 0; s < K / 2; ++s) {  // word s of the index: slots 2 s and 2 s + 1
-                    const int word = (2 * e + h) * (K / 2) + s;
-                    x[h] |= r.v[word] & prmt(m[word >> 1], 0u, word & 1 ? 0xbbaau : 0x9988u);
-                }
-            }
-            out[e] = prmt(x[0], x[1], 0x5410u) | prmt(x[0], x[1], 0x7632u);
-        }
-    }
-    return make_uint4(out[0], out[1], out[2], out[3]);
 }
 
 // whether the index set of K at `idx` is not strictly increasing below G
