@@ -52,8 +52,8 @@ cci_status cci_layer_norm_backward(const void *dy, int64_t lddy, const void *x, 
     if (!aligned(dy, es) || !aligned(x, es) || !aligned(dx, es) || !aligned(mean, 4) || !aligned(rstd, 4) ||
         !aligned(weight, 4) || !aligned(dweight, 4) || !aligned(dbias, 4))
         return CCI_ERR_ALIGN;
-    if (N > 0 && (!workspace || !aligned(workspace, 16) || workspace_bytes < layer_norm_workspace(N, D)))
-        return CCI_ERR_WORKSPACE;
+    const size_t need = N > 0 ? layer_norm_workspace(N, D) : 0;
+    if (need > 0 && (!workspace || !aligned(workspace, 16) || workspace_bytes < need)) return CCI_ERR_WORKSPACE;
     return to_status(launch_layer_norm_backward(dy, lddy, x, ldx, dtype, N, D, mean, rstd, weight, dx, dweight, dbias,
                                                 static_cast<float *>(workspace), as_stream(stream)));
 }

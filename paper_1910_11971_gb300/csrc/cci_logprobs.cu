@@ -108,20 +108,8 @@ __device__ __forceinline__ Sums warp_joined(Sums a)
     return a;
 }
 
-// two fp32 at a time
-__device__ __forceinline__ unsigned long long add2(unsigned long long a, unsigned long long b)
-{
-    unsigned long long r;
-    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-    return r;
-}
-
-__device__ __forceinline__ unsigned long long mul2(unsigned long long a, unsigned long long b)
-{
-    unsigned long long r;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-    return r;
-}
+using row::add2;
+using row::mul2;
 
 // the larger; NaN if either is
 __device__ __forceinline__ float max_nan(float a, float b)

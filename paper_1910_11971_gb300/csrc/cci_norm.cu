@@ -11,8 +11,8 @@
 // registers over all rows of its block; the blocks' sums go to the workspace and a second
 // launch adds them in block order, so the result does not depend on what finishes first.
 // All sums are fp32.
-#include "cci_kernels.h"
 #include "cci_rowops.cuh"
+#include "cci_tc_common.cuh"
 
 namespace cci {
 namespace norm {
@@ -20,9 +20,34 @@ namespace norm {
 // threads of a block with row groups of TPR threads
 constexpr int block_threads(int TPR) { return TPR < 256 ? 256 : TPR; }
 
-// blocks of an SM that the register limit leaves room for
-constexpr int forward_residents(int TPR) { return TPR <= 256 ? 3 : (TPR == 512 ? 2 : 1); }
-constexpr int backward_residents(int TPR) { return TPR <= 256 ? 2 : 1; }
+// blocks of an SM that the registers leave room for
+constexpr int residents(int TPR, bool words, bool backward) { return TPR <= 256 ? (words && !backward ? 3 : 2) : 1; }
+
+// Rows on whole 16-byte words come by bulk copies into a ring of rows per group, as many ahead as shared
+// memory holds; the copies of a row are counted in bytes on its stage's barrier.  Loads into registers, which
+// other rows take, keep less on its way (16384 x 4096 bf16: 50 us forward and 102 backward, now 48 and
+// 78).
+constexpr int kMaxStages = 6;
+
+struct Ring {
+    uint64_t full[kMaxStages];
+};
+
+// untiled bulk copy of `bytes` (a multiple of 16) to shared memory, completing on `bar`; both addresses on 16 bytes
+__device__ __forceinline__ void bulk_load(void *dst, const void *src, uint32_t bytes, uint64_t *bar)
+{
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(
+                     tc::smem_u32(dst)),
+                 "l"(reinterpret_cast<uint64_t>(src)), "r"(bytes), "r"(tc::smem_u32(bar))
+                 : "memory");
+}
+
+// stages of a group's ring: `bytes` a stage, `groups` rings in a block, `blocks` blocks in an SM
+constexpr int stages_of(int bytes, int groups, int blocks)
+{
+    const int fit = (200 * 1024 / blocks) / (bytes * groups);
+    return fit < kMaxStages ? fit : kMaxStages;
+}
 
 // V consecutive fp32 parameters from p[c] on, or `missing` where there are none
 template <int V>
@@ -52,80 +77,197 @@ __device__ __forceinline__ void load_row(row::Raw<T, V> (&raw)[NV], const T *x, 
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
         const int c = (i * TPR + t) * V;
-        if (c < D) raw[i] = row::load_once<T, V>(x + c);
+        if (c < D)
+            raw[i] = row::load_once<T, V>(x + c);
+        else
+            raw[i] = row::Raw<T, V>{};
     }
 }
 
-// ---- forward: E columns per thread, in vectors of V.  Groups walk the rows; the next row's loads are on
-// their way while this one is reduced.  Rows of up to 4096 keep weight and bias in registers ----
+// pairs of a thread's columns: kP of them from kStep vectors at a time, vectors i .. i + kStep - 1
+template <int V>
+struct Pairs {
+    static constexpr int kStep = V == 1 ? 2 : 1, kP = V == 1 ? 1 : V / 2;
+    unsigned long long p[kP];
+};
+
+template <typename T, int V>
+__device__ __forceinline__ Pairs<V> pairs_of(const row::Raw<T, V> *raw)
+{
+    Pairs<V> r;
+    if constexpr (V == 1)
+        r.p[0] = pack2(row::to_f32(raw[0].w), row::to_f32(raw[1].w));
+    else
+        row::unpack2<T, V>(raw[0], r.p);
+    return r;
+}
+
+// the same from a row in memory: global (columns past D: zeros), or a stage of a ring, which holds zeros there
+template <typename T, int V, int TPR, bool RING>
+__device__ __forceinline__ Pairs<V> pairs_at(const T *x, int i, int t, int D)
+{
+    row::Raw<T, V> raw[Pairs<V>::kStep];
+#pragma unroll
+    for (int j = 0; j < Pairs<V>::kStep; ++j) {
+        const int c = ((i + j) * TPR + t) * V;
+        raw[j] = RING || c < D ? row::load<T, V>(x + c) : row::Raw<T, V>{};
+    }
+    return pairs_of<T, V>(raw);
+}
+
+// zeros in the columns past D of `rows` rows of a ring, which no copy writes (one group's threads)
 template <typename T, int V, int E, int TPR>
-__global__ void __launch_bounds__(block_threads(TPR), forward_residents(TPR))
+__device__ __forceinline__ void zero_tails(unsigned char *ring, int rows, int t, int D)
+{
+    constexpr int kWidth = E * TPR;
+    for (int r = 0; r < rows; ++r)
+        for (int c = D + t * V; c < kWidth; c += TPR * V)
+            *reinterpret_cast<uint4 *>(reinterpret_cast<T *>(ring) + r * kWidth + c) = make_uint4(0u, 0u, 0u, 0u);
+}
+
+template <int V, int TPR>
+__device__ __forceinline__ Pairs<V> params2(const float *w, int i, int t, int D, float missing)
+{
+    float f[2 * Pairs<V>::kP] = {};
+#pragma unroll
+    for (int j = 0; j < Pairs<V>::kStep; ++j) {
+        const int c = ((i + j) * TPR + t) * V;
+        if (c < D) params_at<V>(w, c, missing, f + j * V);
+    }
+    Pairs<V> r;
+#pragma unroll
+    for (int j = 0; j < Pairs<V>::kP; ++j) r.p[j] = pack2(f[2 * j], f[2 * j + 1]);
+    return r;
+}
+
+template <typename T, int V, int TPR>
+__device__ __forceinline__ void store_pairs(T *y, int i, int t, int D, const Pairs<V> &o)
+{
+    const int c = (i * TPR + t) * V;
+    if constexpr (V == 1) {
+        const float a = lo_of(o.p[0]), b = hi_of(o.p[0]);
+        if (c < D) row::store<T, 1>(y + c, &a);
+        if (c + TPR < D) row::store<T, 1>(y + c + TPR, &b);
+    } else if (c < D) {
+        row::store2<T, V>(y + c, o.p);
+    }
+}
+
+// ---- forward: E columns per thread, in vectors of V.  Groups walk the rows; the next rows are on their way while
+// one is reduced.  Rows of up to 4096 keep weight and bias in registers ----
+template <typename T, int V, int E, int TPR>
+__global__ void __launch_bounds__(block_threads(TPR), residents(TPR, (V > 1), false))
     norm_kernel(const T *x, int64_t ldx, int64_t N, int D, const float *w, const float *b, float eps, T *y, float *mean,
                 float *rstd)
 {
     constexpr int kGroups = block_threads(TPR) / TPR, kNV = E / V;
-    constexpr bool kHold = TPR <= 256;
+    constexpr bool kHold = TPR <= 256, kBulk = V > 1;
+    constexpr int kStage = E * TPR * static_cast<int>(sizeof(T));
+    constexpr int kStages = stages_of(kStage, kGroups, residents(TPR, (V > 1), false));
+    extern __shared__ __align__(128) unsigned char ring_raw[];
+    __shared__ Ring rings[kGroups];
     __shared__ float buf[kGroups][2][TPR / 32];
+    __shared__ int abort_flag;
     const int group = threadIdx.x / TPR, t = threadIdx.x % TPR;
     const float width = static_cast<float>(D);
     const int64_t step = static_cast<int64_t>(gridDim.x) * kGroups;
-    int64_t n = static_cast<int64_t>(blockIdx.x) * kGroups + group;
-    float wv[kHold ? E : V], bv[kHold ? E : V];
-    row::Raw<T, V> raw[kNV];
-    if (n < N) load_row<T, V, kNV, TPR>(raw, x + n * ldx, t, D);
+    const int64_t n0 = static_cast<int64_t>(blockIdx.x) * kGroups + group;
+    unsigned char *ring = ring_raw + group * kStages * kStage;
+    Ring &R = rings[group];
+    volatile int *abort = &abort_flag;
+    const uint32_t bytes = static_cast<uint32_t>(D) * sizeof(T);
+    auto copy = [&](int64_t n, int s) {
+        tc::mbar_arrive_expect_tx(&R.full[s], bytes);
+        bulk_load(ring + s * kStage, x + n * ldx, bytes, &R.full[s]);
+    };
+    row::Raw<T, V> raw[kBulk ? 1 : kNV];
+    if constexpr (kBulk) {
+        if (threadIdx.x == 0) abort_flag = 0;
+        zero_tails<T, V, E, TPR>(ring, kStages, t, D);
+        if (t == 0) {
+            for (int s = 0; s < kStages; ++s) tc::mbar_init(&R.full[s], 1);
+            asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+            for (int s = 0; s < kStages; ++s)
+                if (n0 + s * step < N) copy(n0 + s * step, s);
+        }
+        __syncthreads();
+    } else {
+        if (n0 < N) load_row<T, V, kNV, TPR>(raw, x + n0 * ldx, t, D);
+    }
+    constexpr int kStep = Pairs<V>::kStep, kP = Pairs<V>::kP;
+    Pairs<V> wv[kHold ? E / 2 / kP : 1], bv[kHold ? E / 2 / kP : 1];
     if constexpr (kHold) {
 #pragma unroll
-        for (int i = 0; i < kNV; ++i) {
-            const int c = (i * TPR + t) * V;
-            if (c < D) {
-                params_at<V>(w, c, 1.f, wv + i * V);
-                params_at<V>(b, c, 0.f, bv + i * V);
-            }
+        for (int i = 0; i < kNV; i += kStep) {
+            wv[i / kStep] = params2<V, TPR>(w, i, t, D, 1.f);
+            bv[i / kStep] = params2<V, TPR>(b, i, t, D, 0.f);
         }
     }
-    for (; n < N; n += step) {
-        float f[E];
-        float s[1] = {0.f}, q[1] = {0.f};
+    int st = 0;
+    uint32_t ph = 0u;
+    for (int64_t n = n0; n < N; n += step) {
+        Pairs<V> f[E / 2 / kP];
+        float s[1], q[1];
+        unsigned long long s2 = 0ull, q2 = 0ull;
+        // a wait that expires leaves wrong results, but every thread goes on: none is left at a barrier
+        if constexpr (kBulk) tc::mbar_wait(&R.full[st], ph, abort, nullptr);
 #pragma unroll
-        for (int i = 0; i < kNV; ++i) {
-            if ((i * TPR + t) * V < D) {
-                row::unpack<T, V>(raw[i], f + i * V);
+        for (int i = 0; i < kNV; i += kStep) {
+            f[i / kStep] = kBulk ? pairs_at<T, V, TPR, true>(reinterpret_cast<const T *>(ring + st * kStage), i, t, D)
+                                 : pairs_of<T, V>(raw + (kBulk ? 0 : i));
 #pragma unroll
-                for (int j = 0; j < V; ++j) s[0] += f[i * V + j];
-            }
+            for (int j = 0; j < kP; ++j) s2 = row::add2(s2, f[i / kStep].p[j]);
         }
-        if (n + step < N) load_row<T, V, kNV, TPR>(raw, x + (n + step) * ldx, t, D);
+        s[0] = lo_of(s2) + hi_of(s2);
+        if constexpr (!kBulk) {
+            if (n + step < N) load_row<T, V, kNV, TPR>(raw, x + (n + step) * ldx, t, D);
+        }
         row::group_sum<TPR>(s, buf[group][0], group, t);
-        const float mu = s[0] / width;
-#pragma unroll
-        for (int i = 0; i < kNV; ++i) {
-            if ((i * TPR + t) * V < D) {
-#pragma unroll
-                for (int j = 0; j < V; ++j) {
-                    f[i * V + j] -= mu;
-                    q[0] += f[i * V + j] * f[i * V + j];
-                }
+        if constexpr (kBulk) {
+            // every thread of the group has its part of the row
+            if (t == 0 && n + kStages * step < N) copy(n + kStages * step, st);
+            if (++st == kStages) {
+                st = 0;
+                ph ^= 1u;
             }
         }
+        const float mu = s[0] / width;
+        const unsigned long long minus_mu = pack2(-mu, -mu);
+#pragma unroll
+        for (int i = 0; i < kNV; i += kStep) {
+#pragma unroll
+            for (int j = 0; j < kP; ++j) {
+                unsigned long long &v = f[i / kStep].p[j];
+                v = row::add2(v, minus_mu);
+                // columns past D add nothing
+                const int c = (i * TPR + t) * V;
+                unsigned long long sq = v;
+                if (c >= D) sq = 0ull;
+                if (V == 1 && c + TPR >= D) sq = pack2(lo_of(sq), 0.f);
+                ffma2(q2, sq, sq);
+            }
+        }
+        q[0] = lo_of(q2) + hi_of(q2);
         row::group_sum<TPR>(q, buf[group][1], group, t);
         const float r = 1.f / sqrtf(q[0] / width + eps);
         if (t == 0) {
             mean[n] = mu;
             rstd[n] = r;
         }
+        const unsigned long long r2 = pack2(r, r);
 #pragma unroll
-        for (int i = 0; i < kNV; ++i) {
-            const int c = (i * TPR + t) * V, h = kHold ? i * V : 0;
-            if (c < D) {
-                if constexpr (!kHold) {
-                    params_at<V>(w, c, 1.f, wv);
-                    params_at<V>(b, c, 0.f, bv);
-                }
-                float o[V];
-#pragma unroll
-                for (int j = 0; j < V; ++j) o[j] = f[i * V + j] * r * wv[h + j] + bv[h + j];
-                row::store<T, V>(y + n * D + c, o);
+        for (int i = 0; i < kNV; i += kStep) {
+            if constexpr (!kHold) {
+                wv[0] = params2<V, TPR>(w, i, t, D, 1.f);
+                bv[0] = params2<V, TPR>(b, i, t, D, 0.f);
             }
+            Pairs<V> o;
+#pragma unroll
+            for (int j = 0; j < kP; ++j) {
+                o.p[j] = bv[kHold ? i / kStep : 0].p[j];
+                ffma2(o.p[j], row::mul2(f[i / kStep].p[j], r2), wv[kHold ? i / kStep : 0].p[j]);
+            }
+            store_pairs<T, V, TPR>(y + n * D, i, t, D, o);
         }
     }
 }
@@ -161,132 +303,266 @@ __global__ void __launch_bounds__(1024)
     }
 }
 
-// ---- backward: dx, and this block's sums of dw and db into part[block][2][D] ----
+// one row's share of dw and db, and of the sums of g = dy w and g xh (columns past D: dy is 0)
+template <int V>
+__device__ __forceinline__ void add_columns(const Pairs<V> &x, const Pairs<V> &dy, const Pairs<V> &w,
+                                            unsigned long long minus_m, unsigned long long r, unsigned long long *dw,
+                                            unsigned long long *db, unsigned long long &s0, unsigned long long &s1)
+{
+#pragma unroll
+    for (int j = 0; j < Pairs<V>::kP; ++j) {
+        const unsigned long long xh = row::mul2(row::add2(x.p[j], minus_m), r);
+        ffma2(dw[j], dy.p[j], xh);
+        db[j] = row::add2(db[j], dy.p[j]);
+        const unsigned long long g = row::mul2(dy.p[j], w.p[j]);
+        s0 = row::add2(s0, g);
+        ffma2(s1, g, xh);
+    }
+}
+
+// dx = (dy w - a - xh b) r
+template <int V>
+__device__ __forceinline__ Pairs<V> input_gradient(const Pairs<V> &x, const Pairs<V> &dy, const Pairs<V> &w,
+                                                   unsigned long long minus_m, unsigned long long r,
+                                                   unsigned long long minus_a, unsigned long long minus_b)
+{
+    Pairs<V> o;
+#pragma unroll
+    for (int j = 0; j < Pairs<V>::kP; ++j) {
+        const unsigned long long xh = row::mul2(row::add2(x.p[j], minus_m), r);
+        unsigned long long q = minus_a;
+        ffma2(q, dy.p[j], w.p[j]);
+        ffma2(q, xh, minus_b);
+        o.p[j] = row::mul2(q, r);
+    }
+    return o;
+}
+
+// ---- backward: dx, and this block's sums of dw and db to pw and pb, each block 2 D further ----
 template <typename T, int V, int E, int TPR>
-__global__ void __launch_bounds__(block_threads(TPR), backward_residents(TPR))
+__global__ void __launch_bounds__(block_threads(TPR), residents(TPR, (V > 1), true))
     norm_backward_kernel(const T *dy, int64_t lddy, const T *x, int64_t ldx, const float *mean, const float *rstd,
-                         const float *w, int64_t N, int D, T *dx, float *part)
+                         const float *w, int64_t N, int D, T *dx, float *pw, float *pb)
 {
     constexpr int kGroups = block_threads(TPR) / TPR, kNV = E / V;
-    // 1024 threads leave no registers to hold x and dy besides dw and db: they are read again
-    // (from L1) for dx
-    constexpr bool kAgain = TPR == 1024;
-    __shared__ float buf[kGroups][2][2 * TPR / 32];
-    __shared__ float comb[kGroups > 1 ? 2 * E * TPR : 1];
+    constexpr int kRow = E * TPR * static_cast<int>(sizeof(T)), kStage = 2 * kRow;  // a stage: x, then dy
+    constexpr int kStages = stages_of(kStage, kGroups, residents(TPR, (V > 1), true));
+    // two stages at least; else, and for rows off whole words, a row is loaded into registers, or where 1024 threads
+    // have none left, both passes over it read global memory, the second from L1
+    constexpr bool kBulk = V > 1 && kStages >= 2, kKeep = !kBulk && TPR < 1024;
+    extern __shared__ __align__(128) unsigned char ring_raw[];
+    __shared__ Ring rings[kGroups];
+    __shared__ float buf[kGroups][2][4 * TPR / 32];
+    __shared__ int abort_flag;
     const int group = threadIdx.x / TPR, t = threadIdx.x % TPR;
     const float width = static_cast<float>(D);
     const int64_t step = static_cast<int64_t>(gridDim.x) * kGroups;
-    float dw[E], db[E], wv[kAgain ? V : E];
-#pragma unroll
-    for (int e = 0; e < E; ++e) dw[e] = db[e] = 0.f;
-    int64_t n = static_cast<int64_t>(blockIdx.x) * kGroups + group;
-    row::Raw<T, V> rx[kAgain ? 1 : kNV], rd[kAgain ? 1 : kNV];
-    float mu = 0.f, r = 0.f;
-    if constexpr (!kAgain) {
-        if (n < N) {
-            load_row<T, V, kNV, TPR>(rx, x + n * ldx, t, D);
-            load_row<T, V, kNV, TPR>(rd, dy + n * lddy, t, D);
-            mu = __ldg(mean + n);
-            r = __ldg(rstd + n);
+    const int64_t n0 = static_cast<int64_t>(blockIdx.x) * kGroups + group;
+    unsigned char *ring = ring_raw + group * kStages * kStage;
+    Ring &R = rings[group];
+    volatile int *abort = &abort_flag;
+    const uint32_t bytes = static_cast<uint32_t>(D) * sizeof(T);
+    auto copy = [&](int64_t n, int s) {
+        tc::mbar_arrive_expect_tx(&R.full[s], 2 * bytes);
+        bulk_load(ring + s * kStage, x + n * ldx, bytes, &R.full[s]);
+        bulk_load(ring + s * kStage + kRow, dy + n * lddy, bytes, &R.full[s]);
+    };
+    // the second launch, which adds the blocks' sums, may be scheduled: it waits for this one
+    tc::launch_next_grid();
+    if constexpr (kBulk) {
+        if (threadIdx.x == 0) abort_flag = 0;
+        zero_tails<T, V, E, TPR>(ring, 2 * kStages, t, D);
+        if (t == 0) {
+            for (int s = 0; s < kStages; ++s) tc::mbar_init(&R.full[s], 1);
+            asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+            for (int s = 0; s < kStages; ++s)
+                if (n0 + s * step < N) copy(n0 + s * step, s);
         }
+        __syncthreads();
+    }
+    constexpr bool kHold = TPR < 1024;  // the weight in registers
+    constexpr int kStep = Pairs<V>::kStep, kP = Pairs<V>::kP;
+    unsigned long long dw[E / 2], db[E / 2];
+    Pairs<V> wv[kHold ? E / 2 / kP : 1];
 #pragma unroll
-        for (int i = 0; i < kNV; ++i)
-            if ((i * TPR + t) * V < D) params_at<V>(w, (i * TPR + t) * V, 1.f, wv + i * V);
+    for (int e = 0; e < E / 2; ++e) dw[e] = db[e] = 0ull;
+    if constexpr (kHold) {
+#pragma unroll
+        for (int i = 0; i < kNV; i += kStep) wv[i / kStep] = params2<V, TPR>(w, i, t, D, 1.f);
     }
     int k = 0;
-    for (; n < N; n += step, k ^= 1) {
-        constexpr int kHold = kAgain ? V : E;
-        float xh[kHold], g[kHold];
-        float s[2] = {0.f, 0.f};
-        if constexpr (kAgain) {
-            mu = __ldg(mean + n);
-            r = __ldg(rstd + n);
-        }
-        const float rn = r;
+    if constexpr (kBulk) {
+        // kRows rows at a time, so that their sums share the exchanges and the barrier
+        constexpr int kRows = kStages % 2 == 0 ? 2 : 1;
+        int st = 0;
+        uint32_t ph = 0u;
+        float mu[kRows], r[kRows];  // of the next rows
+        auto stats_of = [&](int64_t n) {
 #pragma unroll
-        for (int i = 0; i < kNV; ++i) {
-            const int c = (i * TPR + t) * V, h = kAgain ? 0 : i * V;
-            if (c < D) {
-                if constexpr (kAgain) {
-                    rx[0] = row::load<T, V>(x + n * ldx + c);
-                    rd[0] = row::load<T, V>(dy + n * lddy + c);
-                    params_at<V>(w, c, 1.f, wv);
+            for (int q = 0; q < kRows; ++q) {
+                mu[q] = n + q * step < N ? __ldg(mean + n + q * step) : 0.f;
+                r[q] = n + q * step < N ? __ldg(rstd + n + q * step) : 0.f;
+            }
+        };
+        stats_of(n0);
+        for (int64_t n = n0; n < N; n += kRows * step, k ^= 1) {
+            float s[4] = {0.f, 0.f, 0.f, 0.f};
+            float m[kRows], rn[kRows];
+            const T *xr[kRows], *dr[kRows];
+#pragma unroll
+            for (int q = 0; q < kRows; ++q) {
+                xr[q] = reinterpret_cast<const T *>(ring + (st + q) * kStage);
+                dr[q] = reinterpret_cast<const T *>(ring + (st + q) * kStage + kRow);
+                m[q] = mu[q];
+                rn[q] = r[q];
+            }
+            stats_of(n + kRows * step);
+#pragma unroll
+            for (int q = 0; q < kRows; ++q) {
+                if (q > 0 && n + step >= N) break;
+                // a wait that expires leaves wrong results, but every thread goes on: none is left at a barrier
+                tc::mbar_wait(&R.full[st + q], ph, abort, nullptr);
+                const unsigned long long minus_m = pack2(-m[q], -m[q]), rn2 = pack2(rn[q], rn[q]);
+                unsigned long long s0 = 0ull, s1 = 0ull;
+#pragma unroll
+                for (int i = 0; i < kNV; i += kStep) {
+                    const Pairs<V> xp = pairs_at<T, V, TPR, true>(xr[q], i, t, D);
+                    const Pairs<V> gp = pairs_at<T, V, TPR, true>(dr[q], i, t, D);
+                    if constexpr (!kHold) wv[0] = params2<V, TPR>(w, i, t, D, 1.f);
+                    add_columns<V>(xp, gp, wv[kHold ? i / kStep : 0], minus_m, rn2, dw + i / kStep * kP, db + i / kStep * kP, s0, s1);
                 }
-                row::unpack<T, V>(rx[kAgain ? 0 : i], xh + h);
-                row::unpack<T, V>(rd[kAgain ? 0 : i], g + h);
+                s[2 * q] = lo_of(s0) + hi_of(s0);
+                s[2 * q + 1] = lo_of(s1) + hi_of(s1);
+            }
+            row::group_sum4<TPR>(s, buf[group][k], group, t);
+            // every thread of the group has left the rows before these: their stages take the rows after these
+            if (t == 0 && n > n0) {
 #pragma unroll
-                for (int j = 0; j < V; ++j) {
-                    xh[h + j] = (xh[h + j] - mu) * rn;
-                    dw[i * V + j] += g[h + j] * xh[h + j];
-                    db[i * V + j] += g[h + j];
-                    g[h + j] *= wv[h + j];
-                    s[0] += g[h + j];
-                    s[1] += g[h + j] * xh[h + j];
+                for (int q = 0; q < kRows; ++q) {
+                    const int64_t next = n + (kStages - kRows + q) * step;
+                    if (next < N) copy(next, (st == 0 ? kStages : st) - kRows + q);
+                }
+            }
+            if ((st += kRows) == kStages) {
+                st = 0;
+                ph ^= 1u;
+            }
+#pragma unroll
+            for (int q = 0; q < kRows; ++q) {
+                if (q > 0 && n + step >= N) break;
+                const unsigned long long minus_m = pack2(-m[q], -m[q]), rn2 = pack2(rn[q], rn[q]);
+                const float a = s[2 * q] / width, bq = s[2 * q + 1] / width;
+                const unsigned long long minus_a = pack2(-a, -a), minus_b = pack2(-bq, -bq);
+#pragma unroll
+                for (int i = 0; i < kNV; i += kStep) {
+                    const Pairs<V> xp = pairs_at<T, V, TPR, true>(xr[q], i, t, D);
+                    const Pairs<V> gp = pairs_at<T, V, TPR, true>(dr[q], i, t, D);
+                    if constexpr (!kHold) wv[0] = params2<V, TPR>(w, i, t, D, 1.f);
+                    store_pairs<T, V, TPR>(dx + (n + q * step) * D, i, t, D,
+                                           input_gradient<V>(xp, gp, wv[kHold ? i / kStep : 0], minus_m, rn2, minus_a, minus_b));
                 }
             }
         }
-        if constexpr (!kAgain) {
+    } else {
+        float mu = 0.f, r = 0.f;
+        row::Raw<T, V> nx[kKeep ? kNV : 1], nd[kKeep ? kNV : 1];  // the next row
+        if (n0 < N) {
+            mu = __ldg(mean + n0);
+            r = __ldg(rstd + n0);
+            if constexpr (kKeep) {
+                load_row<T, V, kNV, TPR>(nx, x + n0 * ldx, t, D);
+                load_row<T, V, kNV, TPR>(nd, dy + n0 * lddy, t, D);
+            }
+        }
+        for (int64_t n = n0; n < N; n += step, k ^= 1) {
+            const unsigned long long minus_m = pack2(-mu, -mu), rn2 = pack2(r, r);
             if (n + step < N) {
-                load_row<T, V, kNV, TPR>(rx, x + (n + step) * ldx, t, D);
-                load_row<T, V, kNV, TPR>(rd, dy + (n + step) * lddy, t, D);
                 mu = __ldg(mean + n + step);
                 r = __ldg(rstd + n + step);
             }
-        }
-        row::group_sum<TPR>(s, buf[group][k], group, t);
-        const float a = s[0] / width, bq = s[1] / width;
+            const T *xr = x + n * ldx, *dr = dy + n * lddy;
+            row::Raw<T, V> rx[kKeep ? kNV : 1], rd[kKeep ? kNV : 1];
+            if constexpr (kKeep) {
 #pragma unroll
-        for (int i = 0; i < kNV; ++i) {
-            const int c = (i * TPR + t) * V, h = kAgain ? 0 : i * V;
-            if (c < D) {
-                if constexpr (kAgain) {
-                    row::unpack<T, V>(row::load<T, V>(x + n * ldx + c), xh);
-                    row::unpack<T, V>(row::load<T, V>(dy + n * lddy + c), g);
-                    params_at<V>(w, c, 1.f, wv);
-#pragma unroll
-                    for (int j = 0; j < V; ++j) {
-                        xh[j] = (xh[j] - mu) * rn;
-                        g[j] *= wv[j];
-                    }
+                for (int i = 0; i < kNV; ++i) {
+                    rx[i] = nx[i];
+                    rd[i] = nd[i];
                 }
-                float o[V];
+                if (n + step < N) {
+                    load_row<T, V, kNV, TPR>(nx, x + (n + step) * ldx, t, D);
+                    load_row<T, V, kNV, TPR>(nd, dy + (n + step) * lddy, t, D);
+                }
+            }
+            unsigned long long s0 = 0ull, s1 = 0ull;
 #pragma unroll
-                for (int j = 0; j < V; ++j) o[j] = (g[h + j] - a - xh[h + j] * bq) * rn;
-                row::store<T, V>(dx + n * D + c, o);
+            for (int i = 0; i < kNV; i += kStep) {
+                const Pairs<V> xp = kKeep ? pairs_of<T, V>(rx + (kKeep ? i : 0)) : pairs_at<T, V, TPR, false>(xr, i, t, D);
+                const Pairs<V> gp = kKeep ? pairs_of<T, V>(rd + (kKeep ? i : 0)) : pairs_at<T, V, TPR, false>(dr, i, t, D);
+                if constexpr (!kHold) wv[0] = params2<V, TPR>(w, i, t, D, 1.f);
+                add_columns<V>(xp, gp, wv[kHold ? i / kStep : 0], minus_m, rn2, dw + i / kStep * kP, db + i / kStep * kP, s0, s1);
+            }
+            float s[2] = {lo_of(s0) + hi_of(s0), lo_of(s1) + hi_of(s1)};
+            row::group_sum<TPR>(s, buf[group][k], group, t);
+            const float a = s[0] / width, bq = s[1] / width;
+            const unsigned long long minus_a = pack2(-a, -a), minus_b = pack2(-bq, -bq);
+#pragma unroll
+            for (int i = 0; i < kNV; i += kStep) {
+                const Pairs<V> xp = kKeep ? pairs_of<T, V>(rx + (kKeep ? i : 0)) : pairs_at<T, V, TPR, false>(xr, i, t, D);
+                const Pairs<V> gp = kKeep ? pairs_of<T, V>(rd + (kKeep ? i : 0)) : pairs_at<T, V, TPR, false>(dr, i, t, D);
+                if constexpr (!kHold) wv[0] = params2<V, TPR>(w, i, t, D, 1.f);
+                store_pairs<T, V, TPR>(dx + n * D, i, t, D,
+                                       input_gradient<V>(xp, gp, wv[kHold ? i / kStep : 0], minus_m, rn2, minus_a, minus_b));
             }
         }
     }
+    // the rings are done with (all copies were waited for): the groups' sums take their place
+    float *comb = reinterpret_cast<float *>(ring_raw);
+    const bool pw_ok = pw != nullptr, pb_ok = pb != nullptr;
     // the groups' sums, added in group order
     if constexpr (kGroups > 1) {
+        unsigned long long *cp = reinterpret_cast<unsigned long long *>(comb);
         for (int q = 1; q < kGroups; ++q) {
             __syncthreads();
             if (group == q) {
 #pragma unroll
-                for (int e = 0; e < E; ++e) {
-                    comb[(2 * e) * TPR + t] = dw[e];
-                    comb[(2 * e + 1) * TPR + t] = db[e];
+                for (int e = 0; e < E / 2; ++e) {
+                    cp[(2 * e) * TPR + t] = dw[e];
+                    cp[(2 * e + 1) * TPR + t] = db[e];
                 }
             }
             __syncthreads();
             if (group == 0) {
 #pragma unroll
-                for (int e = 0; e < E; ++e) {
-                    dw[e] += comb[(2 * e) * TPR + t];
-                    db[e] += comb[(2 * e + 1) * TPR + t];
+                for (int e = 0; e < E / 2; ++e) {
+                    dw[e] = row::add2(dw[e], cp[(2 * e) * TPR + t]);
+                    db[e] = row::add2(db[e], cp[(2 * e + 1) * TPR + t]);
                 }
             }
         }
     }
     if (group == 0) {
-        float *pw = part + static_cast<int64_t>(blockIdx.x) * 2 * D;
+        pw += static_cast<int64_t>(blockIdx.x) * 2 * D;
+        pb += static_cast<int64_t>(blockIdx.x) * 2 * D;
+        if (V > 1 && (reinterpret_cast<uintptr_t>(pw) | reinterpret_cast<uintptr_t>(pb)) % 16 == 0) {
 #pragma unroll
-        for (int i = 0; i < kNV; ++i) {
-            const int c = (i * TPR + t) * V;
-#pragma unroll
-            for (int j = 0; j < V; ++j) {
+            for (int e = 0; e < E / 2; e += 2) {  // four neighbouring columns
+                const int c = (e / kP * kStep * TPR + t) * V + e % kP * 2;
                 if (c < D) {
-                    pw[c + j] = dw[i * V + j];
-                    pw[D + c + j] = db[i * V + j];
+                    if (pw_ok) *reinterpret_cast<float4 *>(pw + c) = make_float4(lo_of(dw[e]), hi_of(dw[e]), lo_of(dw[e + 1]), hi_of(dw[e + 1]));
+                    if (pb_ok) *reinterpret_cast<float4 *>(pb + c) = make_float4(lo_of(db[e]), hi_of(db[e]), lo_of(db[e + 1]), hi_of(db[e + 1]));
+                }
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < E / 2; ++e) {
+                const int c = (e / kP * kStep * TPR + t) * V + e % kP * 2, d = V == 1 ? c + TPR : c + 1;
+                if (c < D) {
+                    if (pw_ok) pw[c] = lo_of(dw[e]);
+                    if (pb_ok) pb[c] = lo_of(db[e]);
+                }
+                if (d < D) {
+                    if (pw_ok) pw[d] = hi_of(dw[e]);
+                    if (pb_ok) pb[d] = hi_of(db[e]);
                 }
             }
         }
@@ -325,7 +601,7 @@ __global__ void __launch_bounds__(1024)
 template <typename T>
 __global__ void __launch_bounds__(256)
     norm_long_params_kernel(const T *dy, int64_t lddy, const T *x, int64_t ldx, const float *mean, const float *rstd,
-                            int64_t N, int64_t D, float *part)
+                            int64_t N, int64_t D, float *pw, float *pb)
 {
     const int64_t c = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
     if (c >= D) return;
@@ -335,34 +611,54 @@ __global__ void __launch_bounds__(256)
         dw += g * (row::to_f32(x[n * ldx + c]) - __ldg(mean + n)) * __ldg(rstd + n);
         db += g;
     }
-    float *pw = part + static_cast<int64_t>(blockIdx.y) * 2 * D;
-    pw[c] = dw;
-    pw[D + c] = db;
+    const int64_t part = static_cast<int64_t>(blockIdx.y) * 2 * D;
+    if (pw) pw[part + c] = dw;
+    if (pb) pb[part + c] = db;
 }
 
-// dw and db: the sums of the parts (32 columns and 32 interleaved shares of the parts a block, the
-// shares added in order)
+// dw and db: the sums of the parts.  A block takes 32 columns; V of them a thread (4 where D is even, so that every
+// part starts on 16 bytes), the parts in 32 V interleaved shares, so that all loads of a thread are on their way
+// at once; the shares are added in order
+template <int V>
 __global__ void __launch_bounds__(1024)
     norm_params_kernel(const float *part, int parts, int64_t D, float *dw, float *db)
 {
-    __shared__ float sh[32][33];
-    const int lane = threadIdx.x & 31, q = threadIdx.x >> 5;
-    const int64_t c = static_cast<int64_t>(blockIdx.x) * 32 + lane;
-    float s = 0.f;
+    constexpr int kLanes = 32 / V, kShares = 32 * V;
+    __shared__ float sh[kShares][33];
+    tc::wait_prior_grid();
+    const int q = threadIdx.x % kLanes, share = threadIdx.x / kLanes;
+    const int64_t c = static_cast<int64_t>(blockIdx.x) * 32 + q * V;
+    float s[V] = {};
     if (c < 2 * D) {
-#pragma unroll 8
-        for (int p = q; p < parts; p += 32) s += part[static_cast<int64_t>(p) * 2 * D + c];
+#pragma unroll 4
+        for (int p = share; p < parts; p += kShares) {
+            const float *at = part + static_cast<int64_t>(p) * 2 * D + c;
+            if constexpr (V == 4) {
+                const float4 v = *reinterpret_cast<const float4 *>(at);
+                s[0] += v.x;
+                s[1] += v.y;
+                s[2] += v.z;
+                s[3] += v.w;
+            } else {
+                s[0] += *at;
+            }
+        }
     }
-    sh[q][lane] = s;
+#pragma unroll
+    for (int j = 0; j < V; ++j) sh[share][q * V + j] = s[j];
     __syncthreads();
-    // warp q adds column q's shares
-    s = row::warp_sum(sh[lane][q]);
-    const int64_t d = static_cast<int64_t>(blockIdx.x) * 32 + q;
+    // warp w adds column w's shares
+    const int w = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    float sum = 0.f;
+#pragma unroll
+    for (int j = 0; j < V; ++j) sum += sh[lane + 32 * j][w];
+    sum = row::warp_sum(sum);
+    const int64_t d = static_cast<int64_t>(blockIdx.x) * 32 + w;
     if (lane == 0 && d < 2 * D) {
         if (d < D) {
-            if (dw) dw[d] = s;
+            if (dw) dw[d] = sum;
         } else if (db) {
-            db[d - D] = s;
+            db[d - D] = sum;
         }
     }
 }
@@ -377,10 +673,15 @@ struct Args {
     const float *w, *b, *mean_in, *rstd_in;
     float eps;
     void *y;
-    float *mean, *rstd, *part;
+    float *mean, *rstd;
+    float *dw, *db, *part;
     int *parts;  // written: parts of the sums
     cudaStream_t stream;
 };
+
+// where the first part of the sums goes: to the gradients themselves if it is the only one
+float *first_dw(const Args &a) { return *a.parts == 1 ? a.dw : a.part; }
+float *first_db(const Args &a) { return *a.parts == 1 ? a.db : a.part + a.D; }
 
 // columns of a thread: two 16-byte words, or 8 single elements; twice that past 8192 columns, which 1024
 // threads share
@@ -399,26 +700,30 @@ int group_threads(int e, int64_t D)
 }
 
 // blocks of the backward pass' main launch (and parts of its sums)
-int64_t backward_blocks(int e, int64_t N, int64_t D)
+int64_t backward_blocks(int e, bool words, int64_t N, int64_t D)
 {
     if (D > kRegisterColumns) return least(N, 16);
     const int tpr = group_threads(e, D), groups = block_threads(tpr) / tpr;
-    return least((N + groups - 1) / groups, static_cast<int64_t>(row::sm_count()) * backward_residents(tpr));
+    return least((N + groups - 1) / groups, static_cast<int64_t>(row::sm_count()) * residents(tpr, words, true));
 }
 
 // the most parts of any form of a call
 int64_t most_parts(int64_t N, int64_t D)
 {
-    const int64_t a = backward_blocks(8, N, D), b = backward_blocks(16, N, D);
+    const int64_t a = backward_blocks(8, true, N, D), b = backward_blocks(16, true, N, D);  // off whole words: fewer
     return a > b ? a : b;
 }
 
 template <typename T, int V, int E, int TPR>
 cudaError_t forward_one(const Args &a)
 {
-    constexpr int kT = block_threads(TPR), kGroups = kT / TPR;
-    const int64_t blocks = least((a.N + kGroups - 1) / kGroups, static_cast<int64_t>(row::sm_count()) * forward_residents(TPR));
-    norm_kernel<T, V, E, TPR><<<static_cast<unsigned>(blocks), kT, 0, a.stream>>>(
+    constexpr int kT = block_threads(TPR), kGroups = kT / TPR, kStage = E * TPR * static_cast<int>(sizeof(T));
+    constexpr int bytes = V > 1 ? stages_of(kStage, kGroups, residents(TPR, (V > 1), false)) * kStage * kGroups : 0;
+    static SmemAttrCache attr_cache;
+    const cudaError_t attr = smem_attr_once(norm_kernel<T, V, E, TPR>, bytes, attr_cache);
+    if (attr != cudaSuccess) return attr;
+    const int64_t blocks = least((a.N + kGroups - 1) / kGroups, static_cast<int64_t>(row::sm_count()) * residents(TPR, (V > 1), false));
+    norm_kernel<T, V, E, TPR><<<static_cast<unsigned>(blocks), kT, bytes, a.stream>>>(
         static_cast<const T *>(a.x), a.ldx, a.N, static_cast<int>(a.D), a.w, a.b, a.eps, static_cast<T *>(a.y), a.mean,
         a.rstd);
     return cudaGetLastError();
@@ -427,10 +732,18 @@ cudaError_t forward_one(const Args &a)
 template <typename T, int V, int E, int TPR>
 cudaError_t backward_one(const Args &a)
 {
-    *a.parts = static_cast<int>(backward_blocks(thread_columns<T, V>(), a.N, a.D));
-    norm_backward_kernel<T, V, E, TPR><<<static_cast<unsigned>(*a.parts), block_threads(TPR), 0, a.stream>>>(
+    constexpr int kT = block_threads(TPR), kGroups = kT / TPR, kStage = 2 * E * TPR * static_cast<int>(sizeof(T));
+    constexpr int stages = stages_of(kStage, kGroups, residents(TPR, (V > 1), true));
+    constexpr int ring = V > 1 && stages >= 2 ? stages * kStage * kGroups : 0;
+    constexpr int comb = kGroups > 1 ? 2 * E * TPR * static_cast<int>(sizeof(float)) : 0;
+    constexpr int bytes = ring > comb ? ring : comb;
+    static SmemAttrCache attr_cache;
+    const cudaError_t attr = smem_attr_once(norm_backward_kernel<T, V, E, TPR>, bytes, attr_cache);
+    if (attr != cudaSuccess) return attr;
+    *a.parts = static_cast<int>(backward_blocks(thread_columns<T, V>(), V > 1, a.N, a.D));
+    norm_backward_kernel<T, V, E, TPR><<<static_cast<unsigned>(*a.parts), kT, bytes, a.stream>>>(
         static_cast<const T *>(a.dy), a.lddy, static_cast<const T *>(a.x), a.ldx, a.mean_in, a.rstd_in, a.w, a.N,
-        static_cast<int>(a.D), static_cast<T *>(a.y), a.part);
+        static_cast<int>(a.D), static_cast<T *>(a.y), first_dw(a), first_db(a));
     return cudaGetLastError();
 }
 
@@ -493,12 +806,12 @@ cudaError_t backward(const Args &a)
             static_cast<const T *>(a.dy), a.lddy, static_cast<const T *>(a.x), a.ldx, a.mean_in, a.rstd_in, a.w, a.N,
             a.D, static_cast<T *>(a.y));
         const cudaError_t e = cudaGetLastError();
-        if (e != cudaSuccess || !a.part) return e;
-        *a.parts = static_cast<int>(backward_blocks(8, a.N, a.D));
+        if (e != cudaSuccess || (!a.dw && !a.db)) return e;
+        *a.parts = static_cast<int>(backward_blocks(8, true, a.N, a.D));
         const dim3 grid(static_cast<unsigned>((a.D + 255) / 256), static_cast<unsigned>(*a.parts));
         norm_long_params_kernel<T><<<grid, 256, 0, a.stream>>>(static_cast<const T *>(a.dy), a.lddy,
                                                                static_cast<const T *>(a.x), a.ldx, a.mean_in,
-                                                               a.rstd_in, a.N, a.D, a.part);
+                                                               a.rstd_in, a.N, a.D, first_dw(a), first_db(a));
         return cudaGetLastError();
     }
     return whole_words<T>(a) ? launch_rows<T, 16 / sizeof(T), true>(a) : launch_rows<T, 1, true>(a);
@@ -508,7 +821,8 @@ cudaError_t backward(const Args &a)
 
 size_t layer_norm_workspace(int64_t N, int64_t D)
 {
-    return static_cast<size_t>(norm::most_parts(N, D)) * 2 * static_cast<size_t>(D) * sizeof(float);
+    const int64_t parts = norm::most_parts(N, D);
+    return parts > 1 ? static_cast<size_t>(parts) * 2 * static_cast<size_t>(D) * sizeof(float) : 0;
 }
 
 cudaError_t launch_layer_norm(const void *x, int dtype, int64_t N, int64_t D, int64_t ldx, const float *w,
@@ -545,6 +859,8 @@ cudaError_t launch_layer_norm_backward(const void *dy, int64_t lddy, const void 
     a.w = w;
     a.y = dx;
     int parts = 0;
+    a.dw = dw;
+    a.db = db;
     a.part = part;
     a.parts = &parts;
     a.stream = stream;
@@ -552,10 +868,20 @@ cudaError_t launch_layer_norm_backward(const void *dy, int64_t lddy, const void 
         const cudaError_t e = dtype == CCI_F32 ? norm::backward<float>(a) : norm::backward<uint16_t>(a);
         if (e != cudaSuccess) return e;
     }
-    if (!dw && !db) return cudaSuccess;
-    norm::norm_params_kernel<<<static_cast<unsigned>((2 * D + 31) / 32), 1024, 0, stream>>>(
-        part, parts, D, dw, db);
-    return cudaGetLastError();
+    if (parts == 1 || (!dw && !db)) return cudaSuccess;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(static_cast<unsigned>((2 * D + 31) / 32));
+    cfg.blockDim = dim3(1024);
+    cfg.stream = stream;
+    cudaLaunchAttribute la[1];
+    la[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    la[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = la;
+    cfg.numAttrs = 1;
+    const cudaError_t e = D % 2 == 0
+                              ? cudaLaunchKernelEx(&cfg, norm::norm_params_kernel<4>, const_cast<const float *>(part), parts, D, dw, db)
+                              : cudaLaunchKernelEx(&cfg, norm::norm_params_kernel<1>, const_cast<const float *>(part), parts, D, dw, db);
+    return e != cudaSuccess ? e : cudaGetLastError();
 }
 
 }  // namespace cci

@@ -115,6 +115,43 @@ __device__ __forceinline__ void store(T *p, const float *f)
     }
 }
 
+// two fp32 at a time (one instruction for both; ffma2 of cci_common.cuh is the third of them)
+__device__ __forceinline__ unsigned long long add2(unsigned long long a, unsigned long long b)
+{
+    unsigned long long r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+
+__device__ __forceinline__ unsigned long long mul2(unsigned long long a, unsigned long long b)
+{
+    unsigned long long r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+
+// the elements of a vector (V > 1) as V / 2 pairs; pairs to memory
+template <typename T, int V>
+__device__ __forceinline__ void unpack2(const Raw<T, V> &r, unsigned long long *p)
+{
+    float f[V];
+    unpack<T, V>(r, f);
+#pragma unroll
+    for (int j = 0; j < V / 2; ++j) p[j] = pack2(f[2 * j], f[2 * j + 1]);
+}
+
+template <typename T, int V>
+__device__ __forceinline__ void store2(T *to, const unsigned long long *p)
+{
+    float f[V];
+#pragma unroll
+    for (int j = 0; j < V / 2; ++j) {
+        f[2 * j] = lo_of(p[j]);
+        f[2 * j + 1] = hi_of(p[j]);
+    }
+    store<T, V>(to, f);
+}
+
 __device__ __forceinline__ float warp_sum(float v)
 {
 #pragma unroll
@@ -161,6 +198,35 @@ __device__ __forceinline__ void group_sum(float (&v)[N], float *buf, int group, 
             v[i] = warp_sum(s);
         }
     }
+}
+
+// the same for four values at once, which share the steps: a lane carries one of them from the third on (13
+// exchanges in all, 40 for four sums apart)
+template <int TPR>
+__device__ __forceinline__ void group_sum4(float (&v)[4], float *buf, int group, int t)
+{
+    const int lane = t & 31;
+    const bool hi = lane & 16, up = lane & 8;
+    float a = hi ? v[2] : v[0], b = hi ? v[3] : v[1];
+    a += __shfl_xor_sync(0xffffffffu, hi ? v[0] : v[2], 16);
+    b += __shfl_xor_sync(0xffffffffu, hi ? v[1] : v[3], 16);
+    float s = up ? b : a;
+    s += __shfl_xor_sync(0xffffffffu, up ? a : b, 8);
+#pragma unroll
+    for (int o = 4; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+    if constexpr (TPR > 32) {
+        constexpr int kW = TPR / 32;
+        const int mine = lane >> 3, j = lane & 7;
+        if (j == 0) buf[mine * kW + (t >> 5)] = s;
+        group_sync<TPR>(group);
+        s = j < kW ? buf[mine * kW + j] : 0.f;
+#pragma unroll
+        for (int w = 8; w < kW; w += 8) s += buf[mine * kW + w + j];
+#pragma unroll
+        for (int o = 4; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = __shfl_sync(0xffffffffu, s, 8 * i);
 }
 
 }  // namespace row
