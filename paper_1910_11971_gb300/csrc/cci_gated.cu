@@ -200,13 +200,15 @@ __global__ void __launch_bounds__(256)
         row::unpack<T, 8>(row::load_once<T, 8>(dh + i), h);
         row::unpack<float, 8>(row::load_once<float, 8>(g + i), gv);
         row::unpack<float, 8>(row::load_once<float, 8>(u + i), uv);
+        with_act(act, [&](auto code) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            float a;
-            const float s = slope_of(gv[j], act, a);
-            gv[j] = h[j] * uv[j] * s;
-            uv[j] = h[j] * a;
-        }
+            for (int j = 0; j < 8; ++j) {
+                float a;
+                const float s = slope_of<decltype(code)::value>(gv[j], a);
+                gv[j] = h[j] * uv[j] * s;
+                uv[j] = h[j] * a;
+            }
+        });
         store_planes<P>(dg + i, n, gv);
         store_planes<P>(du + i, n, uv);
     }
@@ -220,7 +222,7 @@ unsigned grid_of(int64_t n)
 
 // places in the workspace (bytes from its start; 0 sized where a call does not need one)
 struct Layout {
-    size_t x, wg, wu, dg, du, total;
+    size_t x, wg, wu, dg, du, parts, total;
 };
 
 Layout layout(int dtype, int64_t N, int64_t D, int64_t F, int call)
@@ -240,6 +242,12 @@ Layout layout(int dtype, int64_t N, int64_t D, int64_t F, int call)
     l.wu = take(dense, F * D);
     l.dg = take(call == CCI_GATED_BACKWARD, N * F);
     l.du = take(call == CCI_GATED_BACKWARD, N * F);
+    l.parts = at;
+    if (call == CCI_GATED_BACKWARD) {  // the products follow each other: one place for both
+        const int terms = f32 ? 6 : 1;
+        const size_t dx = plan(kDx, N, D, F, terms).part_bytes, dw = plan(kDw, F, D, N, terms).part_bytes;
+        at += round256(dx > dw ? dx : dw);
+    }
     l.total = at;
     return l;
 }
@@ -402,6 +410,7 @@ cudaError_t launch_gated_backward(const GatedArgs &a, cudaStream_t stream)
     j.terms = f32 ? 6 : 1;
     j.out_f32 = f32;
     j.status = a.status;
+    j.parts = reinterpret_cast<float *>(base + l.parts);
     j.a[0] = Operand{dg, a.N, a.F, planes};
     j.a[1] = Operand{du, a.N, a.F, planes};
     if (a.dX) {

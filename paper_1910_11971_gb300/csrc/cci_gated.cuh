@@ -45,13 +45,17 @@ struct Params {
     int act;             // cci_activation
     int out_f32;
     int save;            // forward: g and u are written too (fp32)
+    // tiles below `whole` are computed whole, one CTA (pair) after the other; the reductions of the rest, where a
+    // last round of tiles would leave most SMs idle, are laid end to end and cut evenly over all of them, their parts
+    // written in fp32 and added by join_kernel
+    int whole;
     uint32_t *status;
 };
 
 // [0] gate, [1] up where an operand or output is one of two
 struct Maps {
     CUtensorMap a[2], b[2], out[2];
-    CUtensorMap save[2];
+    CUtensorMap save[2];  // forward: g and u; else [0]: parts
 };
 
 template <int CG, int BN>
@@ -81,48 +85,60 @@ struct Smem {
 static_assert(sizeof(Smem) <= 1024, "barriers");
 
 // ---- activations, in fp32 ----
-// exp and the quotient in their fast forms (within a few 2^-23 here): the exact ones branch, and one thread's
-// 32 elements then run one after the other.  The epilogue of a 256 x 256 tile of SiLU took more than
-// twice the time of its products with them (prompt of 1999 tokens, 4096 -> 8192: 268 us on the device, 164 with the fast ones)
+// exp and the quotient in their fast forms (within a few 2^-23 here): the exact ones branch, and so does a choice
+// of activation per element, and one thread's elements then run one after the other.  A 256 x 256 tile's epilogue
+// of SiLU took 60 us with both, 19 with the fast forms alone, and takes 4 with the choice made once (prompt of
+// 1999 tokens, 4096 -> 8192: 268, 164 and 143 us on the device)
 __device__ __forceinline__ float sigmoid(float g) { return __fdividef(1.f, 1.f + __expf(-g)); }
 
-__device__ __forceinline__ float act_of(float g, int act)
+template <int ACT>
+__device__ __forceinline__ float act_of(float g)
 {
-    switch (act) {
-        case CCI_ACT_SILU: return __fdividef(g, 1.f + __expf(-g));
-        case CCI_ACT_GELU: return 0.5f * g * erfcf(g * -0.70710678f);
-        case CCI_ACT_GELU_TANH: return g * sigmoid(1.5957691f * (g + 0.044715f * g * g * g));
-        case CCI_ACT_RELU: return g > 0.f ? g : (g != g ? g : 0.f);
-        default: return sigmoid(g);
-    }
+    if constexpr (ACT == CCI_ACT_SILU) return g * sigmoid(g);
+    if constexpr (ACT == CCI_ACT_GELU) return 0.5f * g * erfcf(g * -0.70710678f);
+    if constexpr (ACT == CCI_ACT_GELU_TANH) return g * sigmoid(1.5957691f * (g + 0.044715f * g * g * g));
+    if constexpr (ACT == CCI_ACT_RELU) return g > 0.f ? g : (g != g ? g : 0.f);
+    return sigmoid(g);
 }
 
 // act'(g), act(g) to a
-__device__ __forceinline__ float slope_of(float g, int act, float &a)
+template <int ACT>
+__device__ __forceinline__ float slope_of(float g, float &a)
+{
+    if constexpr (ACT == CCI_ACT_GELU) {
+        const float c = 0.5f * erfcf(g * -0.70710678f);
+        a = g * c;
+        return c + g * 0.39894228f * __expf(-0.5f * g * g);
+    }
+    if constexpr (ACT == CCI_ACT_RELU) {
+        a = act_of<ACT>(g);
+        return g > 0.f ? 1.f : 0.f;
+    }
+    if constexpr (ACT == CCI_ACT_GELU_TANH) {
+        // 0.5 (1 + tanh(z)) = sigmoid(2 z)
+        const float g2 = g * g, p = sigmoid(1.5957691f * (g + 0.044715f * g2 * g));
+        a = g * p;
+        return p + g * p * (1.f - p) * 1.5957691f * (1.f + 3.f * 0.044715f * g2);
+    }
+    const float p = sigmoid(g);
+    if constexpr (ACT == CCI_ACT_SILU) {
+        a = g * p;
+        return p * (1.f + g * (1.f - p));
+    }
+    a = p;
+    return p * (1.f - p);
+}
+
+// f(activation's code as a constant): one choice for a whole run of elements
+template <typename Fn>
+__device__ __forceinline__ void with_act(int act, Fn f)
 {
     switch (act) {
-        case CCI_ACT_SILU: {
-            const float p = sigmoid(g);
-            a = act_of(g, act);
-            return p * (1.f + g * (1.f - p));
-        }
-        case CCI_ACT_GELU: {
-            const float c = 0.5f * erfcf(g * -0.70710678f);
-            a = g * c;
-            return c + g * 0.39894228f * __expf(-0.5f * g * g);
-        }
-        case CCI_ACT_GELU_TANH: {
-            // 0.5 (1 + tanh(z)) = sigmoid(2 z)
-            const float g2 = g * g, p = sigmoid(1.5957691f * (g + 0.044715f * g2 * g));
-            a = g * p;
-            return p + g * p * (1.f - p) * 1.5957691f * (1.f + 3.f * 0.044715f * g2);
-        }
-        case CCI_ACT_RELU: a = act_of(g, act); return g > 0.f ? 1.f : 0.f;
-        default: {
-            const float p = sigmoid(g);
-            a = p;
-            return p * (1.f - p);
-        }
+        case CCI_ACT_SILU: f(std::integral_constant<int, CCI_ACT_SILU>{}); break;
+        case CCI_ACT_GELU: f(std::integral_constant<int, CCI_ACT_GELU>{}); break;
+        case CCI_ACT_GELU_TANH: f(std::integral_constant<int, CCI_ACT_GELU_TANH>{}); break;
+        case CCI_ACT_RELU: f(std::integral_constant<int, CCI_ACT_RELU>{}); break;
+        default: f(std::integral_constant<int, CCI_ACT_SIGMOID>{});
     }
 }
 
@@ -268,6 +284,32 @@ __device__ __forceinline__ void tile_at(const Params &p, int tile, int mt_all, i
 // So it adds kChunk stages at a time, and the output warps add the chunks in registers, to the nearest.
 constexpr int kChunk = 8;
 
+// a CTA's (or pair's) work: stages s0 .. s0 + n - 1 of a tile's reduction; part: -1 if that is all of it, else where
+// its sums go (parts of CG 128 rows)
+struct Work {
+    int tile, s0, n, part;
+};
+
+// unit `unit` of `units`, its j-th piece of work; false: there is none.  per: stages of a tile
+__device__ __forceinline__ bool work_at(const Params &p, int unit, int units, int per, int j, Work &w)
+{
+    const int count = unit < p.whole ? (p.whole - unit + units - 1) / units : 0;
+    if (j < count) {
+        w = Work{unit + j * units, 0, per, -1};
+        return true;
+    }
+    const int64_t rest = static_cast<int64_t>(p.tiles - p.whole) * per;
+    const int64_t b0 = rest * unit / units, b1 = rest * (unit + 1) / units;
+    const int k = j - count, t0 = static_cast<int>(b0 / per);
+    const int64_t cut = static_cast<int64_t>(t0 + 1) * per;  // where the next tile begins: a share is shorter than a tile
+    const int64_t from = k == 0 ? b0 : cut, to = k == 0 && b1 > cut ? cut : b1;
+    if (k > 1 || from >= to) return false;
+    const int tile = t0 + k;
+    w = Work{p.whole + tile, static_cast<int>(from - static_cast<int64_t>(tile) * per), static_cast<int>(to - from), 2 * unit + k};
+    if (w.n == per) w.part = -1;
+    return true;
+}
+
 template <int MODE, int CG, int BN, bool SPLIT>
 __global__ void __launch_bounds__(Cfg<CG, BN>::kThreads, 1)
     product_kernel(const Params p, const __grid_constant__ Maps maps)
@@ -291,6 +333,7 @@ __global__ void __launch_bounds__(Cfg<CG, BN>::kThreads, 1)
     const int mt_all = MODE == kDw ? 2 * p.m_tiles : p.m_tiles;
     const int per_tile = p.pairs * p.terms * p.k_stages;  // stages of a tile
     const int chunk_len = SPLIT ? kChunk : per_tile;
+    Work work;
 
     if (tid == 0) {
         for (int s = 0; s < kStages; ++s) {
@@ -334,9 +377,9 @@ __global__ void __launch_bounds__(Cfg<CG, BN>::kThreads, 1)
             int s = 0, it = 0;
             uint32_t ph = 1u;  // a fresh barrier's preceding phase counts as complete
             bool ok = true;
-            for (int tile = first; tile < p.tiles && ok; tile += step) {
+            for (int j = 0; ok && work_at(p, first, step, per_tile, j, work); ++j) {
                 int mt, nt;
-                tile_at(p, tile, mt_all, mt, nt);
+                tile_at(p, work.tile, mt_all, mt, nt);
                 int which = 0;  // dW: gate or up
                 if (MODE == kDw && mt >= p.m_tiles) {
                     which = 1;
@@ -344,46 +387,51 @@ __global__ void __launch_bounds__(Cfg<CG, BN>::kThreads, 1)
                 }
                 const int m0 = (mt * CG + static_cast<int>(rank)) * C::kM;
                 const int n0 = nt * kNOut;
-                for (int pair = 0; pair < p.pairs && ok; ++pair) {
-                    const CUtensorMap *ma = &maps.a[MODE == kDw ? which : pair];
-                    for (int t = 0; t < p.terms && ok; ++t) {
-                        int pa, pb;
-                        term_planes(t, p.terms, pa, pb);
-                        for (int ks = 0; ks < p.k_stages; ++ks, ++it) {
-                            ok = tc::mbar_wait(&S->empty[s], ph, abort, p.status);
-                            if (!ok) break;
-                            const uint32_t sa = base + s * C::kStage, sb = sa + C::kABytes;
-                            uint32_t bar = tc::smem_u32(&S->full[s]);
-                            if (rank == 0) tc::mbar_arrive_expect_tx(&S->full[s], bytes);
-                            if constexpr (CG == 2) bar = ws::map_to_rank(bar, 0);
-                            const int k0 = ks * 64;
-                            if constexpr (kAMn) {
+                // the stage within its product of planes, that within its pair
+                int ks = work.s0 % p.k_stages, t = work.s0 / p.k_stages % p.terms, pair = work.s0 / (p.k_stages * p.terms);
+                int pa, pb;
+                term_planes(t, p.terms, pa, pb);
+                const CUtensorMap *ma = &maps.a[MODE == kDw ? which : pair];
+                for (int i = 0; i < work.n; ++i, ++it) {
+                    ok = tc::mbar_wait(&S->empty[s], ph, abort, p.status);
+                    if (!ok) break;
+                    const uint32_t sa = base + s * C::kStage, sb = sa + C::kABytes;
+                    uint32_t bar = tc::smem_u32(&S->full[s]);
+                    if (rank == 0) tc::mbar_arrive_expect_tx(&S->full[s], bytes);
+                    if constexpr (CG == 2) bar = ws::map_to_rank(bar, 0);
+                    const int k0 = ks * 64;
+                    if constexpr (kAMn) {
 #pragma unroll
-                                for (int i = 0; i < C::kM / 64; ++i)
-                                    load_3d<CG>(sa + i * 8192, ma, m0 + 64 * i, k0, pa, bar);
-                            } else {
-                                load_3d<CG>(sa, ma, k0, m0, pa, bar);
-                            }
-                            if constexpr (MODE == kForward) {
-                                if constexpr (CG == 2) {
-                                    // the even CTA holds the gate's rows, the odd one the up projection's
-                                    load_3d<CG>(sb, &maps.b[rank], k0, n0, pb, bar);
-                                } else {
-                                    load_3d<CG>(sb, &maps.b[0], k0, n0, pb, bar);
-                                    load_3d<CG>(sb + C::kBBytes / 2, &maps.b[1], k0, n0, pb, bar);
-                                }
-                            } else {
-                                const CUtensorMap *mb = &maps.b[MODE == kDx ? pair : 0];
-                                const int nb = n0 + static_cast<int>(rank) * C::kBRows;
-#pragma unroll
-                                for (int i = 0; i < C::kBRows / 64; ++i)
-                                    load_3d<CG>(sb + i * 8192, mb, nb + 64 * i, k0, pb, bar);
-                            }
-                            if (++s == kStages) {
-                                s = 0;
-                                ph ^= 1u;
-                            }
+                        for (int q = 0; q < C::kM / 64; ++q) load_3d<CG>(sa + q * 8192, ma, m0 + 64 * q, k0, pa, bar);
+                    } else {
+                        load_3d<CG>(sa, ma, k0, m0, pa, bar);
+                    }
+                    if constexpr (MODE == kForward) {
+                        if constexpr (CG == 2) {
+                            // the even CTA holds the gate's rows, the odd one the up projection's
+                            load_3d<CG>(sb, &maps.b[rank], k0, n0, pb, bar);
+                        } else {
+                            load_3d<CG>(sb, &maps.b[0], k0, n0, pb, bar);
+                            load_3d<CG>(sb + C::kBBytes / 2, &maps.b[1], k0, n0, pb, bar);
                         }
+                    } else {
+                        const CUtensorMap *mb = &maps.b[MODE == kDx ? pair & 1 : 0];
+                        const int nb = n0 + static_cast<int>(rank) * C::kBRows;
+#pragma unroll
+                        for (int q = 0; q < C::kBRows / 64; ++q) load_3d<CG>(sb + q * 8192, mb, nb + 64 * q, k0, pb, bar);
+                    }
+                    if (++s == kStages) {
+                        s = 0;
+                        ph ^= 1u;
+                    }
+                    if (++ks == p.k_stages) {
+                        ks = 0;
+                        if (++t == p.terms) {
+                            t = 0;
+                            ++pair;
+                            if (MODE == kDx) ma = &maps.a[pair & 1];
+                        }
+                        term_planes(t, p.terms, pa, pb);
                     }
                 }
             }
@@ -404,8 +452,8 @@ __global__ void __launch_bounds__(Cfg<CG, BN>::kThreads, 1)
             bool ok = true;
             const uint64_t da0 = tile_desc<kAMn>(base), db0 = tile_desc<kBMn>(base + C::kABytes);
             const uint32_t empty0 = tc::smem_u32(&S->empty[0]);
-            for (int tile = first; tile < p.tiles && ok; tile += step) {
-                for (int left = per_tile; left > 0 && ok; left -= chunk_len, ++t) {
+            for (int j = 0; ok && work_at(p, first, step, per_tile, j, work); ++j) {
+                for (int left = work.n; left > 0 && ok; left -= chunk_len, ++t) {
                     const int acc = t & 1, n = left < chunk_len ? left : chunk_len;
                     if (t >= 2) ok = tc::mbar_wait<CG == 2>(&S->acc_empty[acc], ((t >> 1) - 1) & 1, abort, p.status);
                     if (!ok) break;
@@ -499,9 +547,9 @@ __global__ void __launch_bounds__(Cfg<CG, BN>::kThreads, 1)
             }
             ++t;
         };
-        for (int tile = first; tile < p.tiles && ok; tile += step) {
+        for (int j = 0; ok && work_at(p, first, step, per_tile, j, work); ++j) {
             int mt, nt;
-            tile_at(p, tile, mt_all, mt, nt);
+            tile_at(p, work.tile, mt_all, mt, nt);
             int which = 0;
             if (MODE == kDw && mt >= p.m_tiles) {
                 which = 1;
@@ -518,11 +566,15 @@ __global__ void __launch_bounds__(Cfg<CG, BN>::kThreads, 1)
                         put(v, &maps.save[0], n0 + c, r0);
                         put(u, &maps.save[1], n0 + c, r0);
                     }
+                    with_act(p.act, [&](auto act) {
 #pragma unroll
-                    for (int j = 0; j < 32; ++j)
-                        v[j] = __float_as_uint(act_of(__uint_as_float(v[j]), p.act) * __uint_as_float(u[j]));
+                        for (int j = 0; j < 32; ++j)
+                            v[j] = __float_as_uint(act_of<decltype(act)::value>(__uint_as_float(v[j])) * __uint_as_float(u[j]));
+                    });
                 }
-                if (p.out_f32) {
+                if (MODE != kForward && work.part >= 0) {
+                    put(v, &maps.save[0], c, (work.part * CG + static_cast<int>(rank)) * C::kM);
+                } else if (p.out_f32) {
                     put(v, &maps.out[which], n0 + c, r0);
                 } else if constexpr (kNOut == 32) {
 #pragma unroll
@@ -548,7 +600,7 @@ __global__ void __launch_bounds__(Cfg<CG, BN>::kThreads, 1)
                 for (int q = 0; q < BN / 32; ++q)
 #pragma unroll
                     for (int j = 0; j < 32; ++j) sum[q][j] = 0u;
-                for (int left = per_tile; left > 0 && ok; left -= chunk_len) {
+                for (int left = work.n; left > 0 && ok; left -= chunk_len) {
                     ok = acc_wait();
                     if (!ok) break;
 #pragma unroll
@@ -603,6 +655,65 @@ __global__ void __launch_bounds__(Cfg<CG, BN>::kThreads, 1)
     }
 }
 
+// the tiles whose reductions were cut: the sum of a tile's parts, in their order.  A block takes 8 rows of a tile
+// (blockIdx.x: tile, then rows), a thread 8 columns of one
+template <int MODE, int CG, int BN>
+__global__ void __launch_bounds__(BN) join_kernel(const Params p, const float *parts, void *out0, void *out1, int units)
+{
+    constexpr int kBlocks = CG * 128 / 8;
+    const int per = p.pairs * p.terms * p.k_stages;
+    const int rest = static_cast<int>(blockIdx.x) / kBlocks, tile = p.whole + rest;
+    const int row = static_cast<int>(blockIdx.x) % kBlocks * 8 + static_cast<int>(threadIdx.x) / (BN / 8);
+    const int col = static_cast<int>(threadIdx.x) % (BN / 8) * 8;
+    int mt, nt;
+    tile_at(p, tile, MODE == kDw ? 2 * p.m_tiles : p.m_tiles, mt, nt);
+    void *out = out0;
+    if (MODE == kDw && mt >= p.m_tiles) {
+        out = out1;
+        mt -= p.m_tiles;
+    }
+    const int64_t r = static_cast<int64_t>(mt) * CG * 128 + row, c = static_cast<int64_t>(nt) * BN + col;
+    tc::wait_prior_grid();
+    if (r >= p.M || c >= p.N) return;  // N is a multiple of 8
+    // the units whose shares meet the tile: from the one that holds its first stage on
+    const int64_t all = static_cast<int64_t>(p.tiles - p.whole) * per, t0 = static_cast<int64_t>(rest) * per;
+    int unit = static_cast<int>(t0 * units / all);
+    while (all * (unit + 1) / units <= t0) ++unit;
+    float v[8] = {};
+    bool cut = false;
+    for (; unit < units; ++unit) {
+        const int64_t b0 = all * unit / units, b1 = all * (unit + 1) / units;
+        if (b0 >= t0 + per) break;
+        if (b0 <= t0 && b1 >= t0 + per) return;  // computed whole
+        if (b0 == b1) continue;
+        // a unit's second piece if its share began in the tile before
+        const int part = 2 * unit + (b0 < t0 ? 1 : 0);
+        const float4 *at = reinterpret_cast<const float4 *>(parts + (static_cast<int64_t>(part) * CG * 128 + row) * BN + col);
+        const float4 a = at[0], b = at[1];
+        v[0] += a.x;
+        v[1] += a.y;
+        v[2] += a.z;
+        v[3] += a.w;
+        v[4] += b.x;
+        v[5] += b.y;
+        v[6] += b.z;
+        v[7] += b.w;
+        cut = true;
+    }
+    if (!cut) return;
+    const int64_t o = r * p.N + c;
+    if (p.out_f32) {
+        float4 *to = reinterpret_cast<float4 *>(static_cast<float *>(out) + o);
+        to[0] = make_float4(v[0], v[1], v[2], v[3]);
+        to[1] = make_float4(v[4], v[5], v[6], v[7]);
+    } else {
+        uint32_t w[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) w[j] = ws::bf16x2_rn(__float_as_uint(v[2 * j]), __float_as_uint(v[2 * j + 1]));
+        *reinterpret_cast<uint4 *>(static_cast<uint16_t *>(out) + o) = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+}
+
 // ---------------------------------------------------------------------------
 // host
 // ---------------------------------------------------------------------------
@@ -640,11 +751,57 @@ struct Job {
     float *save[2];   // forward: g and u, or null
     int64_t M, N, K;  // rows and columns of an output, length of a reduction
     int terms, act, out_f32;
+    float *parts;     // dX, dW: plan().part_bytes of workspace
     uint32_t *status;
 };
 
+// how a product is tiled: CTAs of a tile, its columns, whether its last tiles' reductions are cut, and the bytes
+// of their parts
+struct Plan {
+    int cg, bn;
+    bool cut;
+    size_t part_bytes;
+};
+
+// The tile whose rounds over the SMs take the fewest cycles.  A 64-deep stage takes its products' time, 512 cycles
+// in a 256 x 256 pair tile, 256 in a 128 x 128 one and 192 in a 128 x 64 one, or that of its copies at about 64
+// bytes a cycle and SM (what L2 gives all SMs at once); a round about 4000 more for the first copies and the last
+// output.  Cutting the last tiles' reductions fills the last round, but writes and reads parts and takes a launch:
+// about 20000 cycles (dX of 4096 tokens, 4096 -> 8192: 256 tiles over 76 pairs, 394 us whole, 291 cut).  The
+// forward pass, whose epilogue wants g and u together, is not cut
+inline Plan plan(Mode mode, int64_t M, int64_t N, int64_t K, int terms)
+{
+    const int64_t sms = ws::sm_count(), outs = mode == kDw ? 2 : 1;
+    const int64_t stages = (K + 63) / 64 * terms * (mode == kDx ? 2 : 1);
+    const int64_t a_rows = mode == kDw || M > 128 ? 128 : (M + 7) / 8 * 8;
+    Plan best{};
+    double least = 0.0;
+    const int shapes[3][3] = {{2, 256, 512}, {1, 128, 256}, {1, 64, 192}};
+    for (const auto &shape : shapes) {
+        const int cg = shape[0], bn = shape[1];
+        if (terms > 1 && cg == 2) continue;  // fp32: the output warps hold a tile's sums
+        const int64_t n = mode == kForward ? bn / 2 : bn, units = sms / cg;
+        const int64_t tiles = (M + 128 * cg - 1) / (128 * cg) * outs * ((N + n - 1) / n);
+        const double copies = static_cast<double>((a_rows + bn / cg) * 128) / 64.0;
+        const double stage = copies > shape[2] ? copies : shape[2], tile = static_cast<double>(stages) * stage;
+        const int64_t rounds = (tiles + units - 1) / units, rest = tiles % units;
+        const double whole = static_cast<double>(rounds) * (tile + 4000.0);
+        double cut = static_cast<double>(tiles) / static_cast<double>(units) * tile + static_cast<double>(rounds) * 4000.0 + 20000.0;
+        // every share has some stages, and is shorter than a tile
+        const bool can = mode != kForward && rest > 0 && rest * stages >= 8 * units;
+        if (!can) cut = whole;
+        const double cost = cut < whole ? cut : whole;
+        if (best.cg == 0 || cost < least) {
+            least = cost;
+            best = Plan{cg, bn, cut < whole, 0};
+            if (best.cut) best.part_bytes = static_cast<size_t>(units) * 2 * cg * 128 * bn * sizeof(float);
+        }
+    }
+    return best;
+}
+
 template <int MODE, int CG, int BN, bool SPLIT>
-cudaError_t launch_tiled(const Job &j, cudaStream_t stream)
+cudaError_t launch_tiled(const Job &j, bool cut, cudaStream_t stream)
 {
     using C = Cfg<CG, BN>;
     constexpr int kNOut = MODE == kForward ? BN / 2 : BN;
@@ -666,6 +823,8 @@ cudaError_t launch_tiled(const Job &j, cudaStream_t stream)
     p.m_tiles = static_cast<int>(mt);
     p.n_tiles = static_cast<int>(nt);
     p.tiles = static_cast<int>(mt * two_out * nt);
+    const int units = ws::sm_count() / CG;
+    p.whole = cut ? p.tiles - p.tiles % units : p.tiles;
     for (int i = 0; i < two_a; ++i)
         if (!operand_map(&maps.a[i], j.a[i], MODE == kDw ? 64 : p.a_rows)) return cudaErrorInvalidValue;
     for (int i = 0; i < two_b; ++i)
@@ -677,11 +836,12 @@ cudaError_t launch_tiled(const Job &j, cudaStream_t stream)
     if (p.save)
         for (int i = 0; i < 2; ++i)
             if (!output_map(&maps.save[i], j.save[i], true, j.M, j.N, 32)) return cudaErrorInvalidValue;
+    if (cut && !output_map(&maps.save[0], j.parts, true, static_cast<int64_t>(units) * 2 * CG * 128, BN, 32))
+        return cudaErrorInvalidValue;
     static SmemAttrCache attr_cache;
     const cudaError_t attr = smem_attr_once(product_kernel<MODE, CG, BN, SPLIT>, static_cast<int>(C::kSmem), attr_cache);
     if (attr != cudaSuccess) return attr;
-    const int64_t slots = ws::sm_count() / CG;
-    const unsigned blocks = static_cast<unsigned>((p.tiles < slots ? p.tiles : slots) * CG);
+    const unsigned blocks = static_cast<unsigned>((cut || p.tiles > units ? units : p.tiles) * CG);
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(blocks);
     cfg.blockDim = dim3(C::kThreads);
@@ -694,30 +854,35 @@ cudaError_t launch_tiled(const Job &j, cudaStream_t stream)
     la[0].val.clusterDim.z = 1;
     cfg.attrs = la;
     cfg.numAttrs = CG == 2 ? 1 : 0;
-    const cudaError_t e = cudaLaunchKernelEx(&cfg, product_kernel<MODE, CG, BN, SPLIT>, p, maps);
-    return e != cudaSuccess ? e : cudaGetLastError();
+    cudaError_t e = cudaLaunchKernelEx(&cfg, product_kernel<MODE, CG, BN, SPLIT>, p, maps);
+    if (e == cudaSuccess) e = cudaGetLastError();
+    if constexpr (MODE != kForward) {
+        if (e != cudaSuccess || !cut) return e;
+        cudaLaunchConfig_t jc = {};
+        jc.gridDim = dim3(static_cast<unsigned>((p.tiles - p.whole) * (CG * 128 / 8)));
+        jc.blockDim = dim3(BN);
+        jc.stream = stream;
+        la[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        la[0].val.programmaticStreamSerializationAllowed = 1;
+        jc.attrs = la;
+        jc.numAttrs = 1;
+        e = cudaLaunchKernelEx(&jc, join_kernel<MODE, CG, BN>, p, const_cast<const float *>(j.parts), j.out[0],
+                               j.out[MODE == kDw ? 1 : 0], units);
+        if (e == cudaSuccess) e = cudaGetLastError();
+    }
+    return e;
 }
 
-// the tile whose rounds over the SMs take the fewest tensor-core cycles: a 64-deep stage takes 512 cycles in a
-// 256 x 256 pair tile, 256 in a 128 x 128 one and 192 in a 128 x 64 one, plus about 4000 a round for the
-// first copies and the last output
 template <int MODE>
 cudaError_t launch(const Job &j, cudaStream_t stream)
 {
-    const int64_t sms = ws::sm_count(), outs = MODE == kDw ? 2 : 1;
-    const int64_t stages = (j.K + 63) / 64 * j.terms * (MODE == kDx ? 2 : 1);
-    auto cycles = [&](int64_t rows, int64_t cols, int64_t slots, int64_t stage) {
-        const int64_t n = MODE == kForward ? cols / 2 : cols;
-        const int64_t tiles = (j.M + rows - 1) / rows * outs * ((j.N + n - 1) / n);
-        return (tiles + slots - 1) / slots * (stages * stage + 4000);
-    };
-    const int64_t pair = cycles(256, 256, sms / 2, 512), wide = cycles(128, 128, sms, 256),
-                  narrow = cycles(128, 64, sms, 192);
-    if (j.terms > 1)  // fp32: the output warps hold a tile's sums
-        return wide <= narrow ? launch_tiled<MODE, 1, 128, true>(j, stream) : launch_tiled<MODE, 1, 64, true>(j, stream);
-    if (pair <= wide && pair <= narrow) return launch_tiled<MODE, 2, 256, false>(j, stream);
-    if (wide <= narrow) return launch_tiled<MODE, 1, 128, false>(j, stream);
-    return launch_tiled<MODE, 1, 64, false>(j, stream);
+    const Plan pl = plan(static_cast<Mode>(MODE), j.M, j.N, j.K, j.terms);
+    if (j.terms > 1)
+        return pl.bn == 128 ? launch_tiled<MODE, 1, 128, true>(j, pl.cut, stream)
+                            : launch_tiled<MODE, 1, 64, true>(j, pl.cut, stream);
+    if (pl.cg == 2) return launch_tiled<MODE, 2, 256, false>(j, pl.cut, stream);
+    return pl.bn == 128 ? launch_tiled<MODE, 1, 128, false>(j, pl.cut, stream)
+                        : launch_tiled<MODE, 1, 64, false>(j, pl.cut, stream);
 }
 
 // few tokens (cci_gated_few.cu): few_tokens, dense weights [F][D] of dtype; few_packed, also the packed ones (wg

@@ -61,7 +61,8 @@ __device__ __forceinline__ void finish(const Args &p, const float *red, int stri
         p.g[o] = g;
         p.u[o] = u;
     }
-    const float h = act_of(g, p.act) * u;
+    float h = 0.f;
+    with_act(p.act, [&](auto act) { h = act_of<decltype(act)::value>(g) * u; });
     if (f32)
         static_cast<float *>(p.H)[o] = h;
     else
