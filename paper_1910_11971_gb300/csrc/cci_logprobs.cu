@@ -454,8 +454,9 @@ __global__ void __launch_bounds__(kThreads, kThreads == 32 ? 28 : 1024 / kThread
             }
             top = fmaxf(top, m);
             if constexpr (TOP && RUN != 512) {
-                uint32_t q = 0u;
-                if (in && (m > neg_inf() || has_number<T, kV>(raw[u]))) q = order_of(fmaxf(m, neg_inf()));
+                uint32_t q = in ? order_of(fmaxf(m, neg_inf())) : 0u;
+                // a vote, so that the rare look at a load without a larger number is a branch
+                if (__any_sync(0xffffffffu, in && !(m > neg_inf()))) q = in && has_number<T, kV>(raw[u]) ? q : 0u;
 #pragma unroll
                 for (int s = kGroup / 2; s > 0; s >>= 1) q = max(q, __shfl_xor_sync(0xffffffffu, q, s));
                 if (lane % kGroup == 0) own[((w - ws) + u * 32 + lane) / kRunWords] = q;
@@ -463,7 +464,8 @@ __global__ void __launch_bounds__(kThreads, kThreads == 32 ? 28 : 1024 / kThread
         }
         if constexpr (TOP && RUN == 512) {
             uint32_t q = order_of(top);
-            if (top == neg_inf()) {
+            // a vote, so that the rare look at loads without a larger number is a branch
+            if (__any_sync(0xffffffffu, !(top > neg_inf()))) {
                 bool any = false;
 #pragma unroll
                 for (int u = 0; u < kU; ++u) any |= (FULL || w + u * 32 + lane < we) && has_number<T, kV>(raw[u]);
@@ -788,7 +790,7 @@ cudaError_t launch_rows(const T *x, int64_t ldx, int64_t N, int64_t V, const Row
 {
     // runs of a warp: its share of the words in whole iterations
     constexpr int64_t kV = 16 / sizeof(T), kIter = 512 / kV, kWarps = kThreads / 32;
-    const int64_t words = V / kV / parts + 1, per_warp = ((words + kWarps - 1) / kWarps + kIter - 1) / kIter * kIter;
+    const int64_t words = (V / kV + parts - 1) / parts, per_warp = ((words + kWarps - 1) / kWarps + kIter - 1) / kIter * kIter;
     const int slots = static_cast<int>((per_warp / (RUN / kV) + 3) / 4 * 4);  // read four at a time
     const size_t bytes = TOP ? static_cast<size_t>(kWarps) * slots * sizeof(uint32_t) : 0;
     if (bytes > 32 * 1024) {
@@ -835,11 +837,19 @@ cudaError_t launch(const T *x, int64_t ldx, int64_t N, int64_t V, const Row &o, 
         return launch_middle<T, 128>(x, ldx, N, V, o, stream);
     }
     // parts of a row where the rows alone leave SMs idle (each holds four blocks).  A part keeps 16384 logits
-    // (32 runs).  More parts than that to fill the last round of blocks cost more than they save: the
-    // alternatives' work at a row's end is per part (1024 x 131072 bf16, 5 alternatives: 145 us in four parts
-    // against 89 in one)
+    // (32 runs).  More parts than that, to fill the last round of blocks, cost more than they save: the
+    // alternatives' work at a row's end is per part (1024 x 131072 bf16, 5 alternatives: 145 us in four parts and
+    // 101 in one, with the kernel of that time)
     int parts = 1;
     while (parts < 8 && N * parts * 2 <= 4 * row::sm_count() && V >= 2 * parts * 16384) parts *= 2;
+    // where the rows fill the SMs: blocks of four warps, eight of an SM, which share the rows out more evenly
+    // (1024 x 131072 bf16: 55 us in blocks of eight warps, 52 so, without alternatives).  Past 131072 logits
+    // their warps' runs would not fit two a lane
+    if (N >= 4 * row::sm_count() && V <= 131072) {
+        if (!o.k) return launch_rows<T, 128, 512, false>(x, ldx, N, V, o, 1, stream);
+        return V <= 16384 ? launch_rows<T, 128, 128, true>(x, ldx, N, V, o, 1, stream)
+                          : launch_rows<T, 128, 512, true>(x, ldx, N, V, o, 1, stream);
+    }
     if (!o.k) return launch_rows<T, 256, 512, false>(x, ldx, N, V, o, parts, stream);
     return V <= 16384 ? launch_rows<T, 256, 128, true>(x, ldx, N, V, o, parts, stream)
                       : launch_rows<T, 256, 512, true>(x, ldx, N, V, o, parts, stream);
