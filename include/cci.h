@@ -539,7 +539,9 @@ cci_status cci_token_logprobs_backward(const void *logits, cci_dtype dtype, int6
  * with fp32 accumulators and one rounding, to the type of H.  bf16: products of the exact
  * values on the tensor cores.  fp32: every operand as three bf16 planes, the six products
  * of planes down to 2^-18 of the whole (what is left out is below 2^-25 |x||w| a term; an
- * infinite input gives NaN where its products of planes do).
+ * infinite input gives NaN where its products of planes do).  Up to 16 tokens: the weights
+ * streamed as they are (fp32: fused multiply-adds), the sums in another order, so a token's last
+ * bits may differ from those it has in a call of more tokens.
  *
  *   X          device [N][D] of dtype
  *   Wg, Wu     device [F][D] of dtype (pruned weights: their dense form, as cci_td_mask
@@ -547,7 +549,7 @@ cci_status cci_token_logprobs_backward(const void *logits, cci_dtype dtype, int6
  *   H          device [N][F] of dtype (written)
  *   g, u       device fp32 [N][F] (written, for cci_gated_linear_backward), or both NULL
  *   workspace  device, 16-byte aligned, cci_gated_workspace_size(CCI_GATED_FORWARD, ...)
- *              bytes (0 for bf16, which needs none); overwritten
+ *              bytes (0 for bf16 and for up to 16 tokens, which need none); overwritten
  *   dev_status device uint32 or NULL (CCI_ERR_TIMEOUT)
  * D and F are multiples of 8; every matrix is 16-byte aligned.  N = 0 is valid and enqueues
  * nothing.
@@ -579,9 +581,11 @@ cci_status cci_gated_linear(const void *X, cci_dtype dtype, int64_t N, int64_t D
 
 /*
  * cci_gated_linear_packed -- cci_gated_linear with both weight matrices in the packed format
- * of cci_pack (Cout = F, R = D, the same G and K): any G and K of that format.  The weights
- * are expanded into the workspace (CCI_GATED_PACKED) and multiplied there, so pruned
- * positions take part as zeros (an infinite x gives NaN).  An index set that is not strictly
+ * of cci_pack (Cout = F, R = D, the same G and K): any G and K of that format, with the bits
+ * of the dense form.  The weights are expanded into the workspace (CCI_GATED_PACKED) and
+ * multiplied there; up to 16 tokens of bf16 read them packed where G is 4 to 32, K a power of two
+ * up to G / 2 and 8, and D * K a multiple of 16.  Pruned positions take part as zeros either way
+ * (an infinite x gives NaN).  An index set that is not strictly
  * increasing or has an index >= G sets CCI_ERR_INDEX in dev_status.
  * Errors: as cci_gated_linear; CCI_ERR_GROUP.
  */

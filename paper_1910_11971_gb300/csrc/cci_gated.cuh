@@ -91,11 +91,28 @@ static_assert(sizeof(Smem) <= 1024, "barriers");
 // 1999 tokens, 4096 -> 8192: 268, 164 and 143 us on the device)
 __device__ __forceinline__ float sigmoid(float g) { return __fdividef(1.f, 1.f + __expf(-g)); }
 
+// the normal distribution's Phi(g) by Abramowitz and Stegun 7.1.26, erf within 1.5e-7 (Phi 3e-7 with roundings), and e^(-g^2 / 2), which it takes
+// on the way.  No branch, half the time of erfcf (a 256 x 256 tile's epilogue 7.3 us with that, 4.9 so)
+__device__ __forceinline__ float normal_cdf(float g, float &e)
+{
+    const float t = __fdividef(1.f, fmaf(fabsf(g), 0.3275911f * 0.70710678f, 1.f));
+    e = __expf(-0.5f * g * g);
+    float q = fmaf(t, 1.061405429f, -1.453152027f);
+    q = fmaf(t, q, 1.421413741f);
+    q = fmaf(t, q, -0.284496736f);
+    q = fmaf(t, q, 0.254829592f);
+    q *= 0.5f * t * e;  // Phi(-|g|)
+    return g > 0.f ? 1.f - q : q;
+}
+
 template <int ACT>
 __device__ __forceinline__ float act_of(float g)
 {
     if constexpr (ACT == CCI_ACT_SILU) return g * sigmoid(g);
-    if constexpr (ACT == CCI_ACT_GELU) return 0.5f * g * erfcf(g * -0.70710678f);
+    if constexpr (ACT == CCI_ACT_GELU) {
+        float e;
+        return g * normal_cdf(g, e);
+    }
     if constexpr (ACT == CCI_ACT_GELU_TANH) return g * sigmoid(1.5957691f * (g + 0.044715f * g * g * g));
     if constexpr (ACT == CCI_ACT_RELU) return g > 0.f ? g : (g != g ? g : 0.f);
     return sigmoid(g);
@@ -106,9 +123,10 @@ template <int ACT>
 __device__ __forceinline__ float slope_of(float g, float &a)
 {
     if constexpr (ACT == CCI_ACT_GELU) {
-        const float c = 0.5f * erfcf(g * -0.70710678f);
+        float e;
+        const float c = normal_cdf(g, e);
         a = g * c;
-        return c + g * 0.39894228f * __expf(-0.5f * g * g);
+        return fmaf(g * 0.39894228f, e, c);
     }
     if constexpr (ACT == CCI_ACT_RELU) {
         a = act_of<ACT>(g);
