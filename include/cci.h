@@ -549,7 +549,7 @@ cci_status cci_token_logprobs_backward(const void *logits, cci_dtype dtype, int6
  *   H          device [N][F] of dtype (written)
  *   g, u       device fp32 [N][F] (written, for cci_gated_linear_backward), or both NULL
  *   workspace  device, 16-byte aligned, cci_gated_workspace_size(CCI_GATED_FORWARD, ...)
- *              bytes (0 for bf16 and for up to 16 tokens, which need none); overwritten
+ *              bytes (0 for bf16, which needs none); overwritten
  *   dev_status device uint32 or NULL (CCI_ERR_TIMEOUT)
  * D and F are multiples of 8; every matrix is 16-byte aligned.  N = 0 is valid and enqueues
  * nothing.

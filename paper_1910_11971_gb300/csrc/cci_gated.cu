@@ -231,7 +231,6 @@ Layout layout(int dtype, int64_t N, int64_t D, int64_t F, int call)
     const size_t planes = f32 ? 3 : 1;
     const bool dense = f32 || call == CCI_GATED_PACKED;  // weights laid out here
     Layout l{};
-    if (call == CCI_GATED_FORWARD && few_tokens(dtype, N)) return l;
     size_t at = 0;
     auto take = [&](bool need, int64_t n) {
         const size_t here = at;

@@ -318,7 +318,7 @@ def test_refusals():
     assert fwd(act=5) == VALUE and fwd(act=-1) == VALUE
     assert fwd(D=12) == UNSUP and fwd(F=20) == UNSUP
     assert fwd(X=FAKE + 8) == ALIGN and fwd(Wu=FAKE + 8) == ALIGN and fwd(H=FAKE + 8) == ALIGN and fwd(g=FAKE + 4, u=FAKE) == ALIGN
-    assert fwd(dt=0, N=40) == WORKSPACE and fwd(dt=0, N=40, ws=FAKE + 8, n=1 << 20) == WORKSPACE
+    assert fwd(dt=0) == WORKSPACE and fwd(dt=0, ws=FAKE + 8, n=1 << 20) == WORKSPACE
     assert fwd(N=0, X=None, H=None) == OK and fwd(N=0, dt=0, X=None, H=None) == OK
 
     def packed(X=FAKE, dt=1, N=4, D=16, gv=FAKE, gi=FAKE, uv=FAKE, ui=FAKE, F=16, G=8, K=2, act=0, H=FAKE, ws=FAKE, n=1 << 20):
@@ -334,7 +334,7 @@ def test_refusals():
     assert bwd(dH=None) == NULL and bwd(g=None) == NULL and bwd(dWg=None) == NULL and bwd(dWu=None) == NULL
     assert bwd(dX=FAKE + 8) == ALIGN and bwd(dH=FAKE + 8) == ALIGN and bwd(n=0) == WORKSPACE and bwd(act=7) == VALUE
     size = cci.lib().cci_gated_workspace_size
-    assert size(0, 1, 4, 16, 16) == 0 and size(0, 0, 4, 16, 16) == 0 and size(0, 0, 40, 16, 16) > 0 and size(2, 1, 4, 16, 16) > 0 and size(3, 1, 4, 16, 16) == 0
+    assert size(0, 1, 4, 16, 16) == 0 and size(0, 0, 4, 16, 16) > 0 and size(2, 1, 4, 16, 16) > 0 and size(3, 1, 4, 16, 16) == 0
     host = torch.zeros((4, 16))
     with pytest.raises(ValueError):
         cci.gated_linear(host, host, host)
