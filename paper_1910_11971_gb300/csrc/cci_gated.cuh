@@ -798,6 +798,7 @@ inline Plan plan(Mode mode, int64_t M, int64_t N, int64_t K, int terms)
     for (const auto &shape : shapes) {
         const int cg = shape[0], bn = shape[1];
         if (terms > 1 && cg == 2) continue;  // fp32: the output warps hold a tile's sums
+        if (cg > sms) continue;              // no device: sizes and refusals are still answered
         const int64_t n = mode == kForward ? bn / 2 : bn, units = sms / cg;
         const int64_t tiles = (M + 128 * cg - 1) / (128 * cg) * outs * ((N + n - 1) / n);
         const double copies = static_cast<double>((a_rows + bn / cg) * 128) / 64.0;
