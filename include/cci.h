@@ -474,8 +474,7 @@ cci_status cci_layer_norm(const void *x, cci_dtype dtype, int64_t N, int64_t D, 
  *   dx         device [N][D] of dtype (written)
  *   dweight, dbias device fp32 [D] (written; zeros for N = 0), each may be NULL
  *   workspace  device, 16-byte aligned, cci_layer_norm_workspace_size(N, D) bytes (which
- *              depends on the current device's number of SMs; 0 for a few rows);
- *              overwritten
+ *              depends on the current device's number of SMs); overwritten
  * Errors: as cci_layer_norm; CCI_ERR_WORKSPACE.
  */
 size_t cci_layer_norm_workspace_size(int64_t N, int64_t D);

@@ -821,8 +821,7 @@ cudaError_t backward(const Args &a)
 
 size_t layer_norm_workspace(int64_t N, int64_t D)
 {
-    const int64_t parts = norm::most_parts(N, D);
-    return parts > 1 ? static_cast<size_t>(parts) * 2 * static_cast<size_t>(D) * sizeof(float) : 0;
+    return static_cast<size_t>(norm::most_parts(N, D)) * 2 * static_cast<size_t>(D) * sizeof(float);
 }
 
 cudaError_t launch_layer_norm(const void *x, int dtype, int64_t N, int64_t D, int64_t ldx, const float *w,
