@@ -28,7 +28,7 @@
  * are DEVICE pointers (except the X_host / Y_host of cci_linear_host); the
  * library allocates nothing.  It keeps no state between calls except three
  * per-device caches, filled on a device's first use: the dynamic shared-memory
- * limit set on each tensor-core kernel, the device's number of SMs, and the device
+ * limit set on each kernel that asks for more than the default, the device's number of SMs, and the device
  * address of the static scratch array of cci_linear_dense_tc_static (see there).  Every
  * call is asynchronous on `stream` (NULL = the legacy default stream) and
  * returns once its kernels are enqueued.  Calls on different streams may run
@@ -538,9 +538,9 @@ cci_status cci_token_logprobs_backward(const void *logits, cci_dtype dtype, int6
  * with fp32 accumulators and one rounding, to the type of H.  bf16: products of the exact
  * values on the tensor cores.  fp32: every operand as three bf16 planes, the six products
  * of planes down to 2^-18 of the whole (what is left out is below 2^-25 |x||w| a term; an
- * infinite input gives NaN where its products of planes do).  Up to 16 tokens: the weights
- * streamed as they are (fp32: fused multiply-adds), the sums in another order, so a token's last
- * bits may differ from those it has in a call of more tokens.
+ * infinite input gives NaN where its products of planes do).  Calls of up to 16 tokens may
+ * stream the weights as they are (fp32: fused multiply-adds), with the sums in another order, so
+ * a token's last bits may differ from those it has in a call of more tokens.
  *
  *   X          device [N][D] of dtype
  *   Wg, Wu     device [F][D] of dtype (pruned weights: their dense form, as cci_td_mask
@@ -580,10 +580,10 @@ cci_status cci_gated_linear(const void *X, cci_dtype dtype, int64_t N, int64_t D
 
 /*
  * cci_gated_linear_packed -- cci_gated_linear with both weight matrices in the packed format
- * of cci_pack (Cout = F, R = D, the same G and K): any G and K of that format, with the bits
- * of the dense form.  The weights are expanded into the workspace (CCI_GATED_PACKED) and
- * multiplied there; up to 16 tokens of bf16 read them packed where G is 4 to 32, K a power of two
- * up to G / 2 and 8, and D * K a multiple of 16.  Pruned positions take part as zeros either way
+ * of cci_pack (Cout = F, R = D, the same G and K): any G and K of that format.  The
+ * weights are expanded into the workspace (CCI_GATED_PACKED) and multiplied there; up to 16
+ * tokens of bf16 read them packed where G is 4, 8, 16 or 32, K a power of two up to G / 2 and 8,
+ * D * K a multiple of 16 and the indices are on 16 bytes.  Pruned positions take part as zeros either way
  * (an infinite x gives NaN).  An index set that is not strictly
  * increasing or has an index >= G sets CCI_ERR_INDEX in dev_status.
  * Errors: as cci_gated_linear; CCI_ERR_GROUP.

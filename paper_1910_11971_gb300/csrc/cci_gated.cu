@@ -315,7 +315,7 @@ size_t gated_workspace(int dtype, int64_t N, int64_t D, int64_t F, int call)
 cudaError_t launch_gated(const GatedArgs &a, cudaStream_t stream)
 {
     using namespace gated;
-    const bool f32 = a.dtype == CCI_F32, packed = a.gate_idx != nullptr, few = few_tokens(a.dtype, a.N);
+    const bool f32 = a.dtype == CCI_F32, packed = a.gate_idx != nullptr, few = few_tokens(a.dtype, a.N, a.F);
     if (packed ? few_packed(a) : few) return launch_few(a, a.Wg, a.Wu, packed, stream);
     const Layout l = layout(a.dtype, a.N, a.D, a.F, packed ? CCI_GATED_PACKED : CCI_GATED_FORWARD);
     char *base = static_cast<char *>(a.workspace);

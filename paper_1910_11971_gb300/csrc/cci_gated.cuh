@@ -906,7 +906,7 @@ cudaError_t launch(const Job &j, cudaStream_t stream)
 
 // few tokens (cci_gated_few.cu): few_tokens, dense weights [F][D] of dtype; few_packed, also the packed ones (wg
 // and wu: the values) as they are
-bool few_tokens(int dtype, int64_t N);
+bool few_tokens(int dtype, int64_t N, int64_t F);
 bool few_packed(const GatedArgs &a);
 cudaError_t launch_few(const GatedArgs &a, const void *wg, const void *wu, bool packed, cudaStream_t stream);
 

@@ -1,10 +1,11 @@
 // cci_gated_few.cu -- the gated block for few tokens (decoding): h = act(X Wg^T) * (X Wu^T).
 //
 // What bounds it: every weight is read once and multiplied with a handful of tokens, so the time is
-// that of the weights' bytes.  The tile kernel (cci_gated.cuh) reaches 0.6 of the memory rate there: it reads a
-// row in 128-byte pieces, one per stage, with as many tiles as SMs at best.  Here a block of eight warps
-// takes eight hidden channels, and its warps read neighbouring 64-byte pieces of the same sixteen
-// rows (gate and up), 512 bytes of a row at a time, straight into registers.
+// that of the weights' bytes.  The tile kernel (cci_gated.cuh) reads a row in 128-byte pieces, one per
+// stage, with as many tiles as SMs at best (4096 -> 8192 bf16, one token: 25.3 us, here 22.0, the
+// bytes' time 19.7).  Here a block of eight warps takes eight hidden channels, and its warps read
+// neighbouring 64-byte pieces of the same sixteen rows (gate and up), 512 bytes of a row at a time,
+// straight into registers.
 //
 // bf16: mma.sync m16n8k16.  The tensor core's rate does not matter here, but its fragment layout does: a
 // lane's 16 bytes of a row are eight consecutive indices, and as the tokens' fragment is read the
@@ -13,8 +14,9 @@
 // Packed weights (values, idx) become fragments in registers: the lanes of a group's rows read the
 // same run, copied to shared memory in bulk, and each keeps the values whose index is its row.
 //
-// fp32: fused multiply-adds, 16 rows by up to eight tokens a warp.  Twice the bytes and no products of planes:
-// up to 16 tokens stay below the memory's time (8 tokens, 4096 -> 8192: 14 us of 39).
+// fp32: fused multiply-adds, 16 rows by up to eight tokens a warp.  Twice the bytes and no products of planes.
+// A token stays at the memory's time, more are bound by the multiply-adds (4096 -> 8192: 1 token 39.5 us of
+// 39.5, 4 51, 8 73, 16 142).
 //
 // The warps' sums are joined in shared memory in warp order: the same bits at every call.
 #include "cci_gated.cuh"
@@ -425,16 +427,25 @@ cudaError_t launch_f32(const Args &p, cudaStream_t stream)
 
 }  // namespace few
 
-bool few_tokens(int dtype, int64_t N)
+// Up to 16 tokens, but for 9 to 16 of bf16 only where the tile kernel has no tile (32 channels) for each SM: past 8
+// tokens the tokens' own reads, which every block makes, weigh as much as the weights.
+//   bf16, here against tiles:  4096 -> 8192: 1 token 22.0 us and 25.3, 8 22.7 and 25.3, 16 32.1 and 25.5;
+//                              1024 -> 8192: 16 tokens 11.3 and 9.3;  4096 -> 4096: 16 tokens 15.8 and 16.6;
+//                              1024 -> 2048: 1 token 3.2 and 6.5, 16 4.2 and 6.5
+//   fp32 (tiles work on planes made in a launch of their own):
+//                              4096 -> 8192: 1 token 39.5 us and 246, 8 73 and 246, 16 142 and 246;
+//                              1024 -> 2048: 1 token 3.8 and 30, 16 18 and 30
+bool few_tokens(int dtype, int64_t N, int64_t F)
 {
-    (void)dtype;
-    return N <= 16;
+    return N <= 8 || (N <= 16 && (dtype == CCI_F32 || F < 32 * static_cast<int64_t>(row::sm_count())));
 }
 
+// Packed weights read as they are, against expanded and multiplied by tiles (4096 -> 8192): G = 8, K = 2 1 token
+// 33.5 us and 62.7, 16 37.9 and 62.7; G = 32, K = 8 1 token 73 and 89, 16 79 and 89
 bool few_packed(const GatedArgs &a)
 {
     auto at16 = [](const void *q) { return reinterpret_cast<uintptr_t>(q) % 16 == 0; };
-    return a.dtype == CCI_BF16 && few_tokens(a.dtype, a.N) && (a.G == 4 || a.G == 8 || a.G == 16 || a.G == 32) &&
+    return a.dtype == CCI_BF16 && a.N <= 16 && (a.G == 4 || a.G == 8 || a.G == 16 || a.G == 32) &&
            (a.K == 1 || a.K == 2 || a.K == 4 || a.K == 8) && 2 * a.K <= a.G && a.D * a.K % 16 == 0 && a.F % 8 == 0 &&
            at16(a.gate_idx) && at16(a.up_idx);
 }

@@ -5,11 +5,13 @@
 //   dw[c]    = sum over n of dy * xh,  db[c] = sum over n of dy
 //
 // Memory bound in both directions (two or three row reads and writes, a dozen operations an
-// element).  A row belongs to a group of 32 to 1024 threads that holds it in registers: the
-// variance is the mean square of the differences from the mean, not a difference of sums, and
-// nothing is read twice.  The backward pass keeps each thread's columns of dw and db in
-// registers over all rows of its block; the blocks' sums go to the workspace and a second
-// launch adds them in block order, so the result does not depend on what finishes first.
+// element).  A row of up to 16384 columns belongs to a group of 32 to 1024 threads and is read
+// from memory once: by bulk copies into shared memory where it lies on whole 16-byte words, else into
+// registers.  The variance is the mean square of the differences from the mean, not a difference
+// of sums.  The backward pass takes its sums and then dx from shared memory, and keeps each
+// thread's columns of dw and db in registers over all rows of its block; the blocks' sums go to the
+// workspace and a second launch adds them in block order (a single block's go straight to dw and
+// db), so the result does not depend on what finishes first.  Longer rows are read again for each pass.
 // All sums are fp32.
 #include "cci_rowops.cuh"
 #include "cci_tc_common.cuh"
