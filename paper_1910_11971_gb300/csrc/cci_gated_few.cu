@@ -107,7 +107,7 @@ __device__ __forceinline__ bool bad_set(const unsigned char *idx, int G)
 }
 
 // A warp's share of a row: 128 indices (four 32-index steps, 256 bytes of a dense row) in turn with the other
-// warps', whatever the weights' form, so that packed weights give the bits of their dense form
+// warps', whatever the weights' form: packed weights give the bits that their dense form gives here
 constexpr int kSteps = 4, kRound = kSteps * kWarps * 32;
 
 // this lane's sums c[m][i] of each set of eight channels and eight tokens, from every warp: channel g of the
@@ -198,7 +198,8 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 4 : 3) bf16_kernel(Args p)
 // ---- packed weights ----
 // A block takes a group (two of G = 4) of each projection: MT sets of eight channels.  Their runs of a round
 // of 1024 indices are contiguous, and bulk copies bring them to shared memory, as many rounds ahead as it
-// holds: registers hold no weights that are on their way.
+// holds: registers hold no weights that are on their way.  What bounds it is taking each row's weights out of the
+// runs, on the integer pipe (60 % of it; 16 tokens, 4096 -> 4096, G = 8, K = 2: 21.2 us of 3.7 for the bytes).
 constexpr int kMaxStages = 8;
 
 struct PackedSmem {
@@ -217,8 +218,13 @@ __device__ __forceinline__ void bulk_load(uint32_t dst, const void *src, uint32_
 // a stage: [gate, up][group][1024 K values, then 1024 K indices]
 constexpr int stage_bytes(int K, int groups) { return 2 * groups * kRound * K * 3; }
 
+// blocks of an SM that registers and shared memory are shared out to.  Sets of eight channels: four with K = 1
+// (G = 8, 4096 -> 4096, 16 tokens: 18.5 us with two, 14.8 so), three with K = 2 (4096 -> 8192, 16 tokens: 39.3 us with
+// two, 36.3 so, 38.6 with four)
+constexpr int packed_blocks(int K, int MT) { return K > 2 ? 1 : (MT > 1 ? 2 : (K == 1 ? 4 : 3)); }
+
 template <int K, int NT, int MT>
-__global__ void __launch_bounds__(kThreads, K <= 2 ? 2 : 1) packed_kernel(Args p, int stages)
+__global__ void __launch_bounds__(kThreads, packed_blocks(K, MT)) packed_kernel(Args p, int stages)
 {
     extern __shared__ __align__(128) unsigned char smem[];
     __shared__ PackedSmem S;
@@ -262,6 +268,9 @@ __global__ void __launch_bounds__(kThreads, K <= 2 ? 2 : 1) packed_kernel(Args p
     float c[MT][NT][4] = {};
     int s = 0;
     uint32_t ph = 0u;
+    // the tokens of a step are loaded a step ahead: their way from L2 is the length of one
+    uint4 x[NT];
+    load_tokens<NT>(x, p, g, warp * kSteps * 32 + t * 8);
     for (int r = 0; r < rounds; ++r) {
         ok = tc::mbar_wait(&S.full[s], ph, abort, p.status);
         ok = __all_sync(0xffffffffu, ok);
@@ -270,8 +279,8 @@ __global__ void __launch_bounds__(kThreads, K <= 2 ? 2 : 1) packed_kernel(Args p
 #pragma unroll
         for (int q = 0; q < kSteps; ++q) {
             const int at = warp * kSteps * 32 + q * 32 + t * 8, k = r * kRound + at;
-            uint4 x[NT];
-            load_tokens<NT>(x, p, g, k);
+            uint4 next[NT];
+            load_tokens<NT>(next, p, g, k + (q < kSteps - 1 ? 32 : kRound - (kSteps - 1) * 32));
             uint4 a[MT], b[MT];
 #pragma unroll
             for (int m = 0; m < MT; ++m) a[m] = b[m] = make_uint4(0u, 0u, 0u, 0u);
@@ -293,6 +302,8 @@ __global__ void __launch_bounds__(kThreads, K <= 2 ? 2 : 1) packed_kernel(Args p
                     mma_bf16(c[m][i], a[m].x, b[m].x, a[m].y, b[m].y, x[i].x, x[i].y);
                     mma_bf16(c[m][i], a[m].z, b[m].z, a[m].w, b[m].w, x[i].z, x[i].w);
                 }
+#pragma unroll
+            for (int i = 0; i < NT; ++i) x[i] = next[i];
         }
         __syncwarp();
         if (lane == 0) tc::mbar_arrive(&S.empty[s]);
@@ -383,8 +394,7 @@ cudaError_t launch_packed(const Args &p, cudaStream_t stream)
 {
     const int groups = (1 << p.log_g) < kF ? kF >> p.log_g : 1, stage = stage_bytes(K, groups);
     constexpr int sums = kWarps * MT * NT * 128 * static_cast<int>(sizeof(float));
-    // K <= 2: stages of up to 72 KB, two blocks of an SM; more: one block with up to 192 KB
-    const int budget = K <= 2 ? 72 * 1024 : 192 * 1024;
+    constexpr int blocks = packed_blocks(K, MT), budget = (blocks == 4 ? 54 : (blocks > 1 ? 72 : 192)) * 1024;
     const int rounds = (p.D + kRound - 1) / kRound;
     int stages = budget / stage < kMaxStages ? budget / stage : kMaxStages;
     if (stages > rounds) stages = rounds;
@@ -441,7 +451,7 @@ bool few_tokens(int dtype, int64_t N, int64_t F)
 }
 
 // Packed weights read as they are, against expanded and multiplied by tiles (4096 -> 8192): G = 8, K = 2 1 token
-// 33.5 us and 62.7, 16 37.9 and 62.7; G = 32, K = 8 1 token 73 and 89, 16 79 and 89
+// 32.8 us and 62.7, 16 36.3 and 62.7; G = 32, K = 8 1 token 72 and 89, 16 79 and 89
 bool few_packed(const GatedArgs &a)
 {
     auto at16 = [](const void *q) { return reinterpret_cast<uintptr_t>(q) % 16 == 0; };
