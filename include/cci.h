@@ -1,6 +1,7 @@
 /*
  * cci.h -- C ABI of libcci.so: forward products of layers with cross-channel
- * intragroup (CCI) sparsity on NVIDIA GB300 (sm_103a).
+ * intragroup (CCI) sparsity on NVIDIA GB300 (sm_103a), and the layers of a language model
+ * around them (layer norm, gated feed-forward block, token log probabilities) in both directions.
  *
  * Method: Yu et al., "Cross-Channel Intragroup Sparsity Neural Network"
  * (arXiv 1910.11971).  For every input feature r of a layer (for a convolution,
@@ -39,7 +40,7 @@
  *     returned directly (nothing is written).
  *   - A failed launch returns CCI_ERR_CUDA.
  *   - Errors found by the kernels while they run (NaN in a pack input, a packed
- *     index >= G, an expired bounded wait) are OR-ed as bits (1u << code) into
+ *     index >= G, a token outside its vocabulary, an expired bounded wait) are OR-ed as bits (1u << code) into
  *     the caller's device word `*dev_status`, if it is not NULL; read it after
  *     synchronising the stream and decode it with cci_decode_device_status().
  *     The library never clears that word.  When a kernel reports an error its
