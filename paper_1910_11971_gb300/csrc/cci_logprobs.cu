@@ -342,7 +342,7 @@ struct Shared {
     alignas(16) uint64_t join[kWarps < 8 ? kMaxTop : 8 * kMaxTop];  // first block of a cluster: the parts' lists
     Sums part[8];                                   // and their sums
     Sums warp[kWarps];
-    int run[kMaxTop];  // the k first runs' slots, -1 past the last
+    int run[kMaxTop];  // the k first runs: warp << 16 | slot (of 4096 at most), -1 past the last
     uint32_t bar;      // order of the k-th run's maximum (0: fewer runs)
     int count;
     Result result;
@@ -529,11 +529,11 @@ __global__ void __launch_bounds__(kThreads, kThreads == 32 ? 28 : 1024 / kThread
             for (int i = 0; i < 2; ++i) {
                 const int at = lane + 32 * i;
                 const uint32_t m = at < run_slots ? own[at] : 0u;
-                mine[i] = m ? static_cast<uint64_t>(m) << 32 | static_cast<uint32_t>(~(warp * run_slots + at)) : 0ull;
+                mine[i] = m ? static_cast<uint64_t>(m) << 32 | static_cast<uint32_t>(~(warp << 16 | at)) : 0ull;
             }
             if (run_slots <= 32) {
-#pragma unroll 8
-                for (int j = 0; j < 32; ++j) above[0] += __shfl_sync(0xffffffffu, mine[0], j) > mine[0];
+#pragma unroll 4
+                for (int j = 0; j < run_slots; ++j) above[0] += __shfl_sync(0xffffffffu, mine[0], j) > mine[0];
             } else {
 #pragma unroll 4
                 for (int j = 0; j < 32; ++j) {
@@ -581,7 +581,7 @@ __global__ void __launch_bounds__(kThreads, kThreads == 32 ? 28 : 1024 / kThread
                     for (int e = 0; e < 4; ++e) above += q[e] >= mine + (j + e < i ? 0u : 1u);
                 }
                 if (above < o.k) {
-                    sh.run[above] = i;
+                    sh.run[above] = i / run_slots << 16 | i % run_slots;
                     if (above == o.k - 1) sh.bar = mine;
                 }
             }
@@ -590,7 +590,7 @@ __global__ void __launch_bounds__(kThreads, kThreads == 32 ? 28 : 1024 / kThread
         const uint32_t bar = sh.bar;
         // element e of a run, as a key (0: none, or no number)
         auto run_key = [&](int run, int e) -> uint64_t {
-            const int q = run / run_slots, word = first_word(q) + (run - q * run_slots) * kRunWords + e / kV;
+            const int q = run >> 16, word = first_word(q) + (run & 0xffff) * kRunWords + e / kV;
             if (word >= first_word(q + 1)) return 0ull;
             const int at = head + word * kV + e % kV;
             const float v = row::to_f32(xr[at]);
@@ -609,8 +609,8 @@ __global__ void __launch_bounds__(kThreads, kThreads == 32 ? 28 : 1024 / kThread
         for (int r0 = warp * kSide; r0 < o.k; r0 += kWarps * kSide) {
             const int r = r0 + (kSide > 1 ? lane / kLanes : 0);
             const int run = r < o.k ? sh.run[r] : -1;
-            const int q = run < 0 ? 0 : run / run_slots;
-            const int from = first_word(q) + (run - q * run_slots) * kRunWords, to = run < 0 ? from : first_word(q + 1);
+            const int q = run < 0 ? 0 : run >> 16;
+            const int from = first_word(q) + (run & 0xffff) * kRunWords, to = run < 0 ? from : first_word(q + 1);
             row::Raw<T, kV> word[kPer];
 #pragma unroll
             for (int u = 0; u < kPer; ++u) {
@@ -625,7 +625,13 @@ __global__ void __launch_bounds__(kThreads, kThreads == 32 ? 28 : 1024 / kThread
                 int ties = 0;
 #pragma unroll
                 for (int j = 0; j < kV; ++j) v[j] = __int_as_float(0x7fc00000);  // NaN is never listed
-                if (at < to) row::unpack<T, kV>(word[u], v);
+                float m = neg_inf();
+                if (at < to) {
+                    row::unpack<T, kV>(word[u], v);
+                    m = raw_max<T, kV>(word[u], v);
+                }
+                // most loads hold none (4096 x 20000 bf16, 20 alternatives: 93.3 us when every element is looked at, 89.8 so)
+                if (!__any_sync(0xffffffffu, at < to && m >= least)) continue;
 #pragma unroll
                 for (int j = 0; j < kV; ++j) {
                     ties += v[j] == least;
@@ -834,7 +840,7 @@ cudaError_t launch(const T *x, int64_t ldx, int64_t N, int64_t V, const Row &o, 
     if (V <= 1024) return launch_short<T, 32>(x, ldx, N, V, o, stream);
     if (V <= 8192) {
         // a warp a row where the rows fill the SMs, else four (bf16: 2432 x 4000 8.6 us and 11.7, 16384 x 8192 57 and
-        // 83; with 5 alternatives 15.0 and 21.2, 110 and 157)
+        // 83; with 5 alternatives 14.9 and 21.2, 108 and 157)
         if (N >= 16 * row::sm_count()) return launch_middle<T, 32>(x, ldx, N, V, o, stream);
         return launch_middle<T, 128>(x, ldx, N, V, o, stream);
     }
@@ -845,8 +851,8 @@ cudaError_t launch(const T *x, int64_t ldx, int64_t N, int64_t V, const Row &o, 
     int parts = 1;
     while (parts < 8 && N * parts * 2 <= 4 * row::sm_count() && V >= 2 * parts * 16384) parts *= 2;
     // where the rows fill the SMs: blocks of four warps, eight of an SM, which share the rows out more evenly
-    // (bf16: 1024 x 131072 55 us in blocks of eight warps, 51 so; 4096 x 20000 50 and 41; with 5 alternatives 71 and 66,
-    // 87 and 71).  Past 131072 logits
+    // (bf16: 1024 x 131072 55 us in blocks of eight warps, 51 so; 4096 x 20000 50 and 41; with 5 alternatives 71 and 64,
+    // 87 and 66).  Past 131072 logits
     // their warps' runs would not fit two a lane
     if (N >= 4 * row::sm_count() && V <= 131072) {
         if (!o.k) return launch_rows<T, 128, 512, false>(x, ldx, N, V, o, 1, stream);
