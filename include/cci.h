@@ -572,7 +572,8 @@ typedef enum cci_gated_call {
     CCI_GATED_BACKWARD = 2
 } cci_gated_call;
 
-/* bytes of workspace of a call (0: none needed, or invalid sizes) */
+/* bytes of workspace of a call (0: none needed, or invalid sizes); the backward pass' depend on the
+ * current device's number of SMs */
 size_t cci_gated_workspace_size(cci_gated_call call, cci_dtype dtype, int64_t N, int64_t D, int64_t F);
 
 cci_status cci_gated_linear(const void *X, cci_dtype dtype, int64_t N, int64_t D, const void *Wg, const void *Wu,

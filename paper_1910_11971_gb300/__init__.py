@@ -626,11 +626,12 @@ def _act_code(act: str) -> int:
 def gated_workspace(call: int, dtype: torch.dtype, N: int, D: int, F: int, device) -> Optional[torch.Tensor]:
     """The workspace of a gated block's call (``GATED_FORWARD``, ``GATED_PACKED`` or ``GATED_BACKWARD``), from
     PyTorch memory: None when it needs none."""
-    return _workspace(_gated_bytes(call, F32 if dtype == torch.float32 else BF16, N, D, F), device)
+    device = torch.device(device)
+    return _workspace(_gated_bytes(call, F32 if dtype == torch.float32 else BF16, N, D, F, device.index), device)
 
 
 @functools.lru_cache(maxsize=4096)
-def _gated_bytes(call: int, dtype: int, N: int, D: int, F: int) -> int:
+def _gated_bytes(call: int, dtype: int, N: int, D: int, F: int, device_index: Optional[int]) -> int:
     return int(lib().cci_gated_workspace_size(call, dtype, N, D, F))
 
 
@@ -653,7 +654,7 @@ def gated_linear(X: torch.Tensor, Wg: torch.Tensor, Wu: torch.Tensor, *, act: st
     g = torch.empty((N, F), dtype=torch.float32, device=X.device) if save else None
     u = torch.empty((N, F), dtype=torch.float32, device=X.device) if save else None
     if workspace is None:
-        workspace = _workspace(_gated_bytes(GATED_FORWARD, code, N, D, F), X.device)
+        workspace = _workspace(_gated_bytes(GATED_FORWARD, code, N, D, F, X.device.index), X.device)
     wp, wb = _ws(workspace)
     _check(lib().cci_gated_linear(X.data_ptr(), code, N, D, Wg.data_ptr(), Wu.data_ptr(), F, _act_code(act),
                                   H.data_ptr(), g.data_ptr() if save else None, u.data_ptr() if save else None,
@@ -680,7 +681,7 @@ def gated_linear_packed(X: torch.Tensor, gate: Tuple[torch.Tensor, torch.Tensor]
         _like(out, (N, F), X.dtype, "out")
     H = out if out is not None else torch.empty((N, F), dtype=X.dtype, device=X.device)
     if workspace is None:
-        workspace = _workspace(_gated_bytes(GATED_PACKED, code, N, D, F), X.device)
+        workspace = _workspace(_gated_bytes(GATED_PACKED, code, N, D, F, X.device.index), X.device)
     wp, wb = _ws(workspace)
     _check(lib().cci_gated_linear_packed(X.data_ptr(), code, N, D, gate[0].data_ptr(), gate[1].data_ptr(),
                                          up[0].data_ptr(), up[1].data_ptr(), F, G, K, _act_code(act), H.data_ptr(),
@@ -706,7 +707,7 @@ def gated_linear_backward(dH: torch.Tensor, X: torch.Tensor, Wg: torch.Tensor, W
     dX = torch.empty_like(X) if need_dx else None
     dWg, dWu = (torch.empty_like(Wg), torch.empty_like(Wu)) if need_dw else (None, None)
     if workspace is None:
-        workspace = _workspace(_gated_bytes(GATED_BACKWARD, code, N, D, F), X.device)
+        workspace = _workspace(_gated_bytes(GATED_BACKWARD, code, N, D, F, X.device.index), X.device)
     wp, wb = _ws(workspace)
     _check(lib().cci_gated_linear_backward(dH.data_ptr(), X.data_ptr(), code, N, D, Wg.data_ptr(), Wu.data_ptr(), F,
                                            _act_code(act), g.data_ptr(), u.data_ptr(),
