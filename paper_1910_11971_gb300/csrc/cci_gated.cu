@@ -243,8 +243,10 @@ Layout layout(int dtype, int64_t N, int64_t D, int64_t F, int call)
     l.dg = take(call == CCI_GATED_BACKWARD, N * F);
     l.du = take(call == CCI_GATED_BACKWARD, N * F);
     l.parts = at;
-    if (call == CCI_GATED_BACKWARD) {  // the products follow each other: one place for both
-        const int terms = f32 ? 6 : 1;
+    const int terms = f32 ? 6 : 1;
+    if (call != CCI_GATED_BACKWARD) {
+        at += round256(plan(kForward, N, F, D, terms).part_bytes);
+    } else {  // the products follow each other: one place for both
         const size_t dx = plan(kDx, N, D, F, terms).part_bytes, dw = plan(kDw, F, D, N, terms).part_bytes;
         at += round256(dx > dw ? dx : dw);
     }
@@ -360,6 +362,7 @@ cudaError_t launch_gated(const GatedArgs &a, cudaStream_t stream)
     j.out[0] = a.H;
     j.save[0] = a.g;
     j.save[1] = a.u;
+    j.parts = reinterpret_cast<float *>(base + l.parts);
     j.M = a.N;
     j.N = a.F;
     j.K = a.D;

@@ -55,7 +55,8 @@ struct Params {
 // [0] gate, [1] up where an operand or output is one of two
 struct Maps {
     CUtensorMap a[2], b[2], out[2];
-    CUtensorMap save[2];  // forward: g and u; else [0]: parts
+    CUtensorMap save[2];  // forward: g and u
+    CUtensorMap parts;
 };
 
 template <int CG, int BN>
@@ -579,6 +580,12 @@ __global__ void __launch_bounds__(Cfg<CG, BN>::kThreads, 1)
             uint32_t o[32];
             // 32 finished columns from c on (forward: v the gate's, u the up projection's)
             auto output = [&](int c, uint32_t (&v)[32], const uint32_t (&u)[32]) {
+                if ((MODE != kForward || SPLIT) && work.part >= 0) {
+                    const int row = (work.part * CG + static_cast<int>(rank)) * C::kM;
+                    put(v, &maps.parts, c, row);
+                    if constexpr (MODE == kForward) put(u, &maps.parts, kNOut + c, row);
+                    return;
+                }
                 if constexpr (MODE == kForward) {
                     if (p.save) {
                         put(v, &maps.save[0], n0 + c, r0);
@@ -590,9 +597,7 @@ __global__ void __launch_bounds__(Cfg<CG, BN>::kThreads, 1)
                             v[j] = __float_as_uint(act_of<decltype(act)::value>(__uint_as_float(v[j])) * __uint_as_float(u[j]));
                     });
                 }
-                if (MODE != kForward && work.part >= 0) {
-                    put(v, &maps.save[0], c, (work.part * CG + static_cast<int>(rank)) * C::kM);
-                } else if (p.out_f32) {
+                if (p.out_f32) {
                     put(v, &maps.out[which], n0 + c, r0);
                 } else if constexpr (kNOut == 32) {
 #pragma unroll
@@ -674,15 +679,17 @@ __global__ void __launch_bounds__(Cfg<CG, BN>::kThreads, 1)
 }
 
 // the tiles whose reductions were cut: the sum of a tile's parts, in their order.  A block takes 8 rows of a tile
-// (blockIdx.x: tile, then rows), a thread 8 columns of one
+// (blockIdx.x: tile, then rows), a thread 8 columns of one (forward: of the gate and of the up projection, as many
+// threads; out0 is H, out1 g and out2 u, or null)
 template <int MODE, int CG, int BN>
-__global__ void __launch_bounds__(BN) join_kernel(const Params p, const float *parts, void *out0, void *out1, int units)
+__global__ void __launch_bounds__(MODE == kForward ? BN / 2 : BN)
+    join_kernel(const Params p, const float *parts, void *out0, void *out1, float *out2, int units)
 {
-    constexpr int kBlocks = CG * 128 / 8;
+    constexpr int kBlocks = CG * 128 / 8, kNOut = MODE == kForward ? BN / 2 : BN, kSums = MODE == kForward ? 2 : 1;
     const int per = p.pairs * p.terms * p.k_stages;
     const int rest = static_cast<int>(blockIdx.x) / kBlocks, tile = p.whole + rest;
-    const int row = static_cast<int>(blockIdx.x) % kBlocks * 8 + static_cast<int>(threadIdx.x) / (BN / 8);
-    const int col = static_cast<int>(threadIdx.x) % (BN / 8) * 8;
+    const int row = static_cast<int>(blockIdx.x) % kBlocks * 8 + static_cast<int>(threadIdx.x) / (kNOut / 8);
+    const int col = static_cast<int>(threadIdx.x) % (kNOut / 8) * 8;
     int mt, nt;
     tile_at(p, tile, MODE == kDw ? 2 * p.m_tiles : p.m_tiles, mt, nt);
     void *out = out0;
@@ -690,44 +697,66 @@ __global__ void __launch_bounds__(BN) join_kernel(const Params p, const float *p
         out = out1;
         mt -= p.m_tiles;
     }
-    const int64_t r = static_cast<int64_t>(mt) * CG * 128 + row, c = static_cast<int64_t>(nt) * BN + col;
+    const int64_t r = static_cast<int64_t>(mt) * CG * 128 + row, c = static_cast<int64_t>(nt) * kNOut + col;
     tc::wait_prior_grid();
     if (r >= p.M || c >= p.N) return;  // N is a multiple of 8
-    // the units whose shares meet the tile: from the one that holds its first stage on
+    // the units whose shares meet the tile: `unit`, which holds its first stage, to `last`, which holds its last one
     const int64_t all = static_cast<int64_t>(p.tiles - p.whole) * per, t0 = static_cast<int64_t>(rest) * per;
-    int unit = static_cast<int>(t0 * units / all);
-    while (all * (unit + 1) / units <= t0) ++unit;
-    float v[8] = {};
-    bool cut = false;
-    for (; unit < units; ++unit) {
-        const int64_t b0 = all * unit / units, b1 = all * (unit + 1) / units;
-        if (b0 >= t0 + per) break;
-        if (b0 <= t0 && b1 >= t0 + per) return;  // computed whole
-        if (b0 == b1) continue;
-        // a unit's second piece if its share began in the tile before
-        const int part = 2 * unit + (b0 < t0 ? 1 : 0);
-        const float4 *at = reinterpret_cast<const float4 *>(parts + (static_cast<int64_t>(part) * CG * 128 + row) * BN + col);
-        const float4 a = at[0], b = at[1];
-        v[0] += a.x;
-        v[1] += a.y;
-        v[2] += a.z;
-        v[3] += a.w;
-        v[4] += b.x;
-        v[5] += b.y;
-        v[6] += b.z;
-        v[7] += b.w;
-        cut = true;
+    auto holder = [&](int64_t stage) {
+        int q = static_cast<int>(stage * units / all);
+        while (all * (q + 1) / units <= stage) ++q;
+        return q;
+    };
+    const int unit = holder(t0), last = holder(t0 + per - 1);
+    if (unit == last) return;  // computed whole
+    // a unit's part is its first piece, but for one whose share began in the tile before
+    const int64_t stride = static_cast<int64_t>(CG * 128) * BN;
+    const float *at = parts + static_cast<int64_t>(row) * BN + col;
+    const float *first = at + (2 * unit + (all * unit / units < t0 ? 1 : 0)) * stride;
+    float v[kSums][8];
+#pragma unroll
+    for (int w = 0; w < kSums; ++w) {
+        *reinterpret_cast<float4 *>(v[w]) = *reinterpret_cast<const float4 *>(first + w * kNOut);
+        *reinterpret_cast<float4 *>(v[w] + 4) = *reinterpret_cast<const float4 *>(first + w * kNOut + 4);
     }
-    if (!cut) return;
+    // the loads of four parts are on their way at a time (3 tokens, 192 -> 8072 fp32, dX of 152 parts: 53 us one by
+    // one, 33 to 35 so)
+#pragma unroll 4
+    for (int q = unit + 1; q <= last; ++q)
+#pragma unroll
+        for (int w = 0; w < kSums; ++w) {
+            const float4 *one = reinterpret_cast<const float4 *>(at + 2 * q * stride + w * kNOut);
+            const float4 a = one[0], b = one[1];
+            v[w][0] += a.x;
+            v[w][1] += a.y;
+            v[w][2] += a.z;
+            v[w][3] += a.w;
+            v[w][4] += b.x;
+            v[w][5] += b.y;
+            v[w][6] += b.z;
+            v[w][7] += b.w;
+        }
     const int64_t o = r * p.N + c;
+    auto store = [&](float *to, const float *from) {
+        reinterpret_cast<float4 *>(to)[0] = make_float4(from[0], from[1], from[2], from[3]);
+        reinterpret_cast<float4 *>(to)[1] = make_float4(from[4], from[5], from[6], from[7]);
+    };
+    if constexpr (MODE == kForward) {
+        if (p.save) {
+            store(static_cast<float *>(out1) + o, v[0]);
+            store(out2 + o, v[1]);
+        }
+        with_act(p.act, [&](auto act) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[0][j] = act_of<decltype(act)::value>(v[0][j]) * v[1][j];
+        });
+    }
     if (p.out_f32) {
-        float4 *to = reinterpret_cast<float4 *>(static_cast<float *>(out) + o);
-        to[0] = make_float4(v[0], v[1], v[2], v[3]);
-        to[1] = make_float4(v[4], v[5], v[6], v[7]);
+        store(static_cast<float *>(out) + o, v[0]);
     } else {
         uint32_t w[4];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) w[j] = ws::bf16x2_rn(__float_as_uint(v[2 * j]), __float_as_uint(v[2 * j + 1]));
+        for (int j = 0; j < 4; ++j) w[j] = ws::bf16x2_rn(__float_as_uint(v[0][2 * j]), __float_as_uint(v[0][2 * j + 1]));
         *reinterpret_cast<uint4 *>(static_cast<uint16_t *>(out) + o) = make_uint4(w[0], w[1], w[2], w[3]);
     }
 }
@@ -769,7 +798,7 @@ struct Job {
     float *save[2];   // forward: g and u, or null
     int64_t M, N, K;  // rows and columns of an output, length of a reduction
     int terms, act, out_f32;
-    float *parts;     // dX, dW: plan().part_bytes of workspace
+    float *parts;     // plan().part_bytes of workspace
     uint32_t *status;
 };
 
@@ -778,6 +807,7 @@ struct Job {
 struct Plan {
     int cg, bn;
     bool cut;
+    int units;  // CTAs (pairs) that share the cut reductions
     size_t part_bytes;
 };
 
@@ -785,8 +815,9 @@ struct Plan {
 // in a 256 x 256 pair tile, 256 in a 128 x 128 one and 192 in a 128 x 64 one, or that of its copies at about 64
 // bytes a cycle and SM (what L2 gives all SMs at once); a round about 4000 more for the first copies and the last
 // output.  Cutting the last tiles' reductions fills the last round, but writes and reads parts and takes a launch:
-// about 20000 cycles (dX of 4096 tokens, 4096 -> 8192: 256 tiles over 76 pairs, 394 us whole, 291 cut).  The
-// forward pass, whose epilogue wants g and u together, is not cut
+// about 20000 cycles (dX of 4096 tokens, 4096 -> 8192: 256 tiles over 76 pairs, 394 us whole, 291 cut).  Where
+// even eight stages each are too few for all SMs, fewer share them.  The forward pass is cut in fp32 alone, where it has
+// a workspace (427 tokens, 4088 -> 648: 122 us whole, 69 cut); its parts hold g and u, which the join then joins
 inline Plan plan(Mode mode, int64_t M, int64_t N, int64_t K, int terms)
 {
     const int64_t sms = ws::sm_count(), outs = mode == kDw ? 2 : 1;
@@ -805,22 +836,24 @@ inline Plan plan(Mode mode, int64_t M, int64_t N, int64_t K, int terms)
         const double stage = copies > shape[2] ? copies : shape[2], tile = static_cast<double>(stages) * stage;
         const int64_t rounds = (tiles + units - 1) / units, rest = tiles % units;
         const double whole = static_cast<double>(rounds) * (tile + 4000.0);
-        double cut = static_cast<double>(tiles) / static_cast<double>(units) * tile + static_cast<double>(rounds) * 4000.0 + 20000.0;
-        // every share has some stages, and is shorter than a tile
-        const bool can = mode != kForward && rest > 0 && rest * stages >= 8 * units;
+        // every share has eight stages or more, and is shorter than a tile
+        const int64_t shares = tiles < units && tiles * stages / 8 < units ? tiles * stages / 8 : units;
+        const bool can = (mode != kForward || terms > 1) && rest > 0 && shares > rest && rest * stages >= 8 * shares;
+        double cut = static_cast<double>(tiles) / static_cast<double>(can ? shares : units) * tile +
+                     static_cast<double>(rounds) * 4000.0 + 20000.0;
         if (!can) cut = whole;
         const double cost = cut < whole ? cut : whole;
         if (best.cg == 0 || cost < least) {
             least = cost;
-            best = Plan{cg, bn, cut < whole, 0};
-            if (best.cut) best.part_bytes = static_cast<size_t>(units) * 2 * cg * 128 * bn * sizeof(float);
+            best = Plan{cg, bn, cut < whole, static_cast<int>(shares), 0};
+            if (best.cut) best.part_bytes = static_cast<size_t>(shares) * 2 * cg * 128 * bn * sizeof(float);
         }
     }
     return best;
 }
 
 template <int MODE, int CG, int BN, bool SPLIT>
-cudaError_t launch_tiled(const Job &j, bool cut, cudaStream_t stream)
+cudaError_t launch_tiled(const Job &j, const Plan &plan, cudaStream_t stream)
 {
     using C = Cfg<CG, BN>;
     constexpr int kNOut = MODE == kForward ? BN / 2 : BN;
@@ -842,7 +875,8 @@ cudaError_t launch_tiled(const Job &j, bool cut, cudaStream_t stream)
     p.m_tiles = static_cast<int>(mt);
     p.n_tiles = static_cast<int>(nt);
     p.tiles = static_cast<int>(mt * two_out * nt);
-    const int units = ws::sm_count() / CG;
+    const bool cut = plan.cut;
+    const int units = cut ? plan.units : ws::sm_count() / CG;
     p.whole = cut ? p.tiles - p.tiles % units : p.tiles;
     for (int i = 0; i < two_a; ++i)
         if (!operand_map(&maps.a[i], j.a[i], MODE == kDw ? 64 : p.a_rows)) return cudaErrorInvalidValue;
@@ -855,7 +889,7 @@ cudaError_t launch_tiled(const Job &j, bool cut, cudaStream_t stream)
     if (p.save)
         for (int i = 0; i < 2; ++i)
             if (!output_map(&maps.save[i], j.save[i], true, j.M, j.N, 32)) return cudaErrorInvalidValue;
-    if (cut && !output_map(&maps.save[0], j.parts, true, static_cast<int64_t>(units) * 2 * CG * 128, BN, 32))
+    if (cut && !output_map(&maps.parts, j.parts, true, static_cast<int64_t>(units) * 2 * CG * 128, BN, 32))
         return cudaErrorInvalidValue;
     static SmemAttrCache attr_cache;
     const cudaError_t attr = smem_attr_once(product_kernel<MODE, CG, BN, SPLIT>, static_cast<int>(C::kSmem), attr_cache);
@@ -875,18 +909,19 @@ cudaError_t launch_tiled(const Job &j, bool cut, cudaStream_t stream)
     cfg.numAttrs = CG == 2 ? 1 : 0;
     cudaError_t e = cudaLaunchKernelEx(&cfg, product_kernel<MODE, CG, BN, SPLIT>, p, maps);
     if (e == cudaSuccess) e = cudaGetLastError();
-    if constexpr (MODE != kForward) {
+    if constexpr (MODE != kForward || SPLIT) {
         if (e != cudaSuccess || !cut) return e;
         cudaLaunchConfig_t jc = {};
         jc.gridDim = dim3(static_cast<unsigned>((p.tiles - p.whole) * (CG * 128 / 8)));
-        jc.blockDim = dim3(BN);
+        jc.blockDim = dim3(kNOut);
         jc.stream = stream;
         la[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
         la[0].val.programmaticStreamSerializationAllowed = 1;
         jc.attrs = la;
         jc.numAttrs = 1;
-        e = cudaLaunchKernelEx(&jc, join_kernel<MODE, CG, BN>, p, const_cast<const float *>(j.parts), j.out[0],
-                               j.out[MODE == kDw ? 1 : 0], units);
+        void *second = MODE == kForward ? static_cast<void *>(j.save[0]) : j.out[MODE == kDw ? 1 : 0];
+        e = cudaLaunchKernelEx(&jc, join_kernel<MODE, CG, BN>, p, const_cast<const float *>(j.parts), j.out[0], second,
+                               j.save[1], units);
         if (e == cudaSuccess) e = cudaGetLastError();
     }
     return e;
@@ -897,11 +932,11 @@ cudaError_t launch(const Job &j, cudaStream_t stream)
 {
     const Plan pl = plan(static_cast<Mode>(MODE), j.M, j.N, j.K, j.terms);
     if (j.terms > 1)
-        return pl.bn == 128 ? launch_tiled<MODE, 1, 128, true>(j, pl.cut, stream)
-                            : launch_tiled<MODE, 1, 64, true>(j, pl.cut, stream);
-    if (pl.cg == 2) return launch_tiled<MODE, 2, 256, false>(j, pl.cut, stream);
-    return pl.bn == 128 ? launch_tiled<MODE, 1, 128, false>(j, pl.cut, stream)
-                        : launch_tiled<MODE, 1, 64, false>(j, pl.cut, stream);
+        return pl.bn == 128 ? launch_tiled<MODE, 1, 128, true>(j, pl, stream)
+                            : launch_tiled<MODE, 1, 64, true>(j, pl, stream);
+    if (pl.cg == 2) return launch_tiled<MODE, 2, 256, false>(j, pl, stream);
+    return pl.bn == 128 ? launch_tiled<MODE, 1, 128, false>(j, pl, stream)
+                        : launch_tiled<MODE, 1, 64, false>(j, pl, stream);
 }
 
 // few tokens (cci_gated_few.cu): few_tokens, dense weights [F][D] of dtype; few_packed, also the packed ones (wg
