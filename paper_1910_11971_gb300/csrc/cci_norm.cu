@@ -51,6 +51,19 @@ constexpr int stages_of(int bytes, int groups, int blocks)
     return fit < kMaxStages ? fit : kMaxStages;
 }
 
+// Parameters of wide rows, which no registers are left for, lie in shared memory beside the ring where that keeps
+// two stages or more: bytes of them, and the ring's stages then.  From L2 they are 8 bytes an element again for every
+// row (forward bf16 8000 x 8192 95 us, 81 so; fp32 16384 x 4096 165 and 123; backward bf16 4000 x 16384 151 and 106).  Not
+// where a block has few rows (forward bf16 100 x 8192: 3.8 us, 4.5 with them), nor in the backward pass of fp32 rows
+// (8000 x 8192: 136 us, 145 with it)
+constexpr int kWideBudget = 224 * 1024;
+constexpr int shared_params(int bytes, int stage) { return (kWideBudget - bytes) / stage >= 2 ? bytes : 0; }
+constexpr int stages_beside(int params, int stage)
+{
+    const int fit = (kWideBudget - params) / stage;
+    return fit < kMaxStages ? fit : kMaxStages;
+}
+
 // V consecutive fp32 parameters from p[c] on, or `missing` where there are none
 template <int V>
 __device__ __forceinline__ void params_at(const float *p, int c, float missing, float *v)
@@ -142,6 +155,35 @@ __device__ __forceinline__ Pairs<V> params2(const float *w, int i, int t, int D,
     return r;
 }
 
+// parameters in shared memory: the words of four of every V columns together, so that neighbours read neighbours
+template <int V, int E, int TPR>
+__device__ __forceinline__ void keep_params(float *to, const float *w, int t, int D, float missing)
+{
+    constexpr int kVectors = E * TPR / V;
+    for (int z = t; z < kVectors; z += TPR) {
+        float f[V] = {};
+        if (z * V < D) params_at<V>(w, z * V, missing, f);
+#pragma unroll
+        for (int j = 0; j < V / 4; ++j)
+            *reinterpret_cast<float4 *>(to + (j * kVectors + z) * 4) =
+                make_float4(f[4 * j], f[4 * j + 1], f[4 * j + 2], f[4 * j + 3]);
+    }
+}
+
+template <int V, int E, int TPR>
+__device__ __forceinline__ Pairs<V> kept_params(const float *from, int i, int t)
+{
+    constexpr int kVectors = E * TPR / V;
+    Pairs<V> r;
+#pragma unroll
+    for (int j = 0; j < V / 4; ++j) {
+        const float4 q = *reinterpret_cast<const float4 *>(from + (j * kVectors + i * TPR + t) * 4);
+        r.p[2 * j] = pack2(q.x, q.y);
+        r.p[2 * j + 1] = pack2(q.z, q.w);
+    }
+    return r;
+}
+
 template <typename T, int V, int TPR>
 __device__ __forceinline__ void store_pairs(T *y, int i, int t, int D, const Pairs<V> &o)
 {
@@ -157,15 +199,25 @@ __device__ __forceinline__ void store_pairs(T *y, int i, int t, int D, const Pai
 
 // ---- forward: E columns per thread, in vectors of V.  Groups walk the rows; the next rows are on their way while
 // one is reduced.  Rows of up to 4096 keep weight and bias in registers ----
-template <typename T, int V, int E, int TPR>
+// its shared memory: the ring, then weight and bias (KEEP: where that can be)
+template <typename T, int V, int E, int TPR, bool KEEP>
+struct Forward {
+    static constexpr int kGroups = block_threads(TPR) / TPR;
+    static constexpr bool kHold = TPR <= 256, kBulk = V > 1;
+    static constexpr int kStage = E * TPR * static_cast<int>(sizeof(T));
+    static constexpr int kParams = KEEP && kBulk && !kHold ? shared_params(2 * E * TPR * 4, kStage) : 0;
+    static constexpr int kStages = kParams ? stages_beside(kParams, kStage) : stages_of(kStage, kGroups, residents(TPR, (V > 1), false));
+    static constexpr int kBytes = kBulk ? kStages * kStage * kGroups + kParams : 0;
+};
+
+template <typename T, int V, int E, int TPR, bool KEEP>
 __global__ void __launch_bounds__(block_threads(TPR), residents(TPR, (V > 1), false))
     norm_kernel(const T *x, int64_t ldx, int64_t N, int D, const float *w, const float *b, float eps, T *y, float *mean,
                 float *rstd)
 {
-    constexpr int kGroups = block_threads(TPR) / TPR, kNV = E / V;
-    constexpr bool kHold = TPR <= 256, kBulk = V > 1;
-    constexpr int kStage = E * TPR * static_cast<int>(sizeof(T));
-    constexpr int kStages = stages_of(kStage, kGroups, residents(TPR, (V > 1), false));
+    using C = Forward<T, V, E, TPR, KEEP>;
+    constexpr int kGroups = C::kGroups, kNV = E / V, kStage = C::kStage, kStages = C::kStages;
+    constexpr bool kHold = C::kHold, kBulk = C::kBulk, kKept = C::kParams > 0;
     extern __shared__ __align__(128) unsigned char ring_raw[];
     __shared__ Ring rings[kGroups];
     __shared__ float buf[kGroups][2][TPR / 32];
@@ -175,6 +227,7 @@ __global__ void __launch_bounds__(block_threads(TPR), residents(TPR, (V > 1), fa
     const int64_t step = static_cast<int64_t>(gridDim.x) * kGroups;
     const int64_t n0 = static_cast<int64_t>(blockIdx.x) * kGroups + group;
     unsigned char *ring = ring_raw + group * kStages * kStage;
+    float *kept = reinterpret_cast<float *>(ring_raw + kStages * kStage);  // with one group
     Ring &R = rings[group];
     volatile int *abort = &abort_flag;
     const uint32_t bytes = static_cast<uint32_t>(D) * sizeof(T);
@@ -186,6 +239,10 @@ __global__ void __launch_bounds__(block_threads(TPR), residents(TPR, (V > 1), fa
     if constexpr (kBulk) {
         if (threadIdx.x == 0) abort_flag = 0;
         zero_tails<T, V, E, TPR>(ring, kStages, t, D);
+        if constexpr (kKept) {
+            keep_params<V, E, TPR>(kept, w, t, D, 1.f);
+            keep_params<V, E, TPR>(kept + E * TPR, b, t, D, 0.f);
+        }
         if (t == 0) {
             for (int s = 0; s < kStages; ++s) tc::mbar_init(&R.full[s], 1);
             asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -259,7 +316,10 @@ __global__ void __launch_bounds__(block_threads(TPR), residents(TPR, (V > 1), fa
         const unsigned long long r2 = pack2(r, r);
 #pragma unroll
         for (int i = 0; i < kNV; i += kStep) {
-            if constexpr (!kHold) {
+            if constexpr (kKept) {
+                wv[0] = kept_params<V, E, TPR>(kept, i, t);
+                bv[0] = kept_params<V, E, TPR>(kept + E * TPR, i, t);
+            } else if constexpr (!kHold) {
                 wv[0] = params2<V, TPR>(w, i, t, D, 1.f);
                 bv[0] = params2<V, TPR>(b, i, t, D, 0.f);
             }
@@ -341,17 +401,32 @@ __device__ __forceinline__ Pairs<V> input_gradient(const Pairs<V> &x, const Pair
 }
 
 // ---- backward: dx, and this block's sums of dw and db to pw and pb, each block 2 D further ----
+// its shared memory: the ring, then the weight; after the rows, the groups' sums
+template <typename T, int V, int E, int TPR>
+struct Backward {
+    static constexpr int kGroups = block_threads(TPR) / TPR;
+    static constexpr bool kHold = TPR < 1024;  // the weight in registers
+    static constexpr int kRow = E * TPR * static_cast<int>(sizeof(T)), kStage = 2 * kRow;  // a stage: x, then dy
+    static constexpr int kParams = V > 1 && !kHold && sizeof(T) == 2 ? shared_params(E * TPR * 4, kStage) : 0;
+    static constexpr int kStages = kParams ? stages_beside(kParams, kStage) : stages_of(kStage, kGroups, residents(TPR, (V > 1), true));
+    static constexpr bool kBulk = V > 1 && kStages >= 2;
+    // rows at a time, so that their sums share the exchanges and the barrier; a ring has one more such set at least
+    static constexpr int kRows = kStages % 2 == 0 && kStages > 2 ? 2 : 1;
+    static constexpr int kRing = kBulk ? kStages * kStage * kGroups + kParams : 0;
+    static constexpr int kSums = kGroups > 1 ? 2 * E * TPR * static_cast<int>(sizeof(float)) : 0;
+    static constexpr int kBytes = kRing > kSums ? kRing : kSums;
+};
+
 template <typename T, int V, int E, int TPR>
 __global__ void __launch_bounds__(block_threads(TPR), residents(TPR, (V > 1), true))
     norm_backward_kernel(const T *dy, int64_t lddy, const T *x, int64_t ldx, const float *mean, const float *rstd,
                          const float *w, int64_t N, int D, T *dx, float *pw, float *pb)
 {
-    constexpr int kGroups = block_threads(TPR) / TPR, kNV = E / V;
-    constexpr int kRow = E * TPR * static_cast<int>(sizeof(T)), kStage = 2 * kRow;  // a stage: x, then dy
-    constexpr int kStages = stages_of(kStage, kGroups, residents(TPR, (V > 1), true));
+    using C = Backward<T, V, E, TPR>;
+    constexpr int kGroups = C::kGroups, kNV = E / V, kRow = C::kRow, kStage = C::kStage, kStages = C::kStages;
     // two stages at least; else, and for rows off whole words, a row is loaded into registers, or where 1024 threads
     // have none left, both passes over it read global memory, the second from L1
-    constexpr bool kBulk = V > 1 && kStages >= 2, kKeep = !kBulk && TPR < 1024;
+    constexpr bool kBulk = C::kBulk, kKeep = !kBulk && TPR < 1024, kHold = C::kHold, kKept = kBulk && C::kParams > 0;
     extern __shared__ __align__(128) unsigned char ring_raw[];
     __shared__ Ring rings[kGroups];
     __shared__ float buf[kGroups][2][4 * TPR / 32];
@@ -361,6 +436,7 @@ __global__ void __launch_bounds__(block_threads(TPR), residents(TPR, (V > 1), tr
     const int64_t step = static_cast<int64_t>(gridDim.x) * kGroups;
     const int64_t n0 = static_cast<int64_t>(blockIdx.x) * kGroups + group;
     unsigned char *ring = ring_raw + group * kStages * kStage;
+    float *kept = reinterpret_cast<float *>(ring_raw + kStages * kStage);  // with one group
     Ring &R = rings[group];
     volatile int *abort = &abort_flag;
     const uint32_t bytes = static_cast<uint32_t>(D) * sizeof(T);
@@ -374,6 +450,7 @@ __global__ void __launch_bounds__(block_threads(TPR), residents(TPR, (V > 1), tr
     if constexpr (kBulk) {
         if (threadIdx.x == 0) abort_flag = 0;
         zero_tails<T, V, E, TPR>(ring, 2 * kStages, t, D);
+        if constexpr (kKept) keep_params<V, E, TPR>(kept, w, t, D, 1.f);
         if (t == 0) {
             for (int s = 0; s < kStages; ++s) tc::mbar_init(&R.full[s], 1);
             asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -382,7 +459,6 @@ __global__ void __launch_bounds__(block_threads(TPR), residents(TPR, (V > 1), tr
         }
         __syncthreads();
     }
-    constexpr bool kHold = TPR < 1024;  // the weight in registers
     constexpr int kStep = Pairs<V>::kStep, kP = Pairs<V>::kP;
     unsigned long long dw[E / 2], db[E / 2];
     Pairs<V> wv[kHold ? E / 2 / kP : 1];
@@ -394,8 +470,7 @@ __global__ void __launch_bounds__(block_threads(TPR), residents(TPR, (V > 1), tr
     }
     int k = 0;
     if constexpr (kBulk) {
-        // kRows rows at a time, so that their sums share the exchanges and the barrier
-        constexpr int kRows = kStages % 2 == 0 ? 2 : 1;
+        constexpr int kRows = C::kRows;
         int st = 0;
         uint32_t ph = 0u;
         float mu[kRows], r[kRows];  // of the next rows
@@ -430,7 +505,10 @@ __global__ void __launch_bounds__(block_threads(TPR), residents(TPR, (V > 1), tr
                 for (int i = 0; i < kNV; i += kStep) {
                     const Pairs<V> xp = pairs_at<T, V, TPR, true>(xr[q], i, t, D);
                     const Pairs<V> gp = pairs_at<T, V, TPR, true>(dr[q], i, t, D);
-                    if constexpr (!kHold) wv[0] = params2<V, TPR>(w, i, t, D, 1.f);
+                    if constexpr (kKept)
+                        wv[0] = kept_params<V, E, TPR>(kept, i, t);
+                    else if constexpr (!kHold)
+                        wv[0] = params2<V, TPR>(w, i, t, D, 1.f);
                     add_columns<V>(xp, gp, wv[kHold ? i / kStep : 0], minus_m, rn2, dw + i / kStep * kP, db + i / kStep * kP, s0, s1);
                 }
                 s[2 * q] = lo_of(s0) + hi_of(s0);
@@ -459,7 +537,10 @@ __global__ void __launch_bounds__(block_threads(TPR), residents(TPR, (V > 1), tr
                 for (int i = 0; i < kNV; i += kStep) {
                     const Pairs<V> xp = pairs_at<T, V, TPR, true>(xr[q], i, t, D);
                     const Pairs<V> gp = pairs_at<T, V, TPR, true>(dr[q], i, t, D);
-                    if constexpr (!kHold) wv[0] = params2<V, TPR>(w, i, t, D, 1.f);
+                    if constexpr (kKept)
+                        wv[0] = kept_params<V, E, TPR>(kept, i, t);
+                    else if constexpr (!kHold)
+                        wv[0] = params2<V, TPR>(w, i, t, D, 1.f);
                     store_pairs<T, V, TPR>(dx + (n + q * step) * D, i, t, D,
                                            input_gradient<V>(xp, gp, wv[kHold ? i / kStep : 0], minus_m, rn2, minus_a, minus_b));
                 }
@@ -716,29 +797,33 @@ int64_t most_parts(int64_t N, int64_t D)
     return a > b ? a : b;
 }
 
-template <typename T, int V, int E, int TPR>
-cudaError_t forward_one(const Args &a)
+template <typename T, int V, int E, int TPR, bool KEEP>
+cudaError_t forward_as(const Args &a, int64_t blocks)
 {
-    constexpr int kT = block_threads(TPR), kGroups = kT / TPR, kStage = E * TPR * static_cast<int>(sizeof(T));
-    constexpr int bytes = V > 1 ? stages_of(kStage, kGroups, residents(TPR, (V > 1), false)) * kStage * kGroups : 0;
+    constexpr int kT = block_threads(TPR), bytes = Forward<T, V, E, TPR, KEEP>::kBytes;
     static SmemAttrCache attr_cache;
-    const cudaError_t attr = smem_attr_once(norm_kernel<T, V, E, TPR>, bytes, attr_cache);
+    const cudaError_t attr = smem_attr_once(norm_kernel<T, V, E, TPR, KEEP>, bytes, attr_cache);
     if (attr != cudaSuccess) return attr;
-    const int64_t blocks = least((a.N + kGroups - 1) / kGroups, static_cast<int64_t>(row::sm_count()) * residents(TPR, (V > 1), false));
-    norm_kernel<T, V, E, TPR><<<static_cast<unsigned>(blocks), kT, bytes, a.stream>>>(
+    norm_kernel<T, V, E, TPR, KEEP><<<static_cast<unsigned>(blocks), kT, bytes, a.stream>>>(
         static_cast<const T *>(a.x), a.ldx, a.N, static_cast<int>(a.D), a.w, a.b, a.eps, static_cast<T *>(a.y), a.mean,
         a.rstd);
     return cudaGetLastError();
 }
 
 template <typename T, int V, int E, int TPR>
+cudaError_t forward_one(const Args &a)
+{
+    constexpr int kGroups = block_threads(TPR) / TPR;
+    const int64_t blocks = least((a.N + kGroups - 1) / kGroups, static_cast<int64_t>(row::sm_count()) * residents(TPR, (V > 1), false));
+    if constexpr (Forward<T, V, E, TPR, true>::kParams > 0)
+        if (a.N > 4 * blocks) return forward_as<T, V, E, TPR, true>(a, blocks);  // rows enough for it
+    return forward_as<T, V, E, TPR, false>(a, blocks);
+}
+
+template <typename T, int V, int E, int TPR>
 cudaError_t backward_one(const Args &a)
 {
-    constexpr int kT = block_threads(TPR), kGroups = kT / TPR, kStage = 2 * E * TPR * static_cast<int>(sizeof(T));
-    constexpr int stages = stages_of(kStage, kGroups, residents(TPR, (V > 1), true));
-    constexpr int ring = V > 1 && stages >= 2 ? stages * kStage * kGroups : 0;
-    constexpr int comb = kGroups > 1 ? 2 * E * TPR * static_cast<int>(sizeof(float)) : 0;
-    constexpr int bytes = ring > comb ? ring : comb;
+    constexpr int kT = block_threads(TPR), bytes = Backward<T, V, E, TPR>::kBytes;
     static SmemAttrCache attr_cache;
     const cudaError_t attr = smem_attr_once(norm_backward_kernel<T, V, E, TPR>, bytes, attr_cache);
     if (attr != cudaSuccess) return attr;
