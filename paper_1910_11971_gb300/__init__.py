@@ -71,9 +71,12 @@ SIGNATURES = {
     "cci_dense_conv2d_tc": (_I32, [_P, _I32, _I64, _I64, _I64, _I64, _P, _I64, _I32, _I32, _I32, _I32,
                                    _I32, _I32, _P, _U32P, _P]),
     "cci_layer_norm": (_I32, [_P, _I32, _I64, _I64, _I64, _P, _P, ctypes.c_float, _P, _P, _P, _P]),
+    "cci_layer_norm_ex": (_I32, [_P, _I32, _I64, _I64, _I64, _P, _P, ctypes.c_float, _P, _P, _P, _U32P, _P]),
     "cci_layer_norm_workspace_size": (ctypes.c_size_t, [_I64, _I64]),
     "cci_layer_norm_backward": (_I32, [_P, _I64, _P, _I64, _I32, _I64, _I64, _P, _P, _P, _P, _P, _P, _P,
                                        ctypes.c_size_t, _P]),
+    "cci_layer_norm_backward_ex": (_I32, [_P, _I64, _P, _I64, _I32, _I64, _I64, _P, _P, _P, _P, _P, _P, _U32P, _P,
+                                          ctypes.c_size_t, _P]),
     "cci_token_logprobs": (_I32, [_P, _I32, _I64, _I64, _I64, _P, _I64, _I32, _P, _P, _P, _P, _P, _U32P, _P]),
     "cci_token_logprobs_backward": (_I32, [_P, _I32, _I64, _I64, _I64, _P, _P, _I64, _P, _P, _P, _P, _I64, _U32P,
                                            _P]),
@@ -520,8 +523,8 @@ def _cuda_vec(t: Optional[torch.Tensor], n: int, name: str, dtype: torch.dtype =
 
 
 def layer_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None, *,
-               eps: float = 1e-5, out: Optional[torch.Tensor] = None):
-    """(y, mean, rstd) of the rows of x[N][D] (``cci_layer_norm``): y in x's dtype, the
+               eps: float = 1e-5, out: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None):
+    """(y, mean, rstd) of the rows of x[N][D] (``cci_layer_norm_ex``): y in x's dtype, the
     fp32 mean and 1 / sqrt(var + eps) of each row for the backward pass.  ``weight`` and ``bias``
     are fp32 [D]; x may have a row stride."""
     ld = _cuda_rows(x, "x")
@@ -532,16 +535,17 @@ def layer_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Opt
     # small outputs are allocated one by one: views of one allocation cost the host more
     mean = torch.empty(N, dtype=torch.float32, device=x.device)
     rstd = torch.empty(N, dtype=torch.float32, device=x.device)
-    _check(lib().cci_layer_norm(x.data_ptr(), _dtype_code(x), N, D, ld, _cuda_vec(weight, D, "weight"),
-                                _cuda_vec(bias, D, "bias"), eps, y.data_ptr(), mean.data_ptr(), rstd.data_ptr(),
-                                _stream(x.device)), "cci_layer_norm")
+    _check(lib().cci_layer_norm_ex(x.data_ptr(), _dtype_code(x), N, D, ld, _cuda_vec(weight, D, "weight"),
+                                   _cuda_vec(bias, D, "bias"), eps, y.data_ptr(), mean.data_ptr(), rstd.data_ptr(),
+                                   status.data_ptr() if status is not None else None, _stream(x.device)),
+           "cci_layer_norm")
     return y, mean, rstd
 
 
 def layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, mean: torch.Tensor, rstd: torch.Tensor,
                         weight: Optional[torch.Tensor] = None, *, out: Optional[torch.Tensor] = None,
-                        workspace: Optional[torch.Tensor] = None):
-    """(dx, dweight, dbias) of ``layer_norm`` (``cci_layer_norm_backward``): dx in x's dtype,
+                        workspace: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None):
+    """(dx, dweight, dbias) of ``layer_norm`` (``cci_layer_norm_backward_ex``): dx in x's dtype,
     the parameters' gradients fp32 [D], whether or not the forward call had them."""
     ldx, lddy = _cuda_rows(x, "x"), _cuda_rows(dy, "dy")
     N, D = x.shape
@@ -555,10 +559,11 @@ def layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, mean: torch.Tensor, r
     if workspace is None:
         workspace = _workspace(_norm_bytes(N, D, x.device.index), x.device)
     wp, wb = _ws(workspace)
-    _check(lib().cci_layer_norm_backward(dy.data_ptr(), lddy, x.data_ptr(), ldx, _dtype_code(x), N, D,
-                                         _cuda_vec(mean, N, "mean"), _cuda_vec(rstd, N, "rstd"),
-                                         _cuda_vec(weight, D, "weight"), dx.data_ptr(), dw.data_ptr(), db.data_ptr(),
-                                         wp, wb, _stream(x.device)), "cci_layer_norm_backward")
+    _check(lib().cci_layer_norm_backward_ex(dy.data_ptr(), lddy, x.data_ptr(), ldx, _dtype_code(x), N, D,
+                                            _cuda_vec(mean, N, "mean"), _cuda_vec(rstd, N, "rstd"),
+                                            _cuda_vec(weight, D, "weight"), dx.data_ptr(), dw.data_ptr(),
+                                            db.data_ptr(), status.data_ptr() if status is not None else None, wp, wb,
+                                            _stream(x.device)), "cci_layer_norm_backward")
     return dx, dw, db
 
 

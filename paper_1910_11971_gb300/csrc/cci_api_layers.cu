@@ -20,8 +20,9 @@ bool rows_ok(int64_t N, int64_t D, int64_t ld) { return N >= 0 && D >= 1 && ld >
 
 extern "C" {
 
-cci_status cci_layer_norm(const void *x, cci_dtype dtype, int64_t N, int64_t D, int64_t ldx, const float *weight,
-                          const float *bias, float eps, void *y, float *mean, float *rstd, cci_stream_t stream)
+cci_status cci_layer_norm_ex(const void *x, cci_dtype dtype, int64_t N, int64_t D, int64_t ldx, const float *weight,
+                             const float *bias, float eps, void *y, float *mean, float *rstd, uint32_t *dev_status,
+                             cci_stream_t stream)
 {
     if (!valid_dtype(dtype)) return CCI_ERR_DTYPE;
     if (N > 0 && (!x || !y || !mean || !rstd)) return CCI_ERR_NULL;
@@ -32,7 +33,14 @@ cci_status cci_layer_norm(const void *x, cci_dtype dtype, int64_t N, int64_t D, 
         !aligned(rstd, 4))
         return CCI_ERR_ALIGN;
     if (N == 0) return CCI_OK;
-    return to_status(launch_layer_norm(x, dtype, N, D, ldx, weight, bias, eps, y, mean, rstd, as_stream(stream)));
+    return to_status(launch_layer_norm(x, dtype, N, D, ldx, weight, bias, eps, y, mean, rstd, dev_status,
+                                       as_stream(stream)));
+}
+
+cci_status cci_layer_norm(const void *x, cci_dtype dtype, int64_t N, int64_t D, int64_t ldx, const float *weight,
+                          const float *bias, float eps, void *y, float *mean, float *rstd, cci_stream_t stream)
+{
+    return cci_layer_norm_ex(x, dtype, N, D, ldx, weight, bias, eps, y, mean, rstd, nullptr, stream);
 }
 
 size_t cci_layer_norm_workspace_size(int64_t N, int64_t D)
@@ -40,10 +48,10 @@ size_t cci_layer_norm_workspace_size(int64_t N, int64_t D)
     return N < 1 || D < 1 || !mul_ok(N, D) ? 0 : layer_norm_workspace(N, D);
 }
 
-cci_status cci_layer_norm_backward(const void *dy, int64_t lddy, const void *x, int64_t ldx, cci_dtype dtype,
-                                   int64_t N, int64_t D, const float *mean, const float *rstd, const float *weight,
-                                   void *dx, float *dweight, float *dbias, void *workspace, size_t workspace_bytes,
-                                   cci_stream_t stream)
+cci_status cci_layer_norm_backward_ex(const void *dy, int64_t lddy, const void *x, int64_t ldx, cci_dtype dtype,
+                                      int64_t N, int64_t D, const float *mean, const float *rstd, const float *weight,
+                                      void *dx, float *dweight, float *dbias, uint32_t *dev_status, void *workspace,
+                                      size_t workspace_bytes, cci_stream_t stream)
 {
     if (!valid_dtype(dtype)) return CCI_ERR_DTYPE;
     if (N > 0 && (!dy || !x || !mean || !rstd || !dx)) return CCI_ERR_NULL;
@@ -55,7 +63,16 @@ cci_status cci_layer_norm_backward(const void *dy, int64_t lddy, const void *x, 
     const size_t need = N > 0 ? layer_norm_workspace(N, D) : 0;
     if (need > 0 && (!workspace || !aligned(workspace, 16) || workspace_bytes < need)) return CCI_ERR_WORKSPACE;
     return to_status(launch_layer_norm_backward(dy, lddy, x, ldx, dtype, N, D, mean, rstd, weight, dx, dweight, dbias,
-                                                static_cast<float *>(workspace), as_stream(stream)));
+                                                static_cast<float *>(workspace), dev_status, as_stream(stream)));
+}
+
+cci_status cci_layer_norm_backward(const void *dy, int64_t lddy, const void *x, int64_t ldx, cci_dtype dtype,
+                                   int64_t N, int64_t D, const float *mean, const float *rstd, const float *weight,
+                                   void *dx, float *dweight, float *dbias, void *workspace, size_t workspace_bytes,
+                                   cci_stream_t stream)
+{
+    return cci_layer_norm_backward_ex(dy, lddy, x, ldx, dtype, N, D, mean, rstd, weight, dx, dweight, dbias, nullptr,
+                                      workspace, workspace_bytes, stream);
 }
 
 cci_status cci_token_logprobs(const void *logits, cci_dtype dtype, int64_t N, int64_t V, int64_t ldx,

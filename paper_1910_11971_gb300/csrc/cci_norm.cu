@@ -33,6 +33,8 @@ constexpr int kMaxStages = 6;
 
 struct Ring {
     uint64_t full[kMaxStages];
+    int64_t row[kMaxStages];  // forward: the row that each stage was copied last
+    int64_t lost;             // backward: the first row of the set at which the group's first thread stopped copying
 };
 
 // untiled bulk copy of `bytes` (a multiple of 16) to shared memory, completing on `bar`; both addresses on 16 bytes
@@ -43,6 +45,21 @@ __device__ __forceinline__ void bulk_load(void *dst, const void *src, uint32_t b
                  "l"(reinterpret_cast<uint64_t>(src)), "r"(bytes), "r"(tc::smem_u32(bar))
                  : "memory");
 }
+
+// A wait that expires sets the block's abort flag and the status word, and its rows come out as NaN.  The group's
+// first thread copies no row into a stage whose last one it did not see land, and before the block ends, or its ring
+// takes other values, waits (again with a limit) for the last copy to each stage.  Here: the last of `issued` rows,
+// which follow each other in the ring
+template <int STAGES>
+__device__ __forceinline__ void drain(Ring &ring, int64_t issued, uint32_t *status)
+{
+    int no_abort = 0;
+#pragma unroll 1
+    for (int64_t r = issued > STAGES ? issued - STAGES : 0; r < issued; ++r)
+        tc::mbar_wait(&ring.full[r % STAGES], static_cast<uint32_t>(r / STAGES) & 1u, &no_abort, status);
+}
+
+__device__ __forceinline__ float nan_f() { return __int_as_float(0x7fc00000); }
 
 // stages of a group's ring: `bytes` a stage, `groups` rings in a block, `blocks` blocks in an SM
 constexpr int stages_of(int bytes, int groups, int blocks)
@@ -210,10 +227,35 @@ struct Forward {
     static constexpr int kBytes = kBulk ? kStages * kStage * kGroups + kParams : 0;
 };
 
+// after an expired wait: NaN to all rows of the block, which cannot tell from then on whose copy was in time.  Not
+// inlined, and everything made again from the block's place: the rows' loop keeps its registers (16384 x 4096 bf16
+// 53.1 us with it inlined and the flag read for each row, 50.7 so)
+template <typename T, int V, int E, int TPR, int STAGES>
+__device__ __noinline__ void lost_rows(Ring *rings, int64_t N, int D, T *y, float *mean, float *rstd, uint32_t *status)
+{
+    constexpr int kGroups = block_threads(TPR) / TPR, kStep = Pairs<V>::kStep;
+    const int group = threadIdx.x / TPR, t = threadIdx.x % TPR;
+    const int64_t step = static_cast<int64_t>(gridDim.x) * kGroups;
+    const int64_t n0 = static_cast<int64_t>(blockIdx.x) * kGroups + group;
+    if (t == 0) {
+        Ring &ring = rings[group];
+        int no_abort = 0;
+        for (int s = 0; s < STAGES && n0 + s * step < N; ++s)
+            tc::mbar_wait(&ring.full[s], static_cast<uint32_t>((ring.row[s] - n0) / step / STAGES) & 1u, &no_abort, status);
+    }
+    Pairs<V> lost;
+#pragma unroll
+    for (int j = 0; j < Pairs<V>::kP; ++j) lost.p[j] = pack2(nan_f(), nan_f());
+    for (int64_t n = n0; n < N; n += step) {
+        for (int i = 0; i < E / V; i += kStep) store_pairs<T, V, TPR>(y + n * D, i, t, D, lost);
+        if (t == 0) mean[n] = rstd[n] = nan_f();
+    }
+}
+
 template <typename T, int V, int E, int TPR, bool KEEP>
 __global__ void __launch_bounds__(block_threads(TPR), residents(TPR, (V > 1), false))
     norm_kernel(const T *x, int64_t ldx, int64_t N, int D, const float *w, const float *b, float eps, T *y, float *mean,
-                float *rstd)
+                float *rstd, uint32_t *status)
 {
     using C = Forward<T, V, E, TPR, KEEP>;
     constexpr int kGroups = C::kGroups, kNV = E / V, kStage = C::kStage, kStages = C::kStages;
@@ -233,6 +275,7 @@ __global__ void __launch_bounds__(block_threads(TPR), residents(TPR, (V > 1), fa
     const uint32_t bytes = static_cast<uint32_t>(D) * sizeof(T);
     auto copy = [&](int64_t n, int s) {
         tc::mbar_arrive_expect_tx(&R.full[s], bytes);
+        R.row[s] = n;
         bulk_load(ring + s * kStage, x + n * ldx, bytes, &R.full[s]);
     };
     row::Raw<T, V> raw[kBulk ? 1 : kNV];
@@ -268,8 +311,9 @@ __global__ void __launch_bounds__(block_threads(TPR), residents(TPR, (V > 1), fa
         Pairs<V> f[E / 2 / kP];
         float s[1], q[1];
         unsigned long long s2 = 0ull, q2 = 0ull;
-        // a wait that expires leaves wrong results, but every thread goes on: none is left at a barrier
-        if constexpr (kBulk) tc::mbar_wait(&R.full[st], ph, abort, nullptr);
+        // after a wait that expired every thread goes on: none is left at a barrier
+        bool landed = true;
+        if constexpr (kBulk) landed = tc::mbar_wait(&R.full[st], ph, abort, status);
 #pragma unroll
         for (int i = 0; i < kNV; i += kStep) {
             f[i / kStep] = kBulk ? pairs_at<T, V, TPR, true>(reinterpret_cast<const T *>(ring + st * kStage), i, t, D)
@@ -284,7 +328,7 @@ __global__ void __launch_bounds__(block_threads(TPR), residents(TPR, (V > 1), fa
         row::group_sum<TPR>(s, buf[group][0], group, t);
         if constexpr (kBulk) {
             // every thread of the group has its part of the row
-            if (t == 0 && n + kStages * step < N) copy(n + kStages * step, st);
+            if (t == 0 && n + kStages * step < N && landed) copy(n + kStages * step, st);
             if (++st == kStages) {
                 st = 0;
                 ph ^= 1u;
@@ -331,6 +375,11 @@ __global__ void __launch_bounds__(block_threads(TPR), residents(TPR, (V > 1), fa
             }
             store_pairs<T, V, TPR>(y + n * D, i, t, D, o);
         }
+    }
+    if constexpr (kBulk) {
+        // the barriers of a row's sums lie between the flag and here; a warp's sums have none
+        if constexpr (TPR == 32) __syncwarp();
+        if (*abort) lost_rows<T, V, E, TPR, kStages>(rings, N, D, y, mean, rstd, status);
     }
 }
 
@@ -420,7 +469,7 @@ struct Backward {
 template <typename T, int V, int E, int TPR>
 __global__ void __launch_bounds__(block_threads(TPR), residents(TPR, (V > 1), true))
     norm_backward_kernel(const T *dy, int64_t lddy, const T *x, int64_t ldx, const float *mean, const float *rstd,
-                         const float *w, int64_t N, int D, T *dx, float *pw, float *pb)
+                         const float *w, int64_t N, int D, T *dx, float *pw, float *pb, uint32_t *status)
 {
     using C = Backward<T, V, E, TPR>;
     constexpr int kGroups = C::kGroups, kNV = E / V, kRow = C::kRow, kStage = C::kStage, kStages = C::kStages;
@@ -473,6 +522,7 @@ __global__ void __launch_bounds__(block_threads(TPR), residents(TPR, (V > 1), tr
         constexpr int kRows = C::kRows;
         int st = 0;
         uint32_t ph = 0u;
+        bool ok = true;
         float mu[kRows], r[kRows];  // of the next rows
         auto stats_of = [&](int64_t n) {
 #pragma unroll
@@ -497,8 +547,14 @@ __global__ void __launch_bounds__(block_threads(TPR), residents(TPR, (V > 1), tr
 #pragma unroll
             for (int q = 0; q < kRows; ++q) {
                 if (q > 0 && n + step >= N) break;
-                // a wait that expires leaves wrong results, but every thread goes on: none is left at a barrier
-                tc::mbar_wait(&R.full[st + q], ph, abort, nullptr);
+                // after a wait that expired every thread goes on, none is left at a barrier, with NaN in the row's sums
+                // and in its own columns of dw and db from then on
+                if (ok && !tc::mbar_wait(&R.full[st + q], ph, abort, status)) {
+                    ok = false;
+#pragma unroll
+                    for (int e = 0; e < E / 2; ++e) dw[e] = db[e] = pack2(nan_f(), nan_f());
+                    if (t == 0) R.lost = n;
+                }
                 const unsigned long long minus_m = pack2(-m[q], -m[q]), rn2 = pack2(rn[q], rn[q]);
                 unsigned long long s0 = 0ull, s1 = 0ull;
 #pragma unroll
@@ -511,12 +567,12 @@ __global__ void __launch_bounds__(block_threads(TPR), residents(TPR, (V > 1), tr
                         wv[0] = params2<V, TPR>(w, i, t, D, 1.f);
                     add_columns<V>(xp, gp, wv[kHold ? i / kStep : 0], minus_m, rn2, dw + i / kStep * kP, db + i / kStep * kP, s0, s1);
                 }
-                s[2 * q] = lo_of(s0) + hi_of(s0);
-                s[2 * q + 1] = lo_of(s1) + hi_of(s1);
+                s[2 * q] = ok ? lo_of(s0) + hi_of(s0) : nan_f();
+                s[2 * q + 1] = ok ? lo_of(s1) + hi_of(s1) : nan_f();
             }
             row::group_sum4<TPR>(s, buf[group][k], group, t);
             // every thread of the group has left the rows before these: their stages take the rows after these
-            if (t == 0 && n > n0) {
+            if (ok && t == 0 && n > n0) {
 #pragma unroll
                 for (int q = 0; q < kRows; ++q) {
                     const int64_t next = n + (kStages - kRows + q) * step;
@@ -545,6 +601,12 @@ __global__ void __launch_bounds__(block_threads(TPR), residents(TPR, (V > 1), tr
                                            input_gradient<V>(xp, gp, wv[kHold ? i / kStep : 0], minus_m, rn2, minus_a, minus_b));
                 }
             }
+        }
+        if (!ok && t == 0) {
+            // a set of rows brings its last stages' copies only once it is summed
+            const int64_t row = (R.lost - n0) / step, rows = (N - n0 + step - 1) / step;
+            const int64_t issued = row > 0 ? row + kStages - kRows : kStages;
+            drain<kStages>(R, issued < rows ? issued : rows, status);
         }
     } else {
         float mu = 0.f, r = 0.f;
@@ -598,7 +660,8 @@ __global__ void __launch_bounds__(block_threads(TPR), residents(TPR, (V > 1), tr
             }
         }
     }
-    // the rings are done with (all copies were waited for): the groups' sums take their place
+    // the rings are done with (every copy was waited for, after a wait that expired by drain): the groups' sums take
+    // their place
     float *comb = reinterpret_cast<float *>(ring_raw);
     const bool pw_ok = pw != nullptr, pb_ok = pb != nullptr;
     // the groups' sums, added in group order
@@ -759,6 +822,7 @@ struct Args {
     float *mean, *rstd;
     float *dw, *db, *part;
     int *parts;  // written: parts of the sums
+    uint32_t *status;
     cudaStream_t stream;
 };
 
@@ -806,7 +870,7 @@ cudaError_t forward_as(const Args &a, int64_t blocks)
     if (attr != cudaSuccess) return attr;
     norm_kernel<T, V, E, TPR, KEEP><<<static_cast<unsigned>(blocks), kT, bytes, a.stream>>>(
         static_cast<const T *>(a.x), a.ldx, a.N, static_cast<int>(a.D), a.w, a.b, a.eps, static_cast<T *>(a.y), a.mean,
-        a.rstd);
+        a.rstd, a.status);
     return cudaGetLastError();
 }
 
@@ -830,7 +894,7 @@ cudaError_t backward_one(const Args &a)
     *a.parts = static_cast<int>(backward_blocks(thread_columns<T, V>(), V > 1, a.N, a.D));
     norm_backward_kernel<T, V, E, TPR><<<static_cast<unsigned>(*a.parts), kT, bytes, a.stream>>>(
         static_cast<const T *>(a.dy), a.lddy, static_cast<const T *>(a.x), a.ldx, a.mean_in, a.rstd_in, a.w, a.N,
-        static_cast<int>(a.D), static_cast<T *>(a.y), first_dw(a), first_db(a));
+        static_cast<int>(a.D), static_cast<T *>(a.y), first_dw(a), first_db(a), a.status);
     return cudaGetLastError();
 }
 
@@ -912,7 +976,8 @@ size_t layer_norm_workspace(int64_t N, int64_t D)
 }
 
 cudaError_t launch_layer_norm(const void *x, int dtype, int64_t N, int64_t D, int64_t ldx, const float *w,
-                              const float *b, float eps, void *y, float *mean, float *rstd, cudaStream_t stream)
+                              const float *b, float eps, void *y, float *mean, float *rstd, uint32_t *status,
+                              cudaStream_t stream)
 {
     norm::Args a{};
     a.x = x;
@@ -925,13 +990,14 @@ cudaError_t launch_layer_norm(const void *x, int dtype, int64_t N, int64_t D, in
     a.y = y;
     a.mean = mean;
     a.rstd = rstd;
+    a.status = status;
     a.stream = stream;
     return dtype == CCI_F32 ? norm::forward<float>(a) : norm::forward<uint16_t>(a);
 }
 
 cudaError_t launch_layer_norm_backward(const void *dy, int64_t lddy, const void *x, int64_t ldx, int dtype, int64_t N,
                                        int64_t D, const float *mean, const float *rstd, const float *w, void *dx,
-                                       float *dw, float *db, float *part, cudaStream_t stream)
+                                       float *dw, float *db, float *part, uint32_t *status, cudaStream_t stream)
 {
     norm::Args a{};
     a.dy = dy;
@@ -949,6 +1015,7 @@ cudaError_t launch_layer_norm_backward(const void *dy, int64_t lddy, const void 
     a.db = db;
     a.part = part;
     a.parts = &parts;
+    a.status = status;
     a.stream = stream;
     if (N > 0) {
         const cudaError_t e = dtype == CCI_F32 ? norm::backward<float>(a) : norm::backward<uint16_t>(a);
