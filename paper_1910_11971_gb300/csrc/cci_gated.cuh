@@ -455,12 +455,16 @@ __global__ void __launch_bounds__(Cfg<CG, BN>::kThreads, 1)
                 }
             }
             // no copy is in flight when the block ends, also after an abort: the even CTA's barriers
-            // count those of both
-            if (rank == 0) {
-                int no_abort = 0;
+            // count those of both.  Nor is a commit: each stage's last one arrives at the `empty` of both CTAs, and
+            // that a later commit (drain) has arrived does not say that an earlier one has.  After an abort some
+            // stages are never committed: the first wait for one expires, and the others give up with it
+            int no_abort = 0;
+            if (rank == 0)
                 for (int d = it > kStages ? it - kStages : 0; d < it; ++d)
                     tc::mbar_wait(&S->full[d % kStages], (d / kStages) & 1, &no_abort, p.status);
-            }
+            no_abort = 0;
+            for (int d = it > kStages ? it - kStages : 0; d < it; ++d)
+                tc::mbar_wait(&S->empty[d % kStages], (d / kStages) & 1, &no_abort, p.status);
         }
         __syncwarp();
     } else if (warp == 1 && rank == 0) {
@@ -655,13 +659,20 @@ __global__ void __launch_bounds__(Cfg<CG, BN>::kThreads, 1)
                 acc_free();
             }
         }
-        if (m == 0) tc::bulk_wait_all();
+        if (m == 0) {
+            tc::bulk_wait_all();
+            if (!ok) {  // accumulators that may be committed all the same: this one and the next
+                int no_abort = 0;
+                for (int a = t; a < t + 2; ++a) tc::mbar_wait(&S->acc_full[a & 1], (a >> 1) & 1, &no_abort, p.status);
+            }
+        }
     }
 
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     __syncthreads();
     if constexpr (CG == 2) {
-        // the last commit signals this CTA's barrier too: it has arrived before either CTA leaves
+        // the last commit signals this CTA's barrier too: it has arrived before either CTA leaves, as those before it
+        // have, for which the copying and the output warps have waited
         if (rank != 0 && tid == 0) {
             int no_abort = 0;
             tc::mbar_wait(&S->drain, 0, &no_abort, p.status);
