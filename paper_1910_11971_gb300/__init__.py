@@ -495,10 +495,20 @@ def dense_conv2d_tc(X: torch.Tensor, Wd: torch.Tensor, Cout: int, KH: int, KW: i
 # the layers around a pruned projection
 # ---------------------------------------------------------------------------
 
-def _cuda_rows(t: torch.Tensor, name: str) -> int:
-    """Row stride of a CUDA matrix whose rows are contiguous."""
-    if not t.is_cuda:
+def _device(t: torch.Tensor, name: str) -> int:
+    """Index of the GPU that holds t, which must be the current one: a call's kernels run there."""
+    index = t.get_device()
+    if index < 0:
         raise ValueError(f"{name} must be a CUDA tensor")
+    if index != torch._C._cuda_getDevice():
+        raise ValueError(f"{name} must be on the current CUDA device")
+    return index
+
+
+def _rows(t: torch.Tensor, name: str, index: Optional[int] = None) -> int:
+    """Row stride of a matrix (on GPU `index`, where that is not known yet) whose rows are contiguous."""
+    if index is not None and t.get_device() != index:
+        raise ValueError(f"{name} must be a CUDA tensor on the call's device")
     if t.dim() != 2:
         raise ValueError(f"{name} must be a matrix")
     rows, cols = t.shape
@@ -510,11 +520,12 @@ def _cuda_rows(t: torch.Tensor, name: str) -> int:
     return ld
 
 
-def _cuda_vec(t: Optional[torch.Tensor], n: int, name: str, dtype: torch.dtype = torch.float32) -> Optional[int]:
-    """Address of a contiguous CUDA vector of n elements (None: NULL)."""
+def _vec(t: Optional[torch.Tensor], n: int, name: str, index: int, dtype: torch.dtype = torch.float32) -> Optional[int]:
+    """Address of a contiguous vector of n elements on GPU `index` (None: NULL)."""
     if t is None:
         return None
-    _cuda_contig(t, name)
+    if t.get_device() != index or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous CUDA tensor on the call's device")
     if t.dtype != dtype:
         raise TypeError(f"{name} must be {dtype}")
     if t.numel() != n:
@@ -522,22 +533,38 @@ def _cuda_vec(t: Optional[torch.Tensor], n: int, name: str, dtype: torch.dtype =
     return t.data_ptr()
 
 
+def _status_word(status: torch.Tensor, index: int) -> int:
+    """Address of a status word (``new_status``) on GPU `index`."""
+    if status.get_device() != index or status.dtype not in (torch.int32, torch.uint32) or status.numel() < 1:
+        raise ValueError("status must be a 32-bit integer CUDA tensor on the call's device")
+    return status.data_ptr()
+
+
+def _space(workspace: torch.Tensor, index: int):
+    """Address and bytes of a workspace on GPU `index`."""
+    if workspace.get_device() != index or not workspace.is_contiguous():
+        raise ValueError("workspace must be a contiguous CUDA tensor on the call's device")
+    return workspace.data_ptr(), workspace.nbytes
+
+
 def layer_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None, *,
                eps: float = 1e-5, out: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None):
     """(y, mean, rstd) of the rows of x[N][D] (``cci_layer_norm_ex``): y in x's dtype, the
     fp32 mean and 1 / sqrt(var + eps) of each row for the backward pass.  ``weight`` and ``bias``
     are fp32 [D]; x may have a row stride."""
-    ld = _cuda_rows(x, "x")
+    index = _device(x, "x")
+    ld = _rows(x, "x")
     N, D = x.shape
     if out is not None:
-        _like(out, (N, D), x.dtype, "out")
+        _like(out, (N, D), x.dtype, "out", index)
     y = out if out is not None else torch.empty((N, D), dtype=x.dtype, device=x.device)
     # small outputs are allocated one by one: views of one allocation cost the host more
     mean = torch.empty(N, dtype=torch.float32, device=x.device)
     rstd = torch.empty(N, dtype=torch.float32, device=x.device)
-    _check(lib().cci_layer_norm_ex(x.data_ptr(), _dtype_code(x), N, D, ld, _cuda_vec(weight, D, "weight"),
-                                   _cuda_vec(bias, D, "bias"), eps, y.data_ptr(), mean.data_ptr(), rstd.data_ptr(),
-                                   status.data_ptr() if status is not None else None, _stream(x.device)),
+    _check(lib().cci_layer_norm_ex(x.data_ptr(), _dtype_code(x), N, D, ld, _vec(weight, D, "weight", index),
+                                   _vec(bias, D, "bias", index), eps, y.data_ptr(), mean.data_ptr(), rstd.data_ptr(),
+                                   None if status is None else _status_word(status, index),
+                                   torch._C._cuda_getCurrentRawStream(index)),
            "cci_layer_norm")
     return y, mean, rstd
 
@@ -547,23 +574,26 @@ def layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, mean: torch.Tensor, r
                         workspace: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None):
     """(dx, dweight, dbias) of ``layer_norm`` (``cci_layer_norm_backward_ex``): dx in x's dtype,
     the parameters' gradients fp32 [D], whether or not the forward call had them."""
-    ldx, lddy = _cuda_rows(x, "x"), _cuda_rows(dy, "dy")
+    index = _device(x, "x")
+    ldx, lddy = _rows(x, "x"), _rows(dy, "dy", index)
     N, D = x.shape
     if dy.shape != x.shape or dy.dtype != x.dtype:
         raise ValueError("dy must have x's shape and dtype")
     if out is not None:
-        _like(out, (N, D), x.dtype, "out")
+        _like(out, (N, D), x.dtype, "out", index)
     dx = out if out is not None else torch.empty((N, D), dtype=x.dtype, device=x.device)
     dw = torch.empty(D, dtype=torch.float32, device=x.device)
     db = torch.empty(D, dtype=torch.float32, device=x.device)
     if workspace is None:
-        workspace = _workspace(_norm_bytes(N, D, x.device.index), x.device)
-    wp, wb = _ws(workspace)
+        workspace = _workspace(_norm_bytes(N, D, index), x.device)
+    wp, wb = (None, 0) if workspace is None else _space(workspace, index)
     _check(lib().cci_layer_norm_backward_ex(dy.data_ptr(), lddy, x.data_ptr(), ldx, _dtype_code(x), N, D,
-                                            _cuda_vec(mean, N, "mean"), _cuda_vec(rstd, N, "rstd"),
-                                            _cuda_vec(weight, D, "weight"), dx.data_ptr(), dw.data_ptr(),
-                                            db.data_ptr(), status.data_ptr() if status is not None else None, wp, wb,
-                                            _stream(x.device)), "cci_layer_norm_backward")
+                                            _vec(mean, N, "mean", index), _vec(rstd, N, "rstd", index),
+                                            _vec(weight, D, "weight", index), dx.data_ptr(), dw.data_ptr(),
+                                            db.data_ptr(),
+                                            None if status is None else _status_word(status, index),
+                                            wp, wb,
+                                            torch._C._cuda_getCurrentRawStream(index)), "cci_layer_norm_backward")
     return dx, dw, db
 
 
@@ -574,7 +604,8 @@ def token_logprobs(logits: torch.Tensor, tokens: torch.Tensor, *, top: int = 0, 
     (maximum, log of the sum of exp(x - maximum)) for the backward pass, and the ``top`` (at most 32)
     most probable tokens' log probabilities and indices, ties to the lower index (None for top = 0).
     The logits may have a row stride."""
-    ld = _cuda_rows(logits, "logits")
+    index = _device(logits, "logits")
+    ld = _rows(logits, "logits")
     N, V = logits.shape
     logp = torch.empty(N, dtype=torch.float32, device=logits.device)
     entropy = torch.empty(N, dtype=torch.float32, device=logits.device)
@@ -582,10 +613,11 @@ def token_logprobs(logits: torch.Tensor, tokens: torch.Tensor, *, top: int = 0, 
     top_logp = torch.empty((N, top), dtype=torch.float32, device=logits.device) if top else None
     top_idx = torch.empty((N, top), dtype=torch.int32, device=logits.device) if top else None
     _check(lib().cci_token_logprobs(logits.data_ptr(), _dtype_code(logits), N, V, ld,
-                                    _cuda_vec(tokens, N, "tokens", torch.int64), ignore_index, top, logp.data_ptr(),
+                                    _vec(tokens, N, "tokens", index, torch.int64), ignore_index, top, logp.data_ptr(),
                                     entropy.data_ptr(), stats.data_ptr(), top_logp.data_ptr() if top else None,
                                     top_idx.data_ptr() if top else None,
-                                    status.data_ptr() if status is not None else None, _stream(logits.device)),
+                                    None if status is None else _status_word(status, index),
+                                    torch._C._cuda_getCurrentRawStream(index)),
            "cci_token_logprobs")
     return logp, entropy, stats, top_logp, top_idx
 
@@ -599,7 +631,8 @@ def token_logprobs_backward(logits: torch.Tensor, tokens: Optional[torch.Tensor]
     of logp weighted by ``dlogp`` and of the entropy weighted by ``dentropy`` (which needs ``entropy``, as
     the forward call returned it).  Rows padded by up to 64 logits keep their stride in the result, unless
     ``out`` is given; ``out`` may be the logits."""
-    ld = _cuda_rows(logits, "logits")
+    index = _device(logits, "logits")
+    ld = _rows(logits, "logits")
     N, V = logits.shape
     if out is None:
         # a padded row's stride (rows then start on the same 16-byte words), not that of a wide matrix' slice
@@ -608,16 +641,16 @@ def token_logprobs_backward(logits: torch.Tensor, tokens: Optional[torch.Tensor]
         if ldd != V:
             out = out[:, :V]
     else:
-        ldd = _cuda_rows(out, "out")
+        ldd = _rows(out, "out", index)
         if out.shape != logits.shape or out.dtype != logits.dtype:
             raise ValueError("out must have the logits' shape and dtype")
     _check(lib().cci_token_logprobs_backward(logits.data_ptr(), _dtype_code(logits), N, V, ld,
-                                             _cuda_vec(stats, 2 * N, "stats"),
-                                             _cuda_vec(tokens, N, "tokens", torch.int64), ignore_index,
-                                             _cuda_vec(dlogp, N, "dlogp"), _cuda_vec(entropy, N, "entropy"),
-                                             _cuda_vec(dentropy, N, "dentropy"), out.data_ptr(), ldd,
-                                             status.data_ptr() if status is not None else None,
-                                             _stream(logits.device)), "cci_token_logprobs_backward")
+                                             _vec(stats, 2 * N, "stats", index),
+                                             _vec(tokens, N, "tokens", index, torch.int64), ignore_index,
+                                             _vec(dlogp, N, "dlogp", index), _vec(entropy, N, "entropy", index),
+                                             _vec(dentropy, N, "dentropy", index), out.data_ptr(), ldd,
+                                             None if status is None else _status_word(status, index),
+                                             torch._C._cuda_getCurrentRawStream(index)), "cci_token_logprobs_backward")
     return out
 
 
@@ -632,12 +665,14 @@ def gated_workspace(call: int, dtype: torch.dtype, N: int, D: int, F: int, devic
     """The workspace of a gated block's call (``GATED_FORWARD``, ``GATED_PACKED`` or ``GATED_BACKWARD``), from
     PyTorch memory: None when it needs none."""
     device = torch.device(device)
-    return _workspace(_gated_bytes(call, F32 if dtype == torch.float32 else BF16, N, D, F, device.index), device)
+    index = device.index if device.index is not None else torch.cuda.current_device()
+    return _workspace(_gated_bytes(call, F32 if dtype == torch.float32 else BF16, N, D, F, index), device)
 
 
 @functools.lru_cache(maxsize=4096)
-def _gated_bytes(call: int, dtype: int, N: int, D: int, F: int, device_index: Optional[int]) -> int:
-    return int(lib().cci_gated_workspace_size(call, dtype, N, D, F))
+def _gated_bytes(call: int, dtype: int, N: int, D: int, F: int, device_index: int) -> int:
+    with torch.cuda.device(device_index):  # some sizes depend on the device's SMs
+        return int(lib().cci_gated_workspace_size(call, dtype, N, D, F))
 
 
 def gated_linear(X: torch.Tensor, Wg: torch.Tensor, Wu: torch.Tensor, *, act: str = "silu", save: bool = False,
@@ -647,23 +682,26 @@ def gated_linear(X: torch.Tensor, Wg: torch.Tensor, Wu: torch.Tensor, *, act: st
     feed-forward block, the activation (a key of ``ACTIVATIONS``) and the product in one kernel.
     X [N][D], Wg and Wu dense [F][D]; D and F multiples of 8.  ``save``: returns (H, g, u) with the fp32
     pre-activations for ``gated_linear_backward``."""
-    _cuda_contig(X, "X")
+    index = _device(X, "X")
+    if not X.is_contiguous():
+        raise ValueError("X must be contiguous")
     N, D = X.shape
     F = Wg.shape[0]
-    _like(Wg, (F, D), X.dtype, "Wg")
-    _like(Wu, (F, D), X.dtype, "Wu")
+    _like(Wg, (F, D), X.dtype, "Wg", index)
+    _like(Wu, (F, D), X.dtype, "Wu", index)
     code = _dtype_code(X)
     if out is not None:
-        _like(out, (N, F), X.dtype, "out")
+        _like(out, (N, F), X.dtype, "out", index)
     H = out if out is not None else torch.empty((N, F), dtype=X.dtype, device=X.device)
     g = torch.empty((N, F), dtype=torch.float32, device=X.device) if save else None
     u = torch.empty((N, F), dtype=torch.float32, device=X.device) if save else None
     if workspace is None:
-        workspace = _workspace(_gated_bytes(GATED_FORWARD, code, N, D, F, X.device.index), X.device)
-    wp, wb = _ws(workspace)
+        workspace = _workspace(_gated_bytes(GATED_FORWARD, code, N, D, F, index), X.device)
+    wp, wb = (None, 0) if workspace is None else _space(workspace, index)
     _check(lib().cci_gated_linear(X.data_ptr(), code, N, D, Wg.data_ptr(), Wu.data_ptr(), F, _act_code(act),
                                   H.data_ptr(), g.data_ptr() if save else None, u.data_ptr() if save else None,
-                                  status.data_ptr() if status is not None else None, wp, wb, _stream(X.device)),
+                                  None if status is None else _status_word(status, index),
+                                  wp, wb, torch._C._cuda_getCurrentRawStream(index)),
            "cci_gated_linear")
     return (H, g, u) if save else H
 
@@ -674,24 +712,26 @@ def gated_linear_packed(X: torch.Tensor, gate: Tuple[torch.Tensor, torch.Tensor]
                         workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
     """``gated_linear`` with packed weights: ``gate`` and ``up`` are the (values, idx) pairs of ``pack``
     for [F][D] weights, both with (G, K) (``cci_gated_linear_packed``)."""
-    _cuda_contig(X, "X")
+    index = _device(X, "X")
+    if not X.is_contiguous():
+        raise ValueError("X must be contiguous")
     N, D = X.shape
     if G < 1 or F % G:
         raise CCIError(3, "gated_linear_packed")
     for (v, i), name in ((gate, "gate"), (up, "up")):
-        _like(v, (F // G, D, K), X.dtype, name + " values")
-        _like(i, (F // G, D, K), torch.uint8, name + " idx")
+        _like(v, (F // G, D, K), X.dtype, name + " values", index)
+        _like(i, (F // G, D, K), torch.uint8, name + " idx", index)
     code = _dtype_code(X)
     if out is not None:
-        _like(out, (N, F), X.dtype, "out")
+        _like(out, (N, F), X.dtype, "out", index)
     H = out if out is not None else torch.empty((N, F), dtype=X.dtype, device=X.device)
     if workspace is None:
-        workspace = _workspace(_gated_bytes(GATED_PACKED, code, N, D, F, X.device.index), X.device)
-    wp, wb = _ws(workspace)
+        workspace = _workspace(_gated_bytes(GATED_PACKED, code, N, D, F, index), X.device)
+    wp, wb = (None, 0) if workspace is None else _space(workspace, index)
     _check(lib().cci_gated_linear_packed(X.data_ptr(), code, N, D, gate[0].data_ptr(), gate[1].data_ptr(),
                                          up[0].data_ptr(), up[1].data_ptr(), F, G, K, _act_code(act), H.data_ptr(),
-                                         status.data_ptr() if status is not None else None, wp, wb,
-                                         _stream(X.device)), "cci_gated_linear_packed")
+                                         None if status is None else _status_word(status, index), wp, wb,
+                                         torch._C._cuda_getCurrentRawStream(index)), "cci_gated_linear_packed")
     return H
 
 
@@ -700,38 +740,42 @@ def gated_linear_backward(dH: torch.Tensor, X: torch.Tensor, Wg: torch.Tensor, W
                           status: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None):
     """(dX, dWg, dWu) of ``gated_linear`` (``cci_gated_linear_backward``) from the gradient of H and the saved
     g and u, each in X's dtype; None for those not asked for (``need_dx``, ``need_dw``)."""
-    _cuda_contig(X, "X")
+    index = _device(X, "X")
+    if not X.is_contiguous():
+        raise ValueError("X must be contiguous")
     N, D = X.shape
     F = Wg.shape[0]
-    _like(dH, (N, F), X.dtype, "dH")
-    _like(Wg, (F, D), X.dtype, "Wg")
-    _like(Wu, (F, D), X.dtype, "Wu")
-    _like(g, (N, F), torch.float32, "g")
-    _like(u, (N, F), torch.float32, "u")
+    _like(dH, (N, F), X.dtype, "dH", index)
+    _like(Wg, (F, D), X.dtype, "Wg", index)
+    _like(Wu, (F, D), X.dtype, "Wu", index)
+    _like(g, (N, F), torch.float32, "g", index)
+    _like(u, (N, F), torch.float32, "u", index)
     code = _dtype_code(X)
     dX = torch.empty_like(X) if need_dx else None
     dWg, dWu = (torch.empty_like(Wg), torch.empty_like(Wu)) if need_dw else (None, None)
     if workspace is None:
-        workspace = _workspace(_gated_bytes(GATED_BACKWARD, code, N, D, F, X.device.index), X.device)
-    wp, wb = _ws(workspace)
+        workspace = _workspace(_gated_bytes(GATED_BACKWARD, code, N, D, F, index), X.device)
+    wp, wb = (None, 0) if workspace is None else _space(workspace, index)
     _check(lib().cci_gated_linear_backward(dH.data_ptr(), X.data_ptr(), code, N, D, Wg.data_ptr(), Wu.data_ptr(), F,
                                            _act_code(act), g.data_ptr(), u.data_ptr(),
                                            dX.data_ptr() if need_dx else None, dWg.data_ptr() if need_dw else None,
                                            dWu.data_ptr() if need_dw else None,
-                                           status.data_ptr() if status is not None else None, wp, wb,
-                                           _stream(X.device)), "cci_gated_linear_backward")
+                                           None if status is None else _status_word(status, index), wp, wb,
+                                           torch._C._cuda_getCurrentRawStream(index)), "cci_gated_linear_backward")
     return dX, dWg, dWu
 
 
-def _like(t: torch.Tensor, shape, dtype: torch.dtype, name: str) -> None:
-    _cuda_contig(t, name)
+def _like(t: torch.Tensor, shape, dtype: torch.dtype, name: str, index: int) -> None:
+    if t.get_device() != index or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous CUDA tensor on the call's device")
     if tuple(t.shape) != tuple(shape) or t.dtype != dtype:
         raise ValueError(f"{name} must be {tuple(shape)} of {dtype}")
 
 
 @functools.lru_cache(maxsize=4096)
 def _norm_bytes(N: int, D: int, device_index: int) -> int:
-    return int(lib().cci_layer_norm_workspace_size(N, D))
+    with torch.cuda.device(device_index):
+        return int(lib().cci_layer_norm_workspace_size(N, D))
 
 
 def kernel_name(dtype: torch.dtype, Cin: int, R: int, Cout: int, G: int, K: int,
