@@ -11,7 +11,8 @@
 // pass keeps the running maximum m, s and t = sum e_v (x_v - m) per thread and rescales them when the
 // maximum moves, in base 2: y = (x - m) log2(e).  The difference comes first: it is exact or
 // nearly so near the maximum whatever the logits' offset, and x log2(e) would overflow for logits
-// at the type's lowest value.
+// at the type's lowest value.  What is subtracted is never below a logit, so no exponential is above 1 and every term
+// of t is at most 0: nothing cancels, s of a row is at least 1, its logarithm and the entropy at least 0.
 //
 // Top alternatives: the pass notes the maximum of every run of 512 consecutive logits (32 to 128 in rows of
 // up to 16384), which costs it one warp reduction.  Of the runs, ordered by maximum and then position,
@@ -119,14 +120,14 @@ __device__ __forceinline__ float max_nan(float a, float b)
     return r;
 }
 
-// a thread's running sums in four independent parts, two of each pair, against a reference m that is not its
-// maximum but within kSlack of it from below: moving the sums at every new maximum costs a warp, whose
-// lanes take turns, more than the elements do
+// a thread's running sums in four independent parts, two of each pair, against a reference m that is at least its
+// maximum: that of all that its warp has seen (rows in one warp's registers: its own), so that the lanes move
+// their sums together, and seldom (a row of 131072 logits over four warps: about five times).  Moved at every maximum
+// of its own, a lane would hold up its warp in nearly every iteration
 struct Running {
     float m;
     unsigned long long s[2], t[2];
 };
-constexpr float kSlack = 40.f;  // e^40 times 2^24 elements stays in fp32
 
 __device__ __forceinline__ Sums sums_of(const Running &a)
 {
@@ -137,7 +138,7 @@ __device__ __forceinline__ Sums sums_of(const Running &a)
 // the sums ready for elements of up to `top`
 __device__ __forceinline__ void raise_to(Running &a, float top)
 {
-    if (top > a.m + kSlack) {
+    if (top > a.m) {
         const Sums s = moved(sums_of(a), top);
         a = Running{top, {pack2(s.s, 0.f), 0ull}, {pack2(s.t, 0.f), 0ull}};
     }
@@ -150,7 +151,7 @@ __device__ __forceinline__ float floor_of(float m)
     return ref_of(m) - fmaxf(140.f, fabsf(ref_of(m)) * 0.03f);
 }
 
-// adds n elements of at most a.m + kSlack to the sums.  CLAMPED: none is below floor_of(a.m), which is finite
+// adds n elements of at most a.m to the sums.  CLAMPED: none is below floor_of(a.m), which is finite
 template <bool CLAMPED, int n>
 __device__ __forceinline__ void add(Running &a, const float (&x)[n])
 {
@@ -176,6 +177,14 @@ __device__ __forceinline__ void add1(Running &a, float x)
 }
 
 using row::warp_max;
+
+// the lanes' largest (no NaN among them), in one instruction
+__device__ __forceinline__ float lanes_max(float v)
+{
+    float r;
+    asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(v));
+    return r;
+}
 
 struct Row {
     const int64_t *tokens;
@@ -430,7 +439,6 @@ __global__ void __launch_bounds__(kThreads, kThreads == 32 ? 28 : 1024 / kThread
     }
     if (parts > 1) cg::this_cluster().barrier_arrive();  // the wait for it: every block of the cluster runs
     Running a{neg_inf(), {0ull, 0ull}, {0ull, 0ull}};
-    float most = neg_inf();  // the thread's maximum
     row::Raw<T, kV> raw[kU];
     const T *next = xw + static_cast<int64_t>(ws + lane) * kV;  // this lane's words of the iteration to load
 #pragma unroll
@@ -462,19 +470,17 @@ __global__ void __launch_bounds__(kThreads, kThreads == 32 ? 28 : 1024 / kThread
                 if (lane % kGroup == 0) own[((w - ws) + u * 32 + lane) / kRunWords] = q;
             }
         }
+        top = lanes_max(top);
         if constexpr (TOP && RUN == 512) {
             uint32_t q = order_of(top);
-            // a vote, so that the rare look at loads without a larger number is a branch
-            if (__any_sync(0xffffffffu, !(top > neg_inf()))) {
+            if (!(top > neg_inf())) {  // the rare look at loads without a larger number
                 bool any = false;
 #pragma unroll
                 for (int u = 0; u < kU; ++u) any |= (FULL || w + u * 32 + lane < we) && has_number<T, kV>(raw[u]);
-                q = any ? q : 0u;
+                q = __any_sync(0xffffffffu, any) ? q : 0u;
             }
-            q = __reduce_max_sync(0xffffffffu, q);
             if (lane == 0) own[(w - ws) / kIter] = q;
         }
-        most = fmaxf(most, top);
         raise_to(a, top);
         // bf16: two elements at a time are raised to a floor, instead of one exponent at a time
         bool clamped = false;
@@ -512,11 +518,10 @@ __global__ void __launch_bounds__(kThreads, kThreads == 32 ? 28 : 1024 / kThread
             edge_at = tail0 + lane - kV;
         if (edge_at >= 0) edge = row::to_f32(xr[edge_at]);
         add1(a, edge);
-        most = fmaxf(most, edge);
     }
 
     // the block's sums, to every thread of its first warp
-    Sums sum = moved(warp_joined(sums_of(a)), warp_max(most));
+    Sums sum = warp_joined(sums_of(a));
     if (lane == 0) sh.warp[warp] = sum;
     // each warp's first k runs, where its lanes hold two at most
     const bool few = run_slots <= 64;
