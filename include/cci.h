@@ -554,7 +554,11 @@ cci_status cci_token_logprobs_backward(const void *logits, cci_dtype dtype, int6
  * of planes down to 2^-18 of the whole (what is left out is below 2^-25 |x||w| a term; an
  * infinite input gives NaN where its products of planes do).  Calls of up to 16 tokens may
  * stream the weights as they are (fp32: fused multiply-adds), with the sums in another order, so
- * a token's last bits may differ from those it has in a call of more tokens.
+ * a token's last bits may differ from those it has in a call of more tokens.  The activations
+ * take the fast exponential and quotient, in fp32 too: act(g) is within n units of 2^-23 of
+ * itself, n = 6 + 2.7 |g| for SiLU and sigmoid, 10 + g^2 for GELU at g < 0 (where the rounding of
+ * g itself is worth g^2 / 2) and 10 above, 6 + 2.7 z for the tanh form with z = 1.6 |g + 0.045 g^3|;
+ * values below 2^-100 may be 0.
  *
  *   X          device [N][D] of dtype
  *   Wg, Wu     device [F][D] of dtype (pruned weights: their dense form, as cci_td_mask
