@@ -142,10 +142,10 @@ __device__ __forceinline__ float slope_of(float g, float &a)
         return g > 0.f ? 1.f : 0.f;
     }
     if constexpr (ACT == CCI_ACT_GELU_TANH) {
-        // 0.5 (1 + tanh(z)) = sigmoid(2 z)
-        const float g2 = g * g, p = sigmoid(1.5957691f * (g + 0.044715f * g2 * g));
+        // 0.5 (1 + tanh(z)) = sigmoid(2 z).  Past 16 the second term is 0, which an infinite g^2 must not meet
+        const float g2 = g * g, p = sigmoid(1.5957691f * (g + 0.044715f * g2 * g)), c = fminf(fmaxf(g, -16.f), 16.f);
         a = g * p;
-        return p + g * p * (1.f - p) * 1.5957691f * (1.f + 3.f * 0.044715f * g2);
+        return p + c * p * (1.f - p) * 1.5957691f * (1.f + 3.f * 0.044715f * c * c);
     }
     const float p = sigmoid(g);
     if constexpr (ACT == CCI_ACT_SILU) {
