@@ -458,16 +458,9 @@ cci_status cci_linear_dense_tc_static(const void *X, cci_dtype dtype, int64_t N,
  * N = 0 is valid and enqueues nothing.  eps must be >= 0 (CCI_ERR_VALUE; NaN too).
  * Errors: CCI_ERR_NULL, CCI_ERR_SHAPE (D < 1, ldx < D), CCI_ERR_DTYPE,
  *         CCI_ERR_ALIGN, CCI_ERR_VALUE, CCI_ERR_CUDA.
- *
- * cci_layer_norm_ex takes a status word too (CCI_ERR_TIMEOUT: the kernel's copies of the
- * rows are waited for with a limit).  With or without one, after an expired wait the rows
- * of its block come out as NaN (y, mean and rstd).
  */
 cci_status cci_layer_norm(const void *x, cci_dtype dtype, int64_t N, int64_t D, int64_t ldx, const float *weight,
                           const float *bias, float eps, void *y, float *mean, float *rstd, cci_stream_t stream);
-cci_status cci_layer_norm_ex(const void *x, cci_dtype dtype, int64_t N, int64_t D, int64_t ldx, const float *weight,
-                             const float *bias, float eps, void *y, float *mean, float *rstd, uint32_t *dev_status,
-                             cci_stream_t stream);
 
 /*
  * cci_layer_norm_backward -- the gradients of cci_layer_norm, with g = dy * weight and
@@ -484,8 +477,9 @@ cci_status cci_layer_norm_ex(const void *x, cci_dtype dtype, int64_t N, int64_t 
  *   workspace  device, 16-byte aligned, cci_layer_norm_workspace_size(N, D) bytes (which
  *              depends on the current device's number of SMs); overwritten
  * Errors: as cci_layer_norm; CCI_ERR_WORKSPACE.
- * cci_layer_norm_backward_ex takes a status word too, as cci_layer_norm_ex; after an expired
- * wait the rows of dx and the columns of dweight and dbias that it touches are NaN.
+ * cci_layer_norm_backward_ex takes a status word too (CCI_ERR_TIMEOUT: the kernel's copies of
+ * the rows are waited for with a limit).  With or without one, after an expired wait the rows
+ * of dx and the columns of dweight and dbias that it touches are NaN.
  */
 size_t cci_layer_norm_workspace_size(int64_t N, int64_t D);
 cci_status cci_layer_norm_backward(const void *dy, int64_t lddy, const void *x, int64_t ldx, cci_dtype dtype,

@@ -71,7 +71,6 @@ SIGNATURES = {
     "cci_dense_conv2d_tc": (_I32, [_P, _I32, _I64, _I64, _I64, _I64, _P, _I64, _I32, _I32, _I32, _I32,
                                    _I32, _I32, _P, _U32P, _P]),
     "cci_layer_norm": (_I32, [_P, _I32, _I64, _I64, _I64, _P, _P, ctypes.c_float, _P, _P, _P, _P]),
-    "cci_layer_norm_ex": (_I32, [_P, _I32, _I64, _I64, _I64, _P, _P, ctypes.c_float, _P, _P, _P, _U32P, _P]),
     "cci_layer_norm_workspace_size": (ctypes.c_size_t, [_I64, _I64]),
     "cci_layer_norm_backward": (_I32, [_P, _I64, _P, _I64, _I32, _I64, _I64, _P, _P, _P, _P, _P, _P, _P,
                                        ctypes.c_size_t, _P]),
@@ -548,8 +547,8 @@ def _space(workspace: torch.Tensor, index: int):
 
 
 def layer_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None, *,
-               eps: float = 1e-5, out: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None):
-    """(y, mean, rstd) of the rows of x[N][D] (``cci_layer_norm_ex``): y in x's dtype, the
+               eps: float = 1e-5, out: Optional[torch.Tensor] = None):
+    """(y, mean, rstd) of the rows of x[N][D] (``cci_layer_norm``): y in x's dtype, the
     fp32 mean and 1 / sqrt(var + eps) of each row for the backward pass.  ``weight`` and ``bias``
     are fp32 [D]; x may have a row stride."""
     index = _device(x, "x")
@@ -561,11 +560,9 @@ def layer_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Opt
     # small outputs are allocated one by one: views of one allocation cost the host more
     mean = torch.empty(N, dtype=torch.float32, device=x.device)
     rstd = torch.empty(N, dtype=torch.float32, device=x.device)
-    _check(lib().cci_layer_norm_ex(x.data_ptr(), _dtype_code(x), N, D, ld, _vec(weight, D, "weight", index),
-                                   _vec(bias, D, "bias", index), eps, y.data_ptr(), mean.data_ptr(), rstd.data_ptr(),
-                                   None if status is None else _status_word(status, index),
-                                   torch._C._cuda_getCurrentRawStream(index)),
-           "cci_layer_norm")
+    _check(lib().cci_layer_norm(x.data_ptr(), _dtype_code(x), N, D, ld, _vec(weight, D, "weight", index),
+                                _vec(bias, D, "bias", index), eps, y.data_ptr(), mean.data_ptr(), rstd.data_ptr(),
+                                torch._C._cuda_getCurrentRawStream(index)), "cci_layer_norm")
     return y, mean, rstd
 
 

@@ -20,9 +20,8 @@ bool rows_ok(int64_t N, int64_t D, int64_t ld) { return N >= 0 && D >= 1 && ld >
 
 extern "C" {
 
-cci_status cci_layer_norm_ex(const void *x, cci_dtype dtype, int64_t N, int64_t D, int64_t ldx, const float *weight,
-                             const float *bias, float eps, void *y, float *mean, float *rstd, uint32_t *dev_status,
-                             cci_stream_t stream)
+cci_status cci_layer_norm(const void *x, cci_dtype dtype, int64_t N, int64_t D, int64_t ldx, const float *weight,
+                          const float *bias, float eps, void *y, float *mean, float *rstd, cci_stream_t stream)
 {
     if (!valid_dtype(dtype)) return CCI_ERR_DTYPE;
     if (N > 0 && (!x || !y || !mean || !rstd)) return CCI_ERR_NULL;
@@ -33,14 +32,7 @@ cci_status cci_layer_norm_ex(const void *x, cci_dtype dtype, int64_t N, int64_t 
         !aligned(rstd, 4))
         return CCI_ERR_ALIGN;
     if (N == 0) return CCI_OK;
-    return to_status(launch_layer_norm(x, dtype, N, D, ldx, weight, bias, eps, y, mean, rstd, dev_status,
-                                       as_stream(stream)));
-}
-
-cci_status cci_layer_norm(const void *x, cci_dtype dtype, int64_t N, int64_t D, int64_t ldx, const float *weight,
-                          const float *bias, float eps, void *y, float *mean, float *rstd, cci_stream_t stream)
-{
-    return cci_layer_norm_ex(x, dtype, N, D, ldx, weight, bias, eps, y, mean, rstd, nullptr, stream);
+    return to_status(launch_layer_norm(x, dtype, N, D, ldx, weight, bias, eps, y, mean, rstd, as_stream(stream)));
 }
 
 size_t cci_layer_norm_workspace_size(int64_t N, int64_t D)

@@ -58,8 +58,7 @@ cudaError_t launch_gemm_pk(const FwdParams &p, cudaStream_t stream);
 // of layer_norm_workspace bytes (N >= 1), which the sums of dw and db need
 size_t layer_norm_workspace(int64_t N, int64_t D);
 cudaError_t launch_layer_norm(const void *x, int dtype, int64_t N, int64_t D, int64_t ldx, const float *w,
-                              const float *b, float eps, void *y, float *mean, float *rstd, uint32_t *status,
-                              cudaStream_t stream);
+                              const float *b, float eps, void *y, float *mean, float *rstd, cudaStream_t stream);
 cudaError_t launch_layer_norm_backward(const void *dy, int64_t lddy, const void *x, int64_t ldx, int dtype, int64_t N,
                                        int64_t D, const float *mean, const float *rstd, const float *w, void *dx,
                                        float *dw, float *db, float *part, uint32_t *status, cudaStream_t stream);

@@ -6,8 +6,9 @@
 //
 // Memory bound in both directions (two or three row reads and writes, a dozen operations an
 // element).  A row of up to 16384 columns belongs to a group of 32 to 1024 threads and is read
-// from memory once: by bulk copies into shared memory where it lies on whole 16-byte words, else into
-// registers.  The variance is the mean square of the differences from the mean, not a difference
+// from memory once: forward into registers, the next row while this one is reduced; backward by bulk copies into
+// shared memory where it lies on whole 16-byte words, else likewise.  The variance is the mean square of the
+// differences from the mean, not a difference
 // of sums.  The backward pass takes its sums and then dx from shared memory, and keeps each
 // thread's columns of dw and db in registers over all rows of its block; the blocks' sums go to the
 // workspace and a second launch adds them in block order (a single block's go straight to dw and
@@ -25,16 +26,16 @@ constexpr int block_threads(int TPR) { return TPR < 256 ? 256 : TPR; }
 // blocks of an SM that the registers leave room for
 constexpr int residents(int TPR, bool words, bool backward) { return TPR <= 256 ? (words && !backward ? 3 : 2) : 1; }
 
-// Rows on whole 16-byte words come by bulk copies into a ring of rows per group, as many ahead as shared
+// Backward, rows on whole 16-byte words come by bulk copies into a ring of rows per group, as many ahead as shared
 // memory holds; the copies of a row are counted in bytes on its stage's barrier.  Loads into registers, which
-// other rows take, keep less on its way (16384 x 4096 bf16: 50 us forward and 102 backward, now 48 and
-// 78).
+// other rows take, keep less of two wide rows on its way (bf16 16384 x 4096: 76 us, 71 so, 4000 x 16384 136 and 105;
+// narrow rows lose, 60000 x 256 29 and 33).  Forward, with one row and no sums to keep, they are as good or better
+// (bf16 16384 x 4096 50.8 us by copies, 48.8 so, 16000 x 2048 30.0 and 26.4, 8000 x 8192 81 and 73) and wait for nothing
 constexpr int kMaxStages = 6;
 
 struct Ring {
     uint64_t full[kMaxStages];
-    int64_t row[kMaxStages];  // forward: the row that each stage was copied last
-    int64_t lost;             // backward: the first row of the set at which the group's first thread stopped copying
+    int64_t lost;  // after an expired wait: the first row of the set at which the group's first thread stopped copying
 };
 
 // untiled bulk copy of `bytes` (a multiple of 16) to shared memory, completing on `bar`; both addresses on 16 bytes
@@ -48,13 +49,20 @@ __device__ __forceinline__ void bulk_load(void *dst, const void *src, uint32_t b
 
 // A wait that expires sets the block's abort flag and the status word, and its rows come out as NaN.  The group's
 // first thread copies no row into a stage whose last one it did not see land, and before the block ends, or its ring
-// takes other values, waits (again with a limit) for the last copy to each stage.  Here: the last of `issued` rows,
-// which follow each other in the ring
-template <int STAGES>
-__device__ __forceinline__ void drain(Ring &ring, int64_t issued, uint32_t *status)
+// takes other values, waits (again with a limit) for the last copy to each stage.  Not inlined, and everything made again
+// from the block's place: the rows' loop keeps its registers (4000 x 12288 bf16: 97.5 us inlined, 90.5 so)
+template <int STAGES, int ROWS, int TPR>
+__device__ __noinline__ void drain(Ring *rings, int64_t N, uint32_t *status)
 {
+    constexpr int kGroups = block_threads(TPR) / TPR;
+    const int group = threadIdx.x / TPR;
+    const int64_t step = static_cast<int64_t>(gridDim.x) * kGroups, n0 = static_cast<int64_t>(blockIdx.x) * kGroups + group;
+    Ring &ring = rings[group];
+    // a set of ROWS rows brings its last stages' copies only once it is summed
+    const int64_t row = (ring.lost - n0) / step, rows = (N - n0 + step - 1) / step;
+    int64_t issued = row > 0 ? row + STAGES - ROWS : STAGES;
+    if (issued > rows) issued = rows;
     int no_abort = 0;
-#pragma unroll 1
     for (int64_t r = issued > STAGES ? issued - STAGES : 0; r < issued; ++r)
         tc::mbar_wait(&ring.full[r % STAGES], static_cast<uint32_t>(r / STAGES) & 1u, &no_abort, status);
 }
@@ -68,11 +76,11 @@ constexpr int stages_of(int bytes, int groups, int blocks)
     return fit < kMaxStages ? fit : kMaxStages;
 }
 
-// Parameters of wide rows, which no registers are left for, lie in shared memory beside the ring where that keeps
-// two stages or more: bytes of them, and the ring's stages then.  From L2 they are 8 bytes an element again for every
-// row (forward bf16 8000 x 8192 95 us, 81 so; fp32 16384 x 4096 165 and 123; backward bf16 4000 x 16384 151 and 106).  Not
-// where a block has few rows (forward bf16 100 x 8192: 3.8 us, 4.5 with them), nor in the backward pass of fp32 rows
-// (8000 x 8192: 136 us, 145 with it)
+// Parameters of wide rows, which no registers are left for, lie in shared memory; backward beside the ring, where that
+// keeps two stages or more: bytes of them, and the ring's stages then.  From L2 they are 8 bytes an element again for
+// every row (forward bf16 8000 x 8192 78.8 us, 73.3 so; fp32 16384 x 4096 126 and 121; backward bf16 4000 x 16384 184 and
+// 105).  Not where a block has few rows (forward bf16 100 x 8192: 3.6 us, 4.2 with them), nor in the backward pass of
+// fp32 rows (8000 x 8192: 136 us, 145 with it)
 constexpr int kWideBudget = 224 * 1024;
 constexpr int shared_params(int bytes, int stage) { return (kWideBudget - bytes) / stage >= 2 ? bytes : 0; }
 constexpr int stages_beside(int params, int stage)
@@ -214,87 +222,32 @@ __device__ __forceinline__ void store_pairs(T *y, int i, int t, int D, const Pai
     }
 }
 
-// ---- forward: E columns per thread, in vectors of V.  Groups walk the rows; the next rows are on their way while
-// one is reduced.  Rows of up to 4096 keep weight and bias in registers ----
-// its shared memory: the ring, then weight and bias (KEEP: where that can be)
-template <typename T, int V, int E, int TPR, bool KEEP>
-struct Forward {
-    static constexpr int kGroups = block_threads(TPR) / TPR;
-    static constexpr bool kHold = TPR <= 256, kBulk = V > 1;
-    static constexpr int kStage = E * TPR * static_cast<int>(sizeof(T));
-    static constexpr int kParams = KEEP && kBulk && !kHold ? shared_params(2 * E * TPR * 4, kStage) : 0;
-    static constexpr int kStages = kParams ? stages_beside(kParams, kStage) : stages_of(kStage, kGroups, residents(TPR, (V > 1), false));
-    static constexpr int kBytes = kBulk ? kStages * kStage * kGroups + kParams : 0;
-};
-
-// after an expired wait: NaN to all rows of the block, which cannot tell from then on whose copy was in time.  Not
-// inlined, and everything made again from the block's place: the rows' loop keeps its registers (16384 x 4096 bf16
-// 53.1 us with it inlined and the flag read for each row, 50.7 so)
-template <typename T, int V, int E, int TPR, int STAGES>
-__device__ __noinline__ void lost_rows(Ring *rings, int64_t N, int D, T *y, float *mean, float *rstd, uint32_t *status)
-{
-    constexpr int kGroups = block_threads(TPR) / TPR, kStep = Pairs<V>::kStep;
-    const int group = threadIdx.x / TPR, t = threadIdx.x % TPR;
-    const int64_t step = static_cast<int64_t>(gridDim.x) * kGroups;
-    const int64_t n0 = static_cast<int64_t>(blockIdx.x) * kGroups + group;
-    if (t == 0) {
-        Ring &ring = rings[group];
-        int no_abort = 0;
-        for (int s = 0; s < STAGES && n0 + s * step < N; ++s)
-            tc::mbar_wait(&ring.full[s], static_cast<uint32_t>((ring.row[s] - n0) / step / STAGES) & 1u, &no_abort, status);
-    }
-    Pairs<V> lost;
-#pragma unroll
-    for (int j = 0; j < Pairs<V>::kP; ++j) lost.p[j] = pack2(nan_f(), nan_f());
-    for (int64_t n = n0; n < N; n += step) {
-        for (int i = 0; i < E / V; i += kStep) store_pairs<T, V, TPR>(y + n * D, i, t, D, lost);
-        if (t == 0) mean[n] = rstd[n] = nan_f();
-    }
-}
+// ---- forward: E columns per thread, in vectors of V.  Groups walk the rows; the next row is on its way while
+// one is reduced.  Groups of up to 256 threads keep weight and bias in registers: bf16 rows of whole words up to 4096
+// columns, others up to 2048 ----
+// bytes of shared memory: weight and bias, where they are kept there (KEEP: rows enough for it)
+template <int V, int E, int TPR, bool KEEP>
+constexpr int kForwardBytes = KEEP && V > 1 && TPR > 256 ? 2 * E * TPR * static_cast<int>(sizeof(float)) : 0;
 
 template <typename T, int V, int E, int TPR, bool KEEP>
 __global__ void __launch_bounds__(block_threads(TPR), residents(TPR, (V > 1), false))
     norm_kernel(const T *x, int64_t ldx, int64_t N, int D, const float *w, const float *b, float eps, T *y, float *mean,
-                float *rstd, uint32_t *status)
+                float *rstd)
 {
-    using C = Forward<T, V, E, TPR, KEEP>;
-    constexpr int kGroups = C::kGroups, kNV = E / V, kStage = C::kStage, kStages = C::kStages;
-    constexpr bool kHold = C::kHold, kBulk = C::kBulk, kKept = C::kParams > 0;
-    extern __shared__ __align__(128) unsigned char ring_raw[];
-    __shared__ Ring rings[kGroups];
+    constexpr int kGroups = block_threads(TPR) / TPR, kNV = E / V;
+    constexpr bool kHold = TPR <= 256, kKept = kForwardBytes<V, E, TPR, KEEP> > 0;
+    extern __shared__ __align__(16) float kept[];  // weight, then bias
     __shared__ float buf[kGroups][2][TPR / 32];
-    __shared__ int abort_flag;
     const int group = threadIdx.x / TPR, t = threadIdx.x % TPR;
     const float width = static_cast<float>(D);
     const int64_t step = static_cast<int64_t>(gridDim.x) * kGroups;
     const int64_t n0 = static_cast<int64_t>(blockIdx.x) * kGroups + group;
-    unsigned char *ring = ring_raw + group * kStages * kStage;
-    float *kept = reinterpret_cast<float *>(ring_raw + kStages * kStage);  // with one group
-    Ring &R = rings[group];
-    volatile int *abort = &abort_flag;
-    const uint32_t bytes = static_cast<uint32_t>(D) * sizeof(T);
-    auto copy = [&](int64_t n, int s) {
-        tc::mbar_arrive_expect_tx(&R.full[s], bytes);
-        R.row[s] = n;
-        bulk_load(ring + s * kStage, x + n * ldx, bytes, &R.full[s]);
-    };
-    row::Raw<T, V> raw[kBulk ? 1 : kNV];
-    if constexpr (kBulk) {
-        if (threadIdx.x == 0) abort_flag = 0;
-        zero_tails<T, V, E, TPR>(ring, kStages, t, D);
-        if constexpr (kKept) {
-            keep_params<V, E, TPR>(kept, w, t, D, 1.f);
-            keep_params<V, E, TPR>(kept + E * TPR, b, t, D, 0.f);
-        }
-        if (t == 0) {
-            for (int s = 0; s < kStages; ++s) tc::mbar_init(&R.full[s], 1);
-            asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-            for (int s = 0; s < kStages; ++s)
-                if (n0 + s * step < N) copy(n0 + s * step, s);
-        }
+    row::Raw<T, V> raw[kNV];
+    if (n0 < N) load_row<T, V, kNV, TPR>(raw, x + n0 * ldx, t, D);
+    if constexpr (kKept) {
+        keep_params<V, E, TPR>(kept, w, t, D, 1.f);
+        keep_params<V, E, TPR>(kept + E * TPR, b, t, D, 0.f);
         __syncthreads();
-    } else {
-        if (n0 < N) load_row<T, V, kNV, TPR>(raw, x + n0 * ldx, t, D);
     }
     constexpr int kStep = Pairs<V>::kStep, kP = Pairs<V>::kP;
     Pairs<V> wv[kHold ? E / 2 / kP : 1], bv[kHold ? E / 2 / kP : 1];
@@ -305,35 +258,19 @@ __global__ void __launch_bounds__(block_threads(TPR), residents(TPR, (V > 1), fa
             bv[i / kStep] = params2<V, TPR>(b, i, t, D, 0.f);
         }
     }
-    int st = 0;
-    uint32_t ph = 0u;
     for (int64_t n = n0; n < N; n += step) {
         Pairs<V> f[E / 2 / kP];
         float s[1], q[1];
         unsigned long long s2 = 0ull, q2 = 0ull;
-        // after a wait that expired every thread goes on: none is left at a barrier
-        bool landed = true;
-        if constexpr (kBulk) landed = tc::mbar_wait(&R.full[st], ph, abort, status);
 #pragma unroll
         for (int i = 0; i < kNV; i += kStep) {
-            f[i / kStep] = kBulk ? pairs_at<T, V, TPR, true>(reinterpret_cast<const T *>(ring + st * kStage), i, t, D)
-                                 : pairs_of<T, V>(raw + (kBulk ? 0 : i));
+            f[i / kStep] = pairs_of<T, V>(raw + i);
 #pragma unroll
             for (int j = 0; j < kP; ++j) s2 = row::add2(s2, f[i / kStep].p[j]);
         }
         s[0] = lo_of(s2) + hi_of(s2);
-        if constexpr (!kBulk) {
-            if (n + step < N) load_row<T, V, kNV, TPR>(raw, x + (n + step) * ldx, t, D);
-        }
+        if (n + step < N) load_row<T, V, kNV, TPR>(raw, x + (n + step) * ldx, t, D);
         row::group_sum<TPR>(s, buf[group][0], group, t);
-        if constexpr (kBulk) {
-            // every thread of the group has its part of the row
-            if (t == 0 && n + kStages * step < N && landed) copy(n + kStages * step, st);
-            if (++st == kStages) {
-                st = 0;
-                ph ^= 1u;
-            }
-        }
         const float mu = s[0] / width;
         const unsigned long long minus_mu = pack2(-mu, -mu);
 #pragma unroll
@@ -375,11 +312,6 @@ __global__ void __launch_bounds__(block_threads(TPR), residents(TPR, (V > 1), fa
             }
             store_pairs<T, V, TPR>(y + n * D, i, t, D, o);
         }
-    }
-    if constexpr (kBulk) {
-        // the barriers of a row's sums lie between the flag and here; a warp's sums have none
-        if constexpr (TPR == 32) __syncwarp();
-        if (*abort) lost_rows<T, V, E, TPR, kStages>(rings, N, D, y, mean, rstd, status);
     }
 }
 
@@ -602,12 +534,7 @@ __global__ void __launch_bounds__(block_threads(TPR), residents(TPR, (V > 1), tr
                 }
             }
         }
-        if (!ok && t == 0) {
-            // a set of rows brings its last stages' copies only once it is summed
-            const int64_t row = (R.lost - n0) / step, rows = (N - n0 + step - 1) / step;
-            const int64_t issued = row > 0 ? row + kStages - kRows : kStages;
-            drain<kStages>(R, issued < rows ? issued : rows, status);
-        }
+        if (!ok && t == 0) drain<kStages, kRows, TPR>(rings, N, status);
     } else {
         float mu = 0.f, r = 0.f;
         row::Raw<T, V> nx[kKeep ? kNV : 1], nd[kKeep ? kNV : 1];  // the next row
@@ -864,13 +791,13 @@ int64_t most_parts(int64_t N, int64_t D)
 template <typename T, int V, int E, int TPR, bool KEEP>
 cudaError_t forward_as(const Args &a, int64_t blocks)
 {
-    constexpr int kT = block_threads(TPR), bytes = Forward<T, V, E, TPR, KEEP>::kBytes;
+    constexpr int kT = block_threads(TPR), bytes = kForwardBytes<V, E, TPR, KEEP>;
     static SmemAttrCache attr_cache;
     const cudaError_t attr = smem_attr_once(norm_kernel<T, V, E, TPR, KEEP>, bytes, attr_cache);
     if (attr != cudaSuccess) return attr;
     norm_kernel<T, V, E, TPR, KEEP><<<static_cast<unsigned>(blocks), kT, bytes, a.stream>>>(
         static_cast<const T *>(a.x), a.ldx, a.N, static_cast<int>(a.D), a.w, a.b, a.eps, static_cast<T *>(a.y), a.mean,
-        a.rstd, a.status);
+        a.rstd);
     return cudaGetLastError();
 }
 
@@ -879,7 +806,7 @@ cudaError_t forward_one(const Args &a)
 {
     constexpr int kGroups = block_threads(TPR) / TPR;
     const int64_t blocks = least((a.N + kGroups - 1) / kGroups, static_cast<int64_t>(row::sm_count()) * residents(TPR, (V > 1), false));
-    if constexpr (Forward<T, V, E, TPR, true>::kParams > 0)
+    if constexpr (kForwardBytes<V, E, TPR, true> > 0)
         if (a.N > 4 * blocks) return forward_as<T, V, E, TPR, true>(a, blocks);  // rows enough for it
     return forward_as<T, V, E, TPR, false>(a, blocks);
 }
@@ -976,8 +903,7 @@ size_t layer_norm_workspace(int64_t N, int64_t D)
 }
 
 cudaError_t launch_layer_norm(const void *x, int dtype, int64_t N, int64_t D, int64_t ldx, const float *w,
-                              const float *b, float eps, void *y, float *mean, float *rstd, uint32_t *status,
-                              cudaStream_t stream)
+                              const float *b, float eps, void *y, float *mean, float *rstd, cudaStream_t stream)
 {
     norm::Args a{};
     a.x = x;
@@ -990,7 +916,6 @@ cudaError_t launch_layer_norm(const void *x, int dtype, int64_t N, int64_t D, in
     a.y = y;
     a.mean = mean;
     a.rstd = rstd;
-    a.status = status;
     a.stream = stream;
     return dtype == CCI_F32 ? norm::forward<float>(a) : norm::forward<uint16_t>(a);
 }

@@ -1,5 +1,5 @@
-"""Layer norm's bounded waits say when they expire: both directions take a status word, no kernel waits without one,
-and a word given to a call that succeeds stays 0."""
+"""Layer norm's bounded waits say when they expire: the backward pass takes a status word, no kernel waits without one,
+and a word given to a call that succeeds stays 0.  The forward pass waits for nothing."""
 import glob
 import os
 import re
@@ -12,7 +12,7 @@ from paper_1910_11971_gb300 import build as cci_build
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 FAKE = 0x10000  # never dereferenced: refused before any launch
-OK, NULL, SHAPE, DTYPE, ALIGN, VALUE, WORKSPACE = 0, 1, 2, 4, 5, 6, 11
+NULL, SHAPE, DTYPE, ALIGN, WORKSPACE = 1, 2, 4, 5, 11
 
 
 def test_every_bounded_wait_has_a_status_word():
@@ -23,18 +23,12 @@ def test_every_bounded_wait_has_a_status_word():
 
 def test_refusals_with_a_status_word():
     cci_build.build()
-    f, b = cci.lib().cci_layer_norm_ex, cci.lib().cci_layer_norm_backward_ex
-
-    def fwd(x=FAKE, dt=0, N=4, D=8, ld=8, eps=1e-5, y=FAKE):
-        return f(x, dt, N, D, ld, FAKE, FAKE, eps, y, FAKE, FAKE, FAKE, None)
-
-    assert fwd(dt=3) == DTYPE and fwd(x=None) == NULL and fwd(ld=7) == SHAPE and fwd(eps=-1.0) == VALUE
-    assert fwd(y=FAKE + 2) == ALIGN and fwd(N=0, x=None, y=None) == OK
+    b = cci.lib().cci_layer_norm_backward_ex
 
     def bwd(dy=FAKE, dt=0, N=4, D=8, ws=FAKE, n=0):
         return b(dy, 8, FAKE, 8, dt, N, D, FAKE, FAKE, FAKE, FAKE, FAKE, FAKE, FAKE, ws, n, None)
 
-    assert bwd(dt=3) == DTYPE and bwd(dy=None) == NULL and bwd(D=0) == SHAPE
+    assert bwd(dt=3) == DTYPE and bwd(dy=FAKE + 2) == ALIGN and bwd(dy=None) == NULL and bwd(D=0) == SHAPE
     assert bwd() == WORKSPACE and bwd(ws=None, n=1 << 20) == WORKSPACE
 
 
@@ -50,16 +44,10 @@ def test_status_stays_clear(N, D, dtype):
     x, dy = (torch.randn((N, D), generator=g, device=dev).to(dtype) for _ in range(2))
     w, b = (torch.randn(D, generator=g, device=dev) for _ in range(2))
     st = cci.new_status(dev)
-    y, mean, rstd = cci.layer_norm(x, w, b, status=st)
+    y, mean, rstd = cci.layer_norm(x, w, b)
     got = cci.layer_norm_backward(dy, x, mean, rstd, w, status=st)
     assert cci.read_status(st) == 0
     assert all(t.isfinite().all() for t in (y, mean, rstd, *got))
-    # the calls without a word: the same bits
+    # again, and without a word: the same bits
     assert all(torch.equal(p, q) for p, q in zip((y, mean, rstd), cci.layer_norm(x, w, b)))
     assert all(torch.equal(p, q) for p, q in zip(got, cci.layer_norm_backward(dy, x, mean, rstd, w)))
-    out = torch.empty_like(y)
-    s = torch.cuda.current_stream(dev).cuda_stream
-    code = 0 if dtype == torch.float32 else 1
-    assert cci.lib().cci_layer_norm(x.data_ptr(), code, N, D, D, w.data_ptr(), b.data_ptr(), 1e-5, out.data_ptr(),
-                                    mean.data_ptr(), rstd.data_ptr(), s) == 0
-    assert torch.equal(out, y)
