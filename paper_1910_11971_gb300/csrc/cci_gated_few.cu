@@ -15,8 +15,10 @@
 // same run, copied to shared memory in bulk, and each keeps the values whose index is its row.
 //
 // fp32: fused multiply-adds, 16 rows by up to eight tokens a warp.  Twice the bytes and no products of planes.
-// A token stays at the memory's time, more are bound by the multiply-adds (4096 -> 8192: 1 token 39.5 us of
-// 39.5, 4 51, 8 73, 16 142).
+// A token stays at the memory's time (4096 -> 8192: 1 token 39.5 us of 39.5, 4 52, 8 73, 16 142).  What bounds more
+// is not the multiply-adds (8 tokens 13 us of them, 16 27) but the tokens' own reads, which every block makes: past
+// four tokens 2048 blocks of four channels read 268 MB of them out of L2, as much as the weights, and past
+// eight the weights are read twice.
 //
 // The warps' sums are joined in shared memory in warp order: the same bits at every call.
 #include "cci_gated.cuh"
@@ -199,7 +201,18 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 4 : 3) bf16_kernel(Args p)
 // A block takes a group (two of G = 4) of each projection: MT sets of eight channels.  Their runs of a round
 // of 1024 indices are contiguous, and bulk copies bring them to shared memory, as many rounds ahead as it
 // holds: registers hold no weights that are on their way.  What bounds it is taking each row's weights out of the
-// runs, on the integer pipe (60 % of it; 16 tokens, 4096 -> 4096, G = 8, K = 2: 21.2 us of 3.7 for the bytes).
+// runs, each row by itself, on the integer pipe: work that grows with G K where the bytes grow with K (60 % of that pipe; 16 tokens,
+// 4096 -> 4096, G = 8, K = 2: 21.3 us of 3.7 for the bytes; its 512 blocks are 1.1 rounds of 456 places).  So
+// packed weights save memory, and time with K = 1 alone; against dense weights of the same block, us:
+//                            1 token              8                16
+//   4096 -> 4096  dense      11.7                 12.8             16.3
+//     G = 8, K = 1, 2        11.9, 19.8           12.1, 20.1       15.1, 21.7
+//     G = 4, K = 2           24.8                 26.5             28.1
+//     G = 32, K = 8          35.7                 36.6             39.2
+//   4096 -> 8192  dense      21.6                 23.5             26.9
+//     G = 8, K = 1, 2        18.2, 33.2           18.9, 33.3       24.0, 36.5
+//     G = 4, K = 2           39.3                 40.6             43.4
+//     G = 32, K = 8          72.5                 74.2             78.5
 constexpr int kMaxStages = 8;
 
 struct PackedSmem {
@@ -451,7 +464,8 @@ bool few_tokens(int dtype, int64_t N, int64_t F)
 }
 
 // Packed weights read as they are, against expanded and multiplied by tiles (4096 -> 8192): G = 8, K = 2 1 token
-// 32.8 us and 62.7, 16 36.3 and 62.7; G = 32, K = 8 1 token 72 and 89, 16 79 and 89
+// 33.2 us and 62.7, 16 36.5 and 62.7; G = 32, K = 8 1 token 72.5 and 89, 16 78.5 and 89.  fp32 is always expanded: G = 8,
+// K = 2, 4096 -> 4096 1 token 57 us and 21 with dense weights, 16 109 and 73, 500 205 and 218
 bool few_packed(const GatedArgs &a)
 {
     auto at16 = [](const void *q) { return reinterpret_cast<uintptr_t>(q) % 16 == 0; };

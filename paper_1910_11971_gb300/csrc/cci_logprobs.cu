@@ -637,7 +637,8 @@ __global__ void __launch_bounds__(kThreads, kThreads == 32 ? 28 : 1024 / kThread
                     row::unpack<T, kV>(word[u], v);
                     m = raw_max<T, kV>(word[u], v);
                 }
-                // most loads hold none (4096 x 20000 bf16, 20 alternatives: 93.3 us when every element is looked at, 89.8 so)
+                // most loads hold none (8 x 131072 fp32, 20 alternatives: 12.4 us when every element is looked at, 11.8
+                // so; many rows 1 % the other way)
                 if (!__any_sync(0xffffffffu, at < to && m >= least)) continue;
 #pragma unroll
                 for (int j = 0; j < kV; ++j) {
@@ -841,13 +842,14 @@ cudaError_t launch_middle(const T *x, int64_t ldx, int64_t N, int64_t V, const R
 template <typename T>
 cudaError_t launch(const T *x, int64_t ldx, int64_t N, int64_t V, const Row &o, cudaStream_t stream)
 {
-    // a warp a row, in its registers (bf16, against the kernel below: 65536 x 600 55 us and 174, 65536 x 1000 67 and 175)
+    // a warp a row, in its registers (bf16, against the kernel below, which reads whole words, with a warp a row:
+    // 65536 x 600 54.9 us and 57.6, 65536 x 1000 66.5 and 59.8; that kernel has no runs short enough for alternatives here)
     if (V <= 128) return launch_short<T, 4>(x, ldx, N, V, o, stream);
     if (V <= 512) return launch_short<T, 16>(x, ldx, N, V, o, stream);
     if (V <= 1024) return launch_short<T, 32>(x, ldx, N, V, o, stream);
     if (V <= 8192) {
-        // a warp a row where the rows fill the SMs, else four (bf16: 2432 x 4000 8.6 us and 11.7, 16384 x 8192 57 and
-        // 83; with 5 alternatives 14.9 and 21.2, 108 and 157)
+        // a warp a row where the rows fill the SMs, else four (bf16: 2432 x 4000 8.3 us and 10.9, 16384 x 8192 55 and
+        // 76; with 5 alternatives 14.4 and 18.5, 106 and 140)
         if (N >= 16 * row::sm_count()) return launch_middle<T, 32>(x, ldx, N, V, o, stream);
         return launch_middle<T, 128>(x, ldx, N, V, o, stream);
     }
@@ -858,8 +860,8 @@ cudaError_t launch(const T *x, int64_t ldx, int64_t N, int64_t V, const Row &o, 
     int parts = 1;
     while (parts < 8 && N * parts * 2 <= 4 * row::sm_count() && V >= 2 * parts * 16384) parts *= 2;
     // where the rows fill the SMs: blocks of four warps, eight of an SM, which share the rows out more evenly
-    // (bf16: 1024 x 131072 55 us in blocks of eight warps, 51 so; 4096 x 20000 50 and 41; with 5 alternatives 71 and 64,
-    // 87 and 66).  Past 131072 logits
+    // (bf16: 1024 x 131072 55 us in blocks of eight warps, 51 so; 4096 x 20000 47 and 40; with 5 alternatives 66 and 62,
+    // 76 and 64).  Past 131072 logits
     // their warps' runs would not fit two a lane
     if (N >= 4 * row::sm_count() && V <= 131072) {
         if (!o.k) return launch_rows<T, 128, 512, false>(x, ldx, N, V, o, 1, stream);

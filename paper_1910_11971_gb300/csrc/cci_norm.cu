@@ -80,7 +80,7 @@ constexpr int stages_of(int bytes, int groups, int blocks)
 // keeps two stages or more: bytes of them, and the ring's stages then.  From L2 they are 8 bytes an element again for
 // every row (forward bf16 8000 x 8192 78.8 us, 73.3 so; fp32 16384 x 4096 126 and 121; backward bf16 4000 x 16384 184 and
 // 105).  Not where a block has few rows (forward bf16 100 x 8192: 3.6 us, 4.2 with them), nor in the backward pass of
-// fp32 rows (8000 x 8192: 136 us, 145 with it)
+// fp32 rows (8000 x 8192: 6 % slower with it)
 constexpr int kWideBudget = 224 * 1024;
 constexpr int shared_params(int bytes, int stage) { return (kWideBudget - bytes) / stage >= 2 ? bytes : 0; }
 constexpr int stages_beside(int params, int stage)
