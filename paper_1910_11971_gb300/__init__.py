@@ -491,7 +491,8 @@ def dense_conv2d_tc(X: torch.Tensor, Wd: torch.Tensor, Cout: int, KH: int, KW: i
 
 
 # ---------------------------------------------------------------------------
-# the layers around a pruned projection
+# the layers around a pruned projection.  Plain functions, as all of this binding: no graph is recorded for
+# tensors that require gradients; a training step makes the *_backward calls itself
 # ---------------------------------------------------------------------------
 
 def _device(t: torch.Tensor, name: str) -> int:
