@@ -626,6 +626,61 @@ cci_status cci_gated_linear_backward(const void *dH, const void *X, cci_dtype dt
                                      void *workspace, size_t workspace_bytes, cci_stream_t stream);
 
 /*
+ * cci_linear_cross_entropy -- the loss of N tokens over a vocabulary of V straight from a head's inputs,
+ * z = X W^T, without keeping the logits:
+ *   loss[n]  = log sum over v of exp(z_v) - z_t,  t = targets[n]
+ *   stats[n] = (m, log sum exp(z - m)), m the row's maximum (the gradient needs them)
+ * with fp32 accumulators (bf16: products of the exact values; fp32: three bf16 planes of every
+ * operand, as cci_gated_linear).  A target equal to `ignore_index` gives loss 0; any other target
+ * outside [0, V) sets CCI_ERR_INDEX in dev_status and gives NaN.  NaN or infinite logits make their row's loss
+ * NaN.
+ *
+ *   X          device [N][D] of dtype
+ *   W          device [V][D] of dtype (pruned weights: their dense form, as cci_td_mask writes it)
+ *   targets    device int64 [N]
+ *   loss       device fp32 [N]; stats fp32 [N][2] (written)
+ *   workspace  device, 16-byte aligned, cci_head_workspace_size(CCI_HEAD_FORWARD, ...) bytes;
+ *              overwritten.  It depends on the current device's number of SMs
+ *   dev_status device uint32 or NULL (CCI_ERR_INDEX, CCI_ERR_TIMEOUT)
+ * D is a multiple of 8; X and W are 16-byte aligned.  V may be any size.  N = 0 is valid and enqueues
+ * nothing.
+ * Errors: CCI_ERR_NULL, CCI_ERR_SHAPE (N < 0, D or V < 1, sizes of 2^30 or more),
+ *         CCI_ERR_UNSUPPORTED (D % 8), CCI_ERR_DTYPE, CCI_ERR_ALIGN, CCI_ERR_WORKSPACE, CCI_ERR_CUDA.
+ */
+typedef enum cci_head_call {
+    CCI_HEAD_FORWARD = 0,
+    CCI_HEAD_BACKWARD = 1
+} cci_head_call;
+
+/* bytes of workspace of a call (0: none needed, or invalid sizes) */
+size_t cci_head_workspace_size(cci_head_call call, cci_dtype dtype, int64_t N, int64_t D, int64_t V);
+
+cci_status cci_linear_cross_entropy(const void *X, cci_dtype dtype, int64_t N, int64_t D, const void *W, int64_t V,
+                                    const int64_t *targets, int64_t ignore_index, float *loss, float *stats,
+                                    uint32_t *dev_status, void *workspace, size_t workspace_bytes,
+                                    cci_stream_t stream);
+
+/*
+ * cci_linear_cross_entropy_backward -- the gradients of cci_linear_cross_entropy from that of the loss:
+ *   P[n][v] = dloss[n] * (softmax(z)[v] - 1[v = t]),  dX = P W,  dW = P^T X
+ * in pieces of the vocabulary, whose logits are computed again.  P is rounded to bf16 for the products (fp32:
+ * split into planes); sums are fp32 in a fixed order, each gradient rounded once to dtype.  Rows whose
+ * target is `ignore_index`, or outside [0, V) (which sets CCI_ERR_INDEX), or whose dloss is 0 have P = 0.
+ *
+ *   dloss      device fp32 [N];  X, W, targets as in the forward call
+ *   stats      as the forward call wrote them
+ *   dX         device [N][D] of dtype (written), or NULL
+ *   dW         device [V][D] of dtype (written; zeros for N = 0), or NULL
+ *   workspace  cci_head_workspace_size(CCI_HEAD_BACKWARD, ...) bytes: about 256 MB for a piece, more
+ *              only where a piece of 2048 entries takes more
+ * Errors: as cci_linear_cross_entropy.
+ */
+cci_status cci_linear_cross_entropy_backward(const float *dloss, const void *X, cci_dtype dtype, int64_t N, int64_t D,
+                                             const void *W, int64_t V, const int64_t *targets, int64_t ignore_index,
+                                             const float *stats, void *dX, void *dW, uint32_t *dev_status,
+                                             void *workspace, size_t workspace_bytes, cci_stream_t stream);
+
+/*
  * cci_kernel_name -- the name of the kernel family that cci_linear_ws /
  * cci_conv2d_ws would run for a layer with these sizes (R = Cin for a product,
  * Cin*KH*KW for a convolution, taken to have strides <= 2) when every pointer is

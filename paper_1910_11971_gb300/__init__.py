@@ -27,6 +27,7 @@ LIB_PATH = os.path.join(_HERE, "_build", "libcci.so")
 F32, BF16 = 0, 1
 ACTIVATIONS = {"silu": 0, "gelu": 1, "gelu_tanh": 2, "relu": 3, "sigmoid": 4}
 GATED_FORWARD, GATED_PACKED, GATED_BACKWARD = 0, 1, 2
+HEAD_FORWARD, HEAD_BACKWARD = 0, 1
 ALGO_AUTO, ALGO_GENERIC, ALGO_REGTILE, ALGO_DENSE_TC, ALGO_EXPAND, ALGO_DENSE_TC_WS = 0, 1, 2, 3, 4, 5
 
 STATUS_NAMES = {
@@ -86,6 +87,11 @@ SIGNATURES = {
                                        ctypes.c_size_t, _P]),
     "cci_gated_linear_backward": (_I32, [_P, _P, _I32, _I64, _I64, _P, _P, _I64, _I32, _P, _P, _P, _P, _P, _U32P, _P,
                                          ctypes.c_size_t, _P]),
+    "cci_head_workspace_size": (ctypes.c_size_t, [_I32, _I32, _I64, _I64, _I64]),
+    "cci_linear_cross_entropy": (_I32, [_P, _I32, _I64, _I64, _P, _I64, _P, _I64, _P, _P, _U32P, _P, ctypes.c_size_t,
+                                        _P]),
+    "cci_linear_cross_entropy_backward": (_I32, [_P, _P, _I32, _I64, _I64, _P, _I64, _P, _I64, _P, _P, _P, _U32P, _P,
+                                                 ctypes.c_size_t, _P]),
     "cci_kernel_name": (ctypes.c_char_p, [_I32, _I64, _I64, _I64, _I32, _I32, _I32]),
     "cci_status_string": (ctypes.c_char_p, [_I32]),
     "cci_decode_device_status": (_I32, [ctypes.c_uint32]),
@@ -761,6 +767,76 @@ def gated_linear_backward(dH: torch.Tensor, X: torch.Tensor, Wg: torch.Tensor, W
                                            None if status is None else _status_word(status, index), wp, wb,
                                            torch._C._cuda_getCurrentRawStream(index)), "cci_gated_linear_backward")
     return dX, dWg, dWu
+
+
+def head_workspace(call: int, dtype: torch.dtype, N: int, D: int, V: int, device) -> Optional[torch.Tensor]:
+    """The workspace of a head's cross entropy (``HEAD_FORWARD`` or ``HEAD_BACKWARD``), from PyTorch memory: None
+    when it needs none."""
+    device = torch.device(device)
+    index = device.index if device.index is not None else torch.cuda.current_device()
+    return _workspace(_head_bytes(call, F32 if dtype == torch.float32 else BF16, N, D, V, index), device)
+
+
+@functools.lru_cache(maxsize=4096)
+def _head_bytes(call: int, dtype: int, N: int, D: int, V: int, device_index: int) -> int:
+    with torch.cuda.device(device_index):  # depends on the device's SMs
+        return int(lib().cci_head_workspace_size(call, dtype, N, D, V))
+
+
+def _head_operands(X: torch.Tensor, W: torch.Tensor):
+    """(device, N, D, V, type's code) of a head's inputs and weights."""
+    index = _device(X, "X")
+    if X.dim() != 2 or not X.is_contiguous():
+        raise ValueError("X must be a contiguous matrix")
+    if W.dim() != 2:
+        raise ValueError("W must be a matrix")
+    N, D = X.shape
+    V = W.shape[0]
+    _like(W, (V, D), X.dtype, "W", index)
+    return index, N, D, V, _dtype_code(X)
+
+
+def linear_cross_entropy(X: torch.Tensor, W: torch.Tensor, targets: torch.Tensor, *, ignore_index: int = -100,
+                         status: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None):
+    """(loss, stats) of the logits X W^T and one target (int64) a row, without keeping the logits
+    (``cci_linear_cross_entropy``): the fp32 loss of each row (0 for ``ignore_index``) and (maximum, log of the sum
+    of exp(logit - maximum)) for the backward pass.  X [N][D], W [V][D]; D a multiple of 8, V of any size."""
+    index, N, D, V, code = _head_operands(X, W)
+    loss = torch.empty(N, dtype=torch.float32, device=X.device)
+    stats = torch.empty((N, 2), dtype=torch.float32, device=X.device)
+    if workspace is None:
+        workspace = _workspace(_head_bytes(HEAD_FORWARD, code, N, D, V, index), X.device)
+    wp, wb = (None, 0) if workspace is None else _space(workspace, index)
+    _check(lib().cci_linear_cross_entropy(X.data_ptr(), code, N, D, W.data_ptr(), V,
+                                          _vec(targets, N, "targets", index, torch.int64), ignore_index,
+                                          loss.data_ptr(), stats.data_ptr(),
+                                          None if status is None else _status_word(status, index), wp, wb,
+                                          torch._C._cuda_getCurrentRawStream(index)), "cci_linear_cross_entropy")
+    return loss, stats
+
+
+def linear_cross_entropy_backward(dloss: torch.Tensor, X: torch.Tensor, W: torch.Tensor, targets: torch.Tensor,
+                                  stats: torch.Tensor, *, ignore_index: int = -100, need_dx: bool = True,
+                                  need_dw: bool = True, status: Optional[torch.Tensor] = None,
+                                  workspace: Optional[torch.Tensor] = None):
+    """(dX, dW) of ``linear_cross_entropy`` (``cci_linear_cross_entropy_backward``) from the fp32 gradient of each
+    row's loss and the forward call's stats, each in X's dtype; None for those not asked for (``need_dx``,
+    ``need_dw``)."""
+    index, N, D, V, code = _head_operands(X, W)
+    dX = torch.empty_like(X) if need_dx else None
+    dW = torch.empty_like(W) if need_dw else None
+    if workspace is None:
+        workspace = _workspace(_head_bytes(HEAD_BACKWARD, code, N, D, V, index), X.device)
+    wp, wb = (None, 0) if workspace is None else _space(workspace, index)
+    _check(lib().cci_linear_cross_entropy_backward(_vec(dloss, N, "dloss", index), X.data_ptr(), code, N, D,
+                                                   W.data_ptr(), V, _vec(targets, N, "targets", index, torch.int64),
+                                                   ignore_index, _vec(stats, 2 * N, "stats", index),
+                                                   dX.data_ptr() if need_dx else None,
+                                                   dW.data_ptr() if need_dw else None,
+                                                   None if status is None else _status_word(status, index), wp, wb,
+                                                   torch._C._cuda_getCurrentRawStream(index)),
+           "cci_linear_cross_entropy_backward")
+    return dX, dW
 
 
 def _like(t: torch.Tensor, shape, dtype: torch.dtype, name: str, index: int) -> None:

@@ -229,3 +229,85 @@ cci_status cci_gated_linear_backward(const void *dH, const void *X, cci_dtype dt
 }
 
 }  // extern "C"
+
+namespace {
+
+// sizes and pointers that both calls of a head's cross entropy have
+cci_status check_head(int dtype, int64_t N, int64_t D, int64_t V, const void *X, const void *W, const int64_t *targets,
+                      const float *stats, const void *workspace, size_t bytes, int call)
+{
+    constexpr int64_t lim = int64_t(1) << 30;  // tile coordinates are 32-bit
+    if (!valid_dtype(dtype)) return CCI_ERR_DTYPE;
+    if (!W || (N > 0 && (!X || !targets || !stats))) return CCI_ERR_NULL;
+    if (N < 0 || D < 1 || V < 1 || N >= lim || D >= lim || V >= lim) return CCI_ERR_SHAPE;
+    if (D % 8 != 0) return CCI_ERR_UNSUPPORTED;
+    if (!aligned(X, 16) || !aligned(W, 16) || !aligned(targets, 8) || !aligned(stats, 4)) return CCI_ERR_ALIGN;
+    const size_t need = N > 0 ? head_workspace(dtype, N, D, V, call) : 0;
+    if (need > 0 && (!workspace || bytes < need || !aligned(workspace, 16))) return CCI_ERR_WORKSPACE;
+    return CCI_OK;
+}
+
+HeadArgs head_args(const void *X, int dtype, int64_t N, int64_t D, const void *W, int64_t V, const int64_t *targets,
+                   int64_t ignore, uint32_t *status, void *workspace)
+{
+    HeadArgs a{};
+    a.X = X;
+    a.dtype = dtype;
+    a.N = N;
+    a.D = D;
+    a.V = V;
+    a.W = W;
+    a.targets = targets;
+    a.ignore = ignore;
+    a.status = status;
+    a.workspace = workspace;
+    return a;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t cci_head_workspace_size(cci_head_call call, cci_dtype dtype, int64_t N, int64_t D, int64_t V)
+{
+    constexpr int64_t lim = int64_t(1) << 30;
+    if (!valid_dtype(dtype) || N < 1 || D < 1 || V < 1 || N >= lim || D >= lim || V >= lim) return 0;
+    if (call < CCI_HEAD_FORWARD || call > CCI_HEAD_BACKWARD) return 0;
+    return head_workspace(dtype, N, D, V, call);
+}
+
+cci_status cci_linear_cross_entropy(const void *X, cci_dtype dtype, int64_t N, int64_t D, const void *W, int64_t V,
+                                    const int64_t *targets, int64_t ignore_index, float *loss, float *stats,
+                                    uint32_t *dev_status, void *workspace, size_t workspace_bytes, cci_stream_t stream)
+{
+    const cci_status st =
+        check_head(dtype, N, D, V, X, W, targets, stats, workspace, workspace_bytes, CCI_HEAD_FORWARD);
+    if (st != CCI_OK) return st;
+    if (N > 0 && !loss) return CCI_ERR_NULL;
+    if (!aligned(loss, 4)) return CCI_ERR_ALIGN;
+    if (N == 0) return CCI_OK;
+    HeadArgs a = head_args(X, dtype, N, D, W, V, targets, ignore_index, dev_status, workspace);
+    a.loss = loss;
+    a.stats = stats;
+    return to_status(launch_head(a, as_stream(stream)));
+}
+
+cci_status cci_linear_cross_entropy_backward(const float *dloss, const void *X, cci_dtype dtype, int64_t N, int64_t D,
+                                             const void *W, int64_t V, const int64_t *targets, int64_t ignore_index,
+                                             const float *stats, void *dX, void *dW, uint32_t *dev_status,
+                                             void *workspace, size_t workspace_bytes, cci_stream_t stream)
+{
+    const cci_status st =
+        check_head(dtype, N, D, V, X, W, targets, stats, workspace, workspace_bytes, CCI_HEAD_BACKWARD);
+    if (st != CCI_OK) return st;
+    if (N > 0 && !dloss) return CCI_ERR_NULL;
+    if (!aligned(dloss, 4) || !aligned(dX, 16) || !aligned(dW, 16)) return CCI_ERR_ALIGN;
+    HeadArgs a = head_args(X, dtype, N, D, W, V, targets, ignore_index, dev_status, workspace);
+    a.stats = const_cast<float *>(stats);
+    a.dloss = dloss;
+    a.dX = dX;
+    a.dW = dW;
+    return to_status(launch_head_backward(a, as_stream(stream)));
+}
+
+}  // extern "C"

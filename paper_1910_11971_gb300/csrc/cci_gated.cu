@@ -18,20 +18,6 @@ namespace gated {
 
 constexpr size_t round256(size_t b) { return (b + 255) / 256 * 256; }
 
-// v as three bf16: each the nearest of what the ones before leave.  A value that does not fit (inf,
-// NaN) is its first plane alone, and one that would round up to inf is cut
-__device__ __forceinline__ void split3(float v, uint32_t (&p)[3])
-{
-    uint32_t b = row::bf16x2(v, 0.f) & 0xffffu;
-    if ((b & 0x7f80u) == 0x7f80u && fabsf(v) <= 3.402823466e38f) b = (__float_as_uint(v) >> 16);
-    p[0] = b;
-    const bool whole = (b & 0x7f80u) != 0x7f80u;
-    const float r1 = whole ? v - __uint_as_float(b << 16) : 0.f;
-    p[1] = row::bf16x2(r1, 0.f) & 0xffffu;
-    const float r2 = r1 - __uint_as_float(p[1] << 16);
-    p[2] = row::bf16x2(r2, 0.f) & 0xffffu;
-}
-
 // eight values to their places in one plane or three, `plane` elements apart
 template <int P>
 __device__ __forceinline__ void store_planes(uint16_t *out, int64_t plane, const float (&v)[8])

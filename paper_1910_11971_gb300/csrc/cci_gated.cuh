@@ -26,11 +26,16 @@
 #pragma once
 
 #include "cci_gemm_ws.cuh"
+#include "cci_rowops.cuh"
 
 namespace cci {
 namespace gated {
 
-enum Mode { kForward = 0, kDx = 1, kDw = 2 };
+// kDxAdd, kDwOne: the same products of one pair of operands (a head's gradients, cci_head.cu), the first added to what
+// the output holds where the launch says so
+enum Mode { kForward = 0, kDx = 1, kDw = 2, kDxAdd = 3, kDwOne = 4 };
+
+constexpr bool is_dw(int mode) { return mode == kDw || mode == kDwOne; }
 
 // everything a launch needs but its tensor maps
 struct Params {
@@ -45,6 +50,7 @@ struct Params {
     int act;             // cci_activation
     int out_f32;
     int save;            // forward: g and u are written too (fp32)
+    int add;             // kDxAdd: the (fp32) output is added to
     // tiles below `whole` are computed whole, one CTA (pair) after the other; the reductions of the rest, where a
     // last round of tiles would leave most SMs idle, are laid end to end and cut evenly over all of them, their parts
     // written in fp32 and added by join_kernel
@@ -277,6 +283,15 @@ __device__ __forceinline__ void load_3d(uint32_t dst, const CUtensorMap *map, in
             : "memory");
 }
 
+// a tile's store that adds to fp32 elements (one addition each: a launch's tiles do not overlap)
+__device__ __forceinline__ void tma_add_2d(const CUtensorMap *map, uint32_t src, int c0, int c1)
+{
+    asm volatile("cp.reduce.async.bulk.tensor.2d.global.shared::cta.add.tile.bulk_group [%0, {%2, %3}], [%1];" ::"l"(
+                     reinterpret_cast<uint64_t>(map)),
+                 "r"(src), "r"(c0), "r"(c1)
+                 : "memory");
+}
+
 // 32 columns of this warp's TMEM lanes, without waiting for them
 __device__ __forceinline__ void tmem_ld32_begin(uint32_t taddr, uint32_t (&v)[32])
 {
@@ -288,6 +303,23 @@ __device__ __forceinline__ void tmem_ld32_begin(uint32_t taddr, uint32_t (&v)[32
           "=r"(v[16]), "=r"(v[17]), "=r"(v[18]), "=r"(v[19]), "=r"(v[20]), "=r"(v[21]), "=r"(v[22]), "=r"(v[23]),
           "=r"(v[24]), "=r"(v[25]), "=r"(v[26]), "=r"(v[27]), "=r"(v[28]), "=r"(v[29]), "=r"(v[30]), "=r"(v[31])
         : "r"(taddr));
+}
+
+// the nearest bf16 of v; v becomes what it leaves.  A value that does not fit (inf, NaN) leaves 0, and one that
+// would round up to inf is cut
+__device__ __forceinline__ uint32_t next_plane(float &v)
+{
+    uint32_t b = row::bf16x2(v, 0.f) & 0xffffu;
+    if ((b & 0x7f80u) == 0x7f80u && fabsf(v) <= 3.402823466e38f) b = __float_as_uint(v) >> 16;
+    v = (b & 0x7f80u) != 0x7f80u ? v - __uint_as_float(b << 16) : 0.f;
+    return b;
+}
+
+// v as three bf16: each the nearest of what the ones before leave
+__device__ __forceinline__ void split3(float v, uint32_t (&p)[3])
+{
+#pragma unroll
+    for (int q = 0; q < 3; ++q) p[q] = next_plane(v);
 }
 
 // products of planes (of A, of B) by term, the smallest first
@@ -345,7 +377,7 @@ __global__ void __launch_bounds__(Cfg<CG, BN>::kThreads, 1)
     product_kernel(const Params p, const __grid_constant__ Maps maps)
 {
     using C = Cfg<CG, BN>;
-    constexpr bool kAMn = MODE == kDw, kBMn = MODE != kForward;
+    constexpr bool kAMn = is_dw(MODE), kBMn = MODE != kForward;
     constexpr int kStages = C::kStages;
     constexpr int kNOut = MODE == kForward ? BN / 2 : BN;  // output columns of a tile
     constexpr uint32_t kIdesc = (1u << 4) | (1u << 7) | (1u << 10) | (static_cast<uint32_t>(kAMn) << 15) |
@@ -541,7 +573,10 @@ __global__ void __launch_bounds__(Cfg<CG, BN>::kThreads, 1)
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             tc::named_sync(1, 128);
             if (m == 0) {
-                tc::tma_store_2d(map, buf, c0, r0);
+                if (MODE == kDxAdd && p.add && map != &maps.parts)
+                    tma_add_2d(map, buf, c0, r0);
+                else
+                    tc::tma_store_2d(map, buf, c0, r0);
                 tc::bulk_commit();
             }
         };
@@ -773,6 +808,20 @@ __global__ void __launch_bounds__(MODE == kForward ? BN / 2 : BN)
             for (int j = 0; j < 8; ++j) v[0][j] = act_of<decltype(act)::value>(v[0][j]) * v[1][j];
         });
     }
+    if constexpr (MODE == kDxAdd) {
+        if (p.add) {
+            const float4 *at = reinterpret_cast<const float4 *>(static_cast<const float *>(out) + o);
+            const float4 a = at[0], b = at[1];
+            v[0][0] += a.x;
+            v[0][1] += a.y;
+            v[0][2] += a.z;
+            v[0][3] += a.w;
+            v[0][4] += b.x;
+            v[0][5] += b.y;
+            v[0][6] += b.z;
+            v[0][7] += b.w;
+        }
+    }
     if (p.out_f32) {
         store(static_cast<float *>(out) + o, v[0]);
     } else {
@@ -792,13 +841,14 @@ struct Operand {
     const void *data;
     int64_t rows, cols;
     int planes;
+    int64_t ld = 0;  // row stride (0: cols); a multiple of 8
 };
 
 // copies of 64 (swizzled 128-byte rows) x box_rows
 inline bool operand_map(CUtensorMap *m, const Operand &o, int box_rows)
 {
     const int64_t dims[3] = {o.cols, o.rows, o.planes};
-    const int64_t strides[2] = {o.cols * 2, o.cols * o.rows * 2};
+    const int64_t ld = o.ld ? o.ld : o.cols, strides[2] = {ld * 2, ld * o.rows * 2};
     const int box[3] = {64, box_rows, 1};
     return ws::make_map_strided(m, o.data, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, dims, strides, box);
 }
@@ -819,7 +869,7 @@ struct Job {
     void *out[2];
     float *save[2];   // forward: g and u, or null
     int64_t M, N, K;  // rows and columns of an output, length of a reduction
-    int terms, act, out_f32;
+    int terms, act, out_f32, add;
     float *parts;     // plan().part_bytes of workspace
     uint32_t *status;
 };
@@ -844,7 +894,7 @@ inline Plan plan(Mode mode, int64_t M, int64_t N, int64_t K, int terms)
 {
     const int64_t sms = ws::sm_count(), outs = mode == kDw ? 2 : 1;
     const int64_t stages = (K + 63) / 64 * terms * (mode == kDx ? 2 : 1);
-    const int64_t a_rows = mode == kDw || M > 128 ? 128 : (M + 7) / 8 * 8;
+    const int64_t a_rows = is_dw(mode) || M > 128 ? 128 : (M + 7) / 8 * 8;
     Plan best{};
     double least = 0.0;
     const int shapes[3][3] = {{2, 256, 512}, {1, 128, 256}, {1, 64, 192}};
@@ -879,7 +929,8 @@ cudaError_t launch_tiled(const Job &j, const Plan &plan, cudaStream_t stream)
 {
     using C = Cfg<CG, BN>;
     constexpr int kNOut = MODE == kForward ? BN / 2 : BN;
-    constexpr int two_a = MODE == kForward ? 1 : 2, two_b = MODE == kDw ? 1 : 2, two_out = MODE == kDw ? 2 : 1;
+    constexpr int two_a = MODE == kDx || MODE == kDw ? 2 : 1, two_b = MODE == kForward || MODE == kDx ? 2 : 1;
+    constexpr int two_out = MODE == kDw ? 2 : 1;
     Params p{};
     Maps maps{};
     p.M = j.M;
@@ -891,6 +942,7 @@ cudaError_t launch_tiled(const Job &j, const Plan &plan, cudaStream_t stream)
     p.act = j.act;
     p.out_f32 = j.out_f32;
     p.save = j.save[0] != nullptr;
+    p.add = j.add;
     p.status = j.status;
     const int64_t mt = (j.M + CG * C::kM - 1) / (CG * C::kM), nt = (j.N + kNOut - 1) / kNOut;
     if (mt * two_out * nt > (int64_t(1) << 30)) return cudaErrorInvalidValue;
@@ -901,7 +953,7 @@ cudaError_t launch_tiled(const Job &j, const Plan &plan, cudaStream_t stream)
     const int units = cut ? plan.units : ws::sm_count() / CG;
     p.whole = cut ? p.tiles - p.tiles % units : p.tiles;
     for (int i = 0; i < two_a; ++i)
-        if (!operand_map(&maps.a[i], j.a[i], MODE == kDw ? 64 : p.a_rows)) return cudaErrorInvalidValue;
+        if (!operand_map(&maps.a[i], j.a[i], is_dw(MODE) ? 64 : p.a_rows)) return cudaErrorInvalidValue;
     for (int i = 0; i < two_b; ++i)
         if (!operand_map(&maps.b[i], j.b[i], MODE == kForward ? (CG == 2 ? C::kBRows : C::kBRows / 2) : 64))
             return cudaErrorInvalidValue;
@@ -967,9 +1019,14 @@ bool few_tokens(int dtype, int64_t N, int64_t F);
 bool few_packed(const GatedArgs &a);
 cudaError_t launch_few(const GatedArgs &a, const void *wg, const void *wu, bool packed, cudaStream_t stream);
 
+// up to three fp32 matrices (of n elements, multiples of 8) as three bf16 planes each, one after the other
+cudaError_t split(const float *const *in, uint16_t *const *out, const int64_t *n, int jobs, cudaStream_t stream);
+
 cudaError_t launch_forward(const Job &j, cudaStream_t stream);
 cudaError_t launch_dx(const Job &j, cudaStream_t stream);
 cudaError_t launch_dw(const Job &j, cudaStream_t stream);
+cudaError_t launch_dx_add(const Job &j, cudaStream_t stream);
+cudaError_t launch_dw_one(const Job &j, cudaStream_t stream);
 
 }  // namespace gated
 }  // namespace cci

@@ -94,6 +94,25 @@ size_t gated_workspace(int dtype, int64_t N, int64_t D, int64_t F, int call);
 cudaError_t launch_gated(const GatedArgs &a, cudaStream_t stream);
 cudaError_t launch_gated_backward(const GatedArgs &a, cudaStream_t stream);
 
+// softmax cross entropy from a head's inputs (cci_head*.cu).  backward: dX and dW may each be null.  workspace:
+// head_workspace bytes for the call (a cci_head_call)
+struct HeadArgs {
+    const void *X;
+    int dtype;
+    int64_t N, D, V;
+    const void *W;
+    const int64_t *targets;
+    int64_t ignore;
+    float *loss, *stats;  // backward: stats is read
+    const float *dloss;
+    void *dX, *dW;
+    uint32_t *status;
+    void *workspace;
+};
+size_t head_workspace(int dtype, int64_t N, int64_t D, int64_t V, int call);
+cudaError_t launch_head(const HeadArgs &a, cudaStream_t stream);
+cudaError_t launch_head_backward(const HeadArgs &a, cudaStream_t stream);
+
 // One register-tiled instantiation: (dtype, G, K) -> tile shape and launcher.
 struct RegtileEntry {
     int dtype, G, K, MG, T, D;
