@@ -492,6 +492,63 @@ cci_status cci_layer_norm_backward_ex(const void *dy, int64_t lddy, const void *
                                       size_t workspace_bytes, cci_stream_t stream);
 
 /*
+ * cci_rms_norm -- with s = x + residual (x alone without one), for N rows of D:
+ *   h[n][c] = s,  rstd[n] = 1 / sqrt(mean over c of s^2 + eps),  y[n][c] = s * rstd[n] * weight[c]
+ * sums in fp32, y and h each rounded once (y from the unrounded s).
+ *
+ *   x          device, N rows of D of dtype, row stride ldx
+ *   residual   the same with row stride ldr, or NULL
+ *   weight     device fp32 [D] or NULL (1)
+ *   y          device [N][D] of dtype (written)
+ *   h          device [N][D] of dtype (written where there is a residual) or NULL; may be the residual or x
+ *              themselves, packed
+ *   rstd       device fp32 [N] (written; the backward pass reads it) or NULL
+ * N = 0 is valid and enqueues nothing.  eps must be >= 0 (CCI_ERR_VALUE; NaN too).
+ * Errors: CCI_ERR_NULL, CCI_ERR_SHAPE (D < 1 or >= 2^30, N >= 2^31, ldx or ldr < D), CCI_ERR_DTYPE, CCI_ERR_ALIGN,
+ *         CCI_ERR_VALUE, CCI_ERR_CUDA.
+ */
+cci_status cci_rms_norm(const void *x, cci_dtype dtype, int64_t N, int64_t D, int64_t ldx, const void *residual,
+                        int64_t ldr, const float *weight, float eps, void *y, void *h, float *rstd,
+                        cci_stream_t stream);
+
+/*
+ * cci_rms_norm_fp8 -- cci_rms_norm with y in 8 bits (e4m3) for a product in 8 bits:
+ *   scale = max(max |y| / 448, 2^-126),  q = e4m3(y / scale), to the nearest, ties to even
+ * with a scale for each row (group 0) or for each 128 columns of it (group 128; the last of a row may cover
+ * fewer).  y is not rounded before.  NaN in y makes the scale and its columns NaN.
+ *
+ *   q          device [N][D], one byte each (written)
+ *   scales     device fp32 [N] or [N][ceil(D / 128)] (written)
+ * D is a multiple of 8 (CCI_ERR_UNSUPPORTED); rows of x and residual, h, weight and q are on 16 bytes.
+ * Errors: as cci_rms_norm; CCI_ERR_GROUP (group is neither 0 nor 128).
+ */
+cci_status cci_rms_norm_fp8(const void *x, cci_dtype dtype, int64_t N, int64_t D, int64_t ldx, const void *residual,
+                            int64_t ldr, const float *weight, float eps, int group, void *q, float *scales, void *h,
+                            float *rstd, cci_stream_t stream);
+
+/*
+ * cci_rms_norm_backward -- the gradients of cci_rms_norm, with g = dy * weight and xh = h * rstd:
+ *   dx = rstd * (g - xh * mean over c of g * xh) + dh
+ *   dweight[c] = sum over n of dy * xh
+ * dx is the gradient of x and of the residual alike; dh is the gradient that h has besides, from where
+ * it is added again.  Sums over n are added in a fixed order: the same call gives the same bits.
+ *
+ *   dy         device, N rows of D of dtype, row stride lddy
+ *   h          as the forward call wrote it (x where it had no residual), row stride ldh
+ *   dh         the same with row stride lddh, or NULL (0)
+ *   rstd, weight as in the forward call
+ *   dx         device [N][D] of dtype (written)
+ *   dweight    device fp32 [D] (written; zeros for N = 0) or NULL
+ *   workspace  device, 16-byte aligned, cci_rms_norm_workspace_size(N, D) bytes (which depends on the
+ *              current device's number of SMs); overwritten
+ * Errors: as cci_rms_norm; CCI_ERR_WORKSPACE.
+ */
+size_t cci_rms_norm_workspace_size(int64_t N, int64_t D);
+cci_status cci_rms_norm_backward(const void *dy, int64_t lddy, const void *h, int64_t ldh, const void *dh, int64_t lddh,
+                                 cci_dtype dtype, int64_t N, int64_t D, const float *rstd, const float *weight, void *dx,
+                                 float *dweight, void *workspace, size_t workspace_bytes, cci_stream_t stream);
+
+/*
  * cci_token_logprobs -- for N rows of V logits x, each with a token t:
  *   logp[n]    = x[t] - log sum exp(x)
  *   entropy[n] = - sum over v of p_v log p_v, p the row's softmax
@@ -538,6 +595,58 @@ cci_status cci_token_logprobs_backward(const void *logits, cci_dtype dtype, int6
                                        const float *stats, const int64_t *tokens, int64_t ignore_index,
                                        const float *dlogp, const float *entropy, const float *dentropy,
                                        void *dlogits, int64_t lddx, uint32_t *dev_status, cci_stream_t stream);
+
+/*
+ * cci_distillation_loss -- what a student's logits x are off a teacher's word on k tokens of each of N rows,
+ * z = x / T and p = softmax(z) over all V:
+ *   loss[n] = - sum over j of q_j log p[idx_j]                          (tail 0)
+ *             with q = softmax over the listed of t_j / T
+ *   loss[n] = - sum over j of q_j log p[idx_j] - q_rest log p_rest      (tail 1)
+ *             with q_j = exp(t_j): t are the teacher's log probabilities, at temperature T already,
+ *             q_rest = max(1 - sum q, 0) and p_rest = sum of p over what is not listed
+ * the teacher's cross entropy against the student: its divergence and the teacher's own entropy, which has no
+ * gradient.  The lists are those of cci_token_logprobs on the teacher's logits.  It is not multiplied
+ * by T^2: the gradient's dloss is the place for that.
+ *   stats[n] = (max z, log sum exp(z - max), log of that sum over what is not listed,
+ *               tail: sum q, else: log sum exp(t_j / T))
+ * An index of -1 lists nothing, whatever its t; a row that lists nothing has loss 0 and no gradient.  t_j may
+ * be -inf (q_j = 0, and listed).  A listed logit of -inf with q_j > 0 makes the loss inf.  Where no unlisted logit is
+ * above -inf, the rest takes no part (q_rest counts as 0).  NaN or +inf in a row makes its loss NaN.  Any other
+ * index outside [0, V), or one that a row lists twice, sets CCI_ERR_INDEX in dev_status and makes the row's loss, and
+ * its gradient, NaN.
+ *
+ *   logits     device, N rows of V of dtype, row stride ldx
+ *   top_idx    device int32 [N][k]; top_logp device fp32 [N][k]
+ *   k          1 .. min(V, CCI_MAX_TEACHER)
+ *   temperature T > 0, finite
+ *   loss       device fp32 [N]; stats device fp32 [N][4], 16-byte aligned (written)
+ *   dev_status device uint32 or NULL
+ * N = 0 is valid and enqueues nothing.
+ * Errors: CCI_ERR_NULL, CCI_ERR_SHAPE (V < 1 or > 2^24, N >= 2^28, N rows of V / 2048 blocks or more than 2^31, ldx < V,
+ *         k out of range), CCI_ERR_DTYPE, CCI_ERR_VALUE (temperature), CCI_ERR_ALIGN, CCI_ERR_CUDA.
+ */
+#define CCI_MAX_TEACHER 128
+cci_status cci_distillation_loss(const void *logits, cci_dtype dtype, int64_t N, int64_t V, int64_t ldx,
+                                 const int32_t *top_idx, const float *top_logp, int k, float temperature, int tail,
+                                 float *loss, float *stats, uint32_t *dev_status, cci_stream_t stream);
+
+/*
+ * cci_distillation_loss_backward -- the gradient of cci_distillation_loss to the logits:
+ *   dlogits[n][v] = dloss[n] / T * (Q p_v - q_v)            for the listed, Q = sum q + q_rest
+ *                   dloss[n] / T * (Q p_v - q_rest r_v)     for others, r_v = p_v / p_rest (tail 0: Q p_v)
+ * Rows of -inf alone and rows that list nothing get 0.
+ *
+ *   dloss      device fp32 [N]; logits, top_idx, top_logp, k, temperature, tail as in the forward call
+ *   stats      as it wrote them
+ *   dlogits    device, N rows of V of dtype, row stride lddx (written; may be the logits themselves, with
+ *              the same stride).  Rows at the same offset from a 16-byte boundary as the logits' are
+ *              written in whole vectors
+ * Errors: as cci_distillation_loss; CCI_ERR_SHAPE also for lddx < V.
+ */
+cci_status cci_distillation_loss_backward(const float *dloss, const void *logits, cci_dtype dtype, int64_t N, int64_t V,
+                                          int64_t ldx, const int32_t *top_idx, const float *top_logp, int k,
+                                          float temperature, int tail, const float *stats, void *dlogits, int64_t lddx,
+                                          cci_stream_t stream);
 
 /*
  * cci_gated_linear -- the gated feed-forward block's two projections, activation and

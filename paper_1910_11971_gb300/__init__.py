@@ -87,6 +87,14 @@ SIGNATURES = {
                                        ctypes.c_size_t, _P]),
     "cci_gated_linear_backward": (_I32, [_P, _P, _I32, _I64, _I64, _P, _P, _I64, _I32, _P, _P, _P, _P, _P, _U32P, _P,
                                          ctypes.c_size_t, _P]),
+    "cci_distillation_loss": (_I32, [_P, _I32, _I64, _I64, _I64, _P, _P, _I32, ctypes.c_float, _I32, _P, _P, _U32P, _P]),
+    "cci_distillation_loss_backward": (_I32, [_P, _P, _I32, _I64, _I64, _I64, _P, _P, _I32, ctypes.c_float, _I32, _P, _P,
+                                              _I64, _P]),
+    "cci_rms_norm": (_I32, [_P, _I32, _I64, _I64, _I64, _P, _I64, _P, ctypes.c_float, _P, _P, _P, _P]),
+    "cci_rms_norm_fp8": (_I32, [_P, _I32, _I64, _I64, _I64, _P, _I64, _P, ctypes.c_float, _I32, _P, _P, _P, _P, _P]),
+    "cci_rms_norm_workspace_size": (ctypes.c_size_t, [_I64, _I64]),
+    "cci_rms_norm_backward": (_I32, [_P, _I64, _P, _I64, _P, _I64, _I32, _I64, _I64, _P, _P, _P, _P, _P,
+                                     ctypes.c_size_t, _P]),
     "cci_head_workspace_size": (ctypes.c_size_t, [_I32, _I32, _I64, _I64, _I64]),
     "cci_linear_cross_entropy": (_I32, [_P, _I32, _I64, _I64, _P, _I64, _P, _I64, _P, _P, _U32P, _P, ctypes.c_size_t,
                                         _P]),
@@ -601,6 +609,87 @@ def layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, mean: torch.Tensor, r
     return dx, dw, db
 
 
+def _summed(x: torch.Tensor, residual: Optional[torch.Tensor], h: Optional[torch.Tensor]):
+    """(device, N, D, ldx, residual's address and stride, h) of a root-mean-square norm's rows."""
+    index = _device(x, "x")
+    ld = _rows(x, "x")
+    N, D = x.shape
+    if residual is None:
+        if h is not None:
+            raise ValueError("h is written only where there is a residual")
+        return index, N, D, ld, None, D, None
+    ldr = _rows(residual, "residual", index)
+    if residual.shape != x.shape or residual.dtype != x.dtype:
+        raise ValueError("residual must have x's shape and dtype")
+    if h is None:
+        h = torch.empty((N, D), dtype=x.dtype, device=x.device)
+    else:
+        _like(h, (N, D), x.dtype, "h", index)
+    return index, N, D, ld, residual.data_ptr(), ldr, h
+
+
+def rms_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, *, residual: Optional[torch.Tensor] = None,
+             eps: float = 1e-5, out: Optional[torch.Tensor] = None, h: Optional[torch.Tensor] = None):
+    """(y, h, rstd) of the rows of x[N][D] (``cci_rms_norm``): h = x + residual and y = (x + residual) rstd weight in
+    x's dtype, rstd the fp32 1 / sqrt(mean square + eps) of each row; without a residual h is x itself.  ``weight`` is
+    fp32 [D]; x and residual may have row strides.  ``out`` takes y and ``h`` takes h, which may be the
+    residual (the residual stream updated in place)."""
+    index, N, D, ld, rp, ldr, h = _summed(x, residual, h)
+    if out is not None:
+        _like(out, (N, D), x.dtype, "out", index)
+    y = out if out is not None else torch.empty((N, D), dtype=x.dtype, device=x.device)
+    rstd = torch.empty(N, dtype=torch.float32, device=x.device)
+    _check(lib().cci_rms_norm(x.data_ptr(), _dtype_code(x), N, D, ld, rp, ldr, _vec(weight, D, "weight", index), eps,
+                              y.data_ptr(), None if h is None else h.data_ptr(), rstd.data_ptr(),
+                              torch._C._cuda_getCurrentRawStream(index)), "cci_rms_norm")
+    return y, x if h is None else h, rstd
+
+
+def rms_norm_fp8(x: torch.Tensor, weight: Optional[torch.Tensor] = None, *, residual: Optional[torch.Tensor] = None,
+                 group: int = 0, eps: float = 1e-5, h: Optional[torch.Tensor] = None):
+    """(q, scales, h, rstd): ``rms_norm`` with y in 8 bits (``cci_rms_norm_fp8``), y = q * scale: q [N][D] of
+    ``torch.float8_e4m3fn``, fp32 scales [N][1] (``group`` 0) or one per 128 columns, [N][ceil(D / 128)] (``group``
+    128).  D a multiple of 8."""
+    index, N, D, ld, rp, ldr, h = _summed(x, residual, h)
+    q = torch.empty((N, D), dtype=torch.float8_e4m3fn, device=x.device)
+    scales = torch.empty((N, -(-D // 128) if group else 1), dtype=torch.float32, device=x.device)
+    rstd = torch.empty(N, dtype=torch.float32, device=x.device)
+    _check(lib().cci_rms_norm_fp8(x.data_ptr(), _dtype_code(x), N, D, ld, rp, ldr, _vec(weight, D, "weight", index), eps,
+                                  group, q.data_ptr(), scales.data_ptr(), None if h is None else h.data_ptr(),
+                                  rstd.data_ptr(), torch._C._cuda_getCurrentRawStream(index)), "cci_rms_norm_fp8")
+    return q, scales, x if h is None else h, rstd
+
+
+def rms_norm_backward(dy: torch.Tensor, h: torch.Tensor, rstd: torch.Tensor, weight: Optional[torch.Tensor] = None, *,
+                      dh: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
+                      workspace: Optional[torch.Tensor] = None):
+    """(dx, dweight) of ``rms_norm`` (``cci_rms_norm_backward``) from the gradient of y and, with ``dh``, the one that
+    h has besides: dx, of x and of the residual alike, in h's dtype, the weight's gradient fp32 [D], whether or not the
+    forward call had one."""
+    index = _device(h, "h")
+    ldh, lddy = _rows(h, "h"), _rows(dy, "dy", index)
+    N, D = h.shape
+    if dy.shape != h.shape or dy.dtype != h.dtype:
+        raise ValueError("dy must have h's shape and dtype")
+    lddh = D
+    if dh is not None:
+        lddh = _rows(dh, "dh", index)
+        if dh.shape != h.shape or dh.dtype != h.dtype:
+            raise ValueError("dh must have h's shape and dtype")
+    if out is not None:
+        _like(out, (N, D), h.dtype, "out", index)
+    dx = out if out is not None else torch.empty((N, D), dtype=h.dtype, device=h.device)
+    dw = torch.empty(D, dtype=torch.float32, device=h.device)
+    if workspace is None:
+        workspace = _workspace(_rms_bytes(N, D, index), h.device)
+    wp, wb = (None, 0) if workspace is None else _space(workspace, index)
+    _check(lib().cci_rms_norm_backward(dy.data_ptr(), lddy, h.data_ptr(), ldh, None if dh is None else dh.data_ptr(),
+                                       lddh, _dtype_code(h), N, D, _vec(rstd, N, "rstd", index),
+                                       _vec(weight, D, "weight", index), dx.data_ptr(), dw.data_ptr(), wp, wb,
+                                       torch._C._cuda_getCurrentRawStream(index)), "cci_rms_norm_backward")
+    return dx, dw
+
+
 def token_logprobs(logits: torch.Tensor, tokens: torch.Tensor, *, top: int = 0, ignore_index: int = -100,
                    status: Optional[torch.Tensor] = None):
     """(logp, entropy, stats, top_logp, top_idx) of the rows of logits[N][V] and one token (int64) each
@@ -656,6 +745,67 @@ def token_logprobs_backward(logits: torch.Tensor, tokens: Optional[torch.Tensor]
                                              None if status is None else _status_word(status, index),
                                              torch._C._cuda_getCurrentRawStream(index)), "cci_token_logprobs_backward")
     return out
+
+
+def distillation_loss(logits: torch.Tensor, top_idx: torch.Tensor, top_logp: torch.Tensor, *, temperature: float = 1.0,
+                      tail: bool = False, status: Optional[torch.Tensor] = None):
+    """(loss, stats) of a student's logits[N][V] against a teacher's top_idx (int32) and top_logp (fp32) [N][k]
+    (``cci_distillation_loss``; the lists of ``token_logprobs(..., top=k)`` on the teacher's logits, k at most 128): the
+    cross entropy of the teacher's listed probabilities, renormalised at the temperature or, with ``tail``, as they are
+    with all that is not listed as one more outcome; index -1 lists nothing.  ``stats`` [N][4] is for the backward
+    pass.  The logits may have a row stride."""
+    index = _device(logits, "logits")
+    ld = _rows(logits, "logits")
+    N, V = logits.shape
+    ip, vp, k = _lists(top_idx, top_logp, N, index)
+    loss = torch.empty(N, dtype=torch.float32, device=logits.device)
+    stats = torch.empty((N, 4), dtype=torch.float32, device=logits.device)
+    _check(lib().cci_distillation_loss(logits.data_ptr(), _dtype_code(logits), N, V, ld, ip, vp, k, temperature, int(tail),
+                                       loss.data_ptr(), stats.data_ptr(),
+                                       None if status is None else _status_word(status, index),
+                                       torch._C._cuda_getCurrentRawStream(index)), "cci_distillation_loss")
+    return loss, stats
+
+
+def distillation_loss_backward(dloss: torch.Tensor, logits: torch.Tensor, top_idx: torch.Tensor, top_logp: torch.Tensor,
+                               stats: torch.Tensor, *, temperature: float = 1.0, tail: bool = False,
+                               out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """The gradient of ``distillation_loss`` to the logits, in their dtype (``cci_distillation_loss_backward``), from the
+    fp32 gradient of each row's loss and the forward call's stats.  Rows padded by up to 64 logits keep their stride in
+    the result, unless ``out`` is given; ``out`` may be the logits."""
+    index = _device(logits, "logits")
+    ld = _rows(logits, "logits")
+    N, V = logits.shape
+    ip, vp, k = _lists(top_idx, top_logp, N, index)
+    out, ldd = _like_logits(logits, ld, out, index)
+    _check(lib().cci_distillation_loss_backward(_vec(dloss, N, "dloss", index), logits.data_ptr(), _dtype_code(logits), N,
+                                                V, ld, ip, vp, k, temperature, int(tail),
+                                                _vec(stats, 4 * N, "stats", index), out.data_ptr(), ldd,
+                                                torch._C._cuda_getCurrentRawStream(index)),
+           "cci_distillation_loss_backward")
+    return out
+
+
+def _lists(top_idx: torch.Tensor, top_logp: torch.Tensor, N: int, index: int):
+    """Addresses and width of a teacher's lists [N][k]."""
+    if top_idx.dim() != 2 or top_idx.shape[0] != N or top_logp.shape != top_idx.shape:
+        raise ValueError(f"top_idx and top_logp must be ({N}, k)")
+    k = top_idx.shape[1]
+    return _vec(top_idx, N * k, "top_idx", index, torch.int32), _vec(top_logp, N * k, "top_logp", index), k
+
+
+def _like_logits(logits: torch.Tensor, ld: int, out: Optional[torch.Tensor], index: int):
+    """A gradient's rows for logits of row stride ld, and their stride."""
+    N, V = logits.shape
+    if out is None:
+        # a padded row's stride (rows then start on the same 16-byte words), not that of a wide matrix' slice
+        ldd = ld if ld <= V + 64 else V
+        out = torch.empty((N, ldd), dtype=logits.dtype, device=logits.device)
+        return (out[:, :V] if ldd != V else out), ldd
+    ldd = _rows(out, "out", index)
+    if out.shape != logits.shape or out.dtype != logits.dtype:
+        raise ValueError("out must have the logits' shape and dtype")
+    return out, ldd
 
 
 def _act_code(act: str) -> int:
@@ -850,6 +1000,12 @@ def _like(t: torch.Tensor, shape, dtype: torch.dtype, name: str, index: int) -> 
 def _norm_bytes(N: int, D: int, device_index: int) -> int:
     with torch.cuda.device(device_index):
         return int(lib().cci_layer_norm_workspace_size(N, D))
+
+
+@functools.lru_cache(maxsize=4096)
+def _rms_bytes(N: int, D: int, device_index: int) -> int:
+    with torch.cuda.device(device_index):
+        return int(lib().cci_rms_norm_workspace_size(N, D))
 
 
 def kernel_name(dtype: torch.dtype, Cin: int, R: int, Cout: int, G: int, K: int,

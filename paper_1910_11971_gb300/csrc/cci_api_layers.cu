@@ -311,3 +311,131 @@ cci_status cci_linear_cross_entropy_backward(const float *dloss, const void *X, 
 }
 
 }  // extern "C"
+
+namespace {
+
+// sizes and pointers of both forward forms of the root-mean-square norm
+cci_status check_rms(int dtype, int64_t N, int64_t D, const void *x, int64_t ldx, const void *residual, int64_t ldr,
+                     const float *weight, float eps, const void *y, const void *h, const float *rstd)
+{
+    if (!valid_dtype(dtype)) return CCI_ERR_DTYPE;
+    if (N > 0 && (!x || !y)) return CCI_ERR_NULL;
+    // a block takes rows, or a row where it is long; columns are counted in 32 bits
+    if (!rows_ok(N, D, ldx) || (residual && !rows_ok(N, D, ldr)) || N >= kMaxRows || D >= kMaxRows / 2) return CCI_ERR_SHAPE;
+    if (!(eps >= 0.0f)) return CCI_ERR_VALUE;  // also NaN
+    const size_t es = elem_size(dtype);
+    if (!aligned(x, es) || !aligned(residual, es) || !aligned(h, es) || !aligned(weight, 4) || !aligned(rstd, 4))
+        return CCI_ERR_ALIGN;
+    return CCI_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+cci_status cci_rms_norm(const void *x, cci_dtype dtype, int64_t N, int64_t D, int64_t ldx, const void *residual,
+                        int64_t ldr, const float *weight, float eps, void *y, void *h, float *rstd, cci_stream_t stream)
+{
+    const cci_status st = check_rms(dtype, N, D, x, ldx, residual, ldr, weight, eps, y, h, rstd);
+    if (st != CCI_OK) return st;
+    if (!aligned(y, elem_size(dtype))) return CCI_ERR_ALIGN;
+    if (N == 0) return CCI_OK;
+    return to_status(launch_rms_norm(x, ldx, residual, ldr, dtype, N, D, weight, eps, y, h, rstd, nullptr, 0,
+                                     as_stream(stream)));
+}
+
+cci_status cci_rms_norm_fp8(const void *x, cci_dtype dtype, int64_t N, int64_t D, int64_t ldx, const void *residual,
+                            int64_t ldr, const float *weight, float eps, int group, void *q, float *scales, void *h,
+                            float *rstd, cci_stream_t stream)
+{
+    const cci_status st = check_rms(dtype, N, D, x, ldx, residual, ldr, weight, eps, q, h, rstd);
+    if (st != CCI_OK) return st;
+    if (N > 0 && !scales) return CCI_ERR_NULL;
+    if (group != 0 && group != 128) return CCI_ERR_GROUP;
+    if (D % 8 != 0) return CCI_ERR_UNSUPPORTED;
+    const int64_t es = static_cast<int64_t>(elem_size(dtype));
+    if (!aligned(x, 16) || ldx * es % 16 != 0 || !aligned(residual, 16) || (residual && ldr * es % 16 != 0) ||
+        !aligned(h, 16) || !aligned(weight, 16) || !aligned(q, 16) || !aligned(scales, 4))
+        return CCI_ERR_ALIGN;
+    if (N == 0) return CCI_OK;
+    const int groups = group == 0 ? 1 : static_cast<int>((D + 127) / 128);
+    return to_status(launch_rms_norm(x, ldx, residual, ldr, dtype, N, D, weight, eps, q, h, rstd, scales, groups,
+                                     as_stream(stream)));
+}
+
+size_t cci_rms_norm_workspace_size(int64_t N, int64_t D)
+{
+    return N < 1 || D < 1 || N >= kMaxRows || D >= kMaxRows / 2 ? 0 : rms_norm_workspace(N, D);
+}
+
+cci_status cci_rms_norm_backward(const void *dy, int64_t lddy, const void *h, int64_t ldh, const void *dh, int64_t lddh,
+                                 cci_dtype dtype, int64_t N, int64_t D, const float *rstd, const float *weight, void *dx,
+                                 float *dweight, void *workspace, size_t workspace_bytes, cci_stream_t stream)
+{
+    if (!valid_dtype(dtype)) return CCI_ERR_DTYPE;
+    if (N > 0 && (!dy || !h || !rstd || !dx)) return CCI_ERR_NULL;
+    if (!rows_ok(N, D, lddy) || !rows_ok(N, D, ldh) || (dh && !rows_ok(N, D, lddh)) || N >= kMaxRows || D >= kMaxRows / 2)
+        return CCI_ERR_SHAPE;
+    const size_t es = elem_size(dtype);
+    if (!aligned(dy, es) || !aligned(h, es) || !aligned(dh, es) || !aligned(dx, es) || !aligned(rstd, 4) ||
+        !aligned(weight, 4) || !aligned(dweight, 4))
+        return CCI_ERR_ALIGN;
+    const size_t need = N > 0 ? rms_norm_workspace(N, D) : 0;
+    if (need > 0 && (!workspace || !aligned(workspace, 16) || workspace_bytes < need)) return CCI_ERR_WORKSPACE;
+    return to_status(launch_rms_norm_backward(dy, lddy, h, ldh, dh, lddh, dtype, N, D, rstd, weight, dx, dweight,
+                                              static_cast<float *>(workspace), as_stream(stream)));
+}
+
+}  // extern "C"
+
+namespace {
+
+// sizes and pointers that both calls of a distillation have
+cci_status check_distillation(int dtype, int64_t N, int64_t V, const void *logits, int64_t ldx, const int32_t *idx,
+                              const float *value, int k, float temperature, const float *stats)
+{
+    if (!valid_dtype(dtype)) return CCI_ERR_DTYPE;
+    if (N > 0 && (!logits || !idx || !value || !stats)) return CCI_ERR_NULL;
+    // a row takes up to eight blocks forward, and a block for 2048 logits or more backward
+    if (!rows_ok(N, V, ldx) || V > kMaxLogits || N >= kMaxRows / 8 || N * ((V + 2054) / 2048) >= kMaxRows || k < 1 ||
+        k > CCI_MAX_TEACHER || k > V)
+        return CCI_ERR_SHAPE;
+    if (!(temperature > 0.0f) || temperature > 3.4e38f) return CCI_ERR_VALUE;  // also NaN
+    if (!aligned(logits, elem_size(dtype)) || !aligned(idx, 4) || !aligned(value, 4) || !aligned(stats, 16))
+        return CCI_ERR_ALIGN;
+    return CCI_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+cci_status cci_distillation_loss(const void *logits, cci_dtype dtype, int64_t N, int64_t V, int64_t ldx,
+                                 const int32_t *top_idx, const float *top_logp, int k, float temperature, int tail,
+                                 float *loss, float *stats, uint32_t *dev_status, cci_stream_t stream)
+{
+    const cci_status st = check_distillation(dtype, N, V, logits, ldx, top_idx, top_logp, k, temperature, stats);
+    if (st != CCI_OK) return st;
+    if (N > 0 && !loss) return CCI_ERR_NULL;
+    if (!aligned(loss, 4)) return CCI_ERR_ALIGN;
+    if (N == 0) return CCI_OK;
+    return to_status(launch_distillation(logits, dtype, N, V, ldx, top_idx, top_logp, k, temperature, tail != 0, loss,
+                                         stats, dev_status, as_stream(stream)));
+}
+
+cci_status cci_distillation_loss_backward(const float *dloss, const void *logits, cci_dtype dtype, int64_t N, int64_t V,
+                                          int64_t ldx, const int32_t *top_idx, const float *top_logp, int k,
+                                          float temperature, int tail, const float *stats, void *dlogits, int64_t lddx,
+                                          cci_stream_t stream)
+{
+    const cci_status st = check_distillation(dtype, N, V, logits, ldx, top_idx, top_logp, k, temperature, stats);
+    if (st != CCI_OK) return st;
+    if (N > 0 && (!dloss || !dlogits)) return CCI_ERR_NULL;
+    if (!rows_ok(N, V, lddx)) return CCI_ERR_SHAPE;
+    if (!aligned(dloss, 4) || !aligned(dlogits, elem_size(dtype))) return CCI_ERR_ALIGN;
+    if (N == 0) return CCI_OK;
+    return to_status(launch_distillation_backward(dloss, logits, dtype, N, V, ldx, top_idx, top_logp, k, temperature,
+                                                  tail != 0, stats, dlogits, lddx, as_stream(stream)));
+}
+
+}  // extern "C"

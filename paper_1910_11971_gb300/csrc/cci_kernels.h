@@ -94,6 +94,24 @@ size_t gated_workspace(int dtype, int64_t N, int64_t D, int64_t F, int call);
 cudaError_t launch_gated(const GatedArgs &a, cudaStream_t stream);
 cudaError_t launch_gated_backward(const GatedArgs &a, cudaStream_t stream);
 
+// distillation from a teacher's top logits (cci_distill.cu)
+cudaError_t launch_distillation(const void *x, int dtype, int64_t N, int64_t V, int64_t ldx, const int32_t *idx,
+                                const float *value, int k, float T, int tail, float *loss, float *stats,
+                                uint32_t *status, cudaStream_t stream);
+cudaError_t launch_distillation_backward(const float *dloss, const void *x, int dtype, int64_t N, int64_t V, int64_t ldx,
+                                         const int32_t *idx, const float *value, int k, float T, int tail,
+                                         const float *stats, void *dx, int64_t lddx, cudaStream_t stream);
+
+// root-mean-square norm (cci_rms.cu); scales: y is e4m3, with `groups` scales a row (null: y of the rows' type).
+// part: the backward pass' workspace of rms_norm_workspace bytes (N >= 1); dw may be null
+size_t rms_norm_workspace(int64_t N, int64_t D);
+cudaError_t launch_rms_norm(const void *x, int64_t ldx, const void *residual, int64_t ldr, int dtype, int64_t N, int64_t D,
+                            const float *w, float eps, void *y, void *h, float *rstd, float *scales, int groups,
+                            cudaStream_t stream);
+cudaError_t launch_rms_norm_backward(const void *dy, int64_t lddy, const void *h, int64_t ldh, const void *dh, int64_t lddh,
+                                     int dtype, int64_t N, int64_t D, const float *rstd, const float *w, void *dx, float *dw,
+                                     float *part, cudaStream_t stream);
+
 // softmax cross entropy from a head's inputs (cci_head*.cu).  backward: dX and dW may each be null.  workspace:
 // head_workspace bytes for the call (a cci_head_call)
 struct HeadArgs {
