@@ -41,7 +41,8 @@ struct Args {
     const float *dloss;
     void *dx;
     int64_t lddx;
-    int parts, chunks;    // blocks of a row, forward and backward
+    int parts;            // blocks of a row, forward
+    int chunks, steps;    // warps of a row, backward, and their steps of 1024 logits
 };
 
 __device__ __forceinline__ float neg_inf() { return __int_as_float(0xff800000); }
@@ -62,16 +63,26 @@ __device__ __forceinline__ int shift_of(const T *row)
     return static_cast<int>(reinterpret_cast<uintptr_t>(row) / sizeof(T)) & (16 / sizeof(T) - 1);
 }
 
-// eight logits from e on; -inf outside of the row
+// eight logits from e on as they lie in memory; -inf outside of the row
 template <typename T>
-__device__ __forceinline__ void load_group(const T *row, int e, int V, float (&f)[8])
+__device__ __forceinline__ row::Raw<T, 8> load_group(const T *row, int e, int V)
 {
-    if (e >= 0 && e + 8 <= V) {
-        row::unpack<T, 8>(row::load_once<T, 8>(row + e), f);
-    } else {
+    if (e >= 0 && e + 8 <= V) return row::load_once<T, 8>(row + e);
+    row::Raw<T, 8> raw;
+    uint32_t w[2 * sizeof(T)];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) f[j] = e + j >= 0 && e + j < V ? row::to_f32(row[e + j]) : neg_inf();
+    for (int j = 0; j < 8; ++j) {
+        const bool in = e + j >= 0 && e + j < V;
+        if constexpr (sizeof(T) == 4) {
+            w[j] = in ? __float_as_uint(row[e + j]) : 0xff800000u;
+        } else {
+            const uint32_t v = in ? row[e + j] : 0xff80u;
+            w[j / 2] = j % 2 ? w[j / 2] | v << 16 : v;
+        }
     }
+#pragma unroll
+    for (int i = 0; i < static_cast<int>(sizeof(T)) / 2; ++i) raw.w[i] = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
+    return raw;
 }
 
 struct Sums {
@@ -142,41 +153,52 @@ __global__ void __launch_bounds__(TPB) loss_kernel(const Args a)
         }
         __syncthreads();
         const uint8_t *mask = reinterpret_cast<const uint8_t *>(bits);
-        // the bounds are the same for a warp's lanes, so that they find their common maximum together
-        for (int g = g0 + (t & ~31); g < g1; g += kU * TPB) {
+        // the bounds are the same for a warp's lanes, so that they find their common maximum together; the next groups
+        // are on their way while these are summed
+        row::Raw<T, 8> raw[kU];
+        auto load = [&](int g) {
+#pragma unroll
+            for (int u = 0; u < kU; ++u) {
+                const int q = g + u * TPB + lane;
+                raw[u] = load_group(x, q < g1 ? 8 * q - s : V, V);
+            }
+        };
+        int g = g0 + (t & ~31);
+        if (g < g1) load(g);
+        for (; g < g1; g += kU * TPB) {
             float f[kU][8];
+#pragma unroll
+            for (int u = 0; u < kU; ++u) row::unpack<T, 8>(raw[u], f[u]);
+            if (g + kU * TPB < g1) load(g + kU * TPB);
             float top = neg_inf();
 #pragma unroll
             for (int u = 0; u < kU; ++u) {
                 const int q = g + u * TPB + lane;
-                if (q < g1) {
-                    load_group(x, 8 * q - s, V, f[u]);
-                    const uint32_t m = mask[q - g0];
-                    if (m) {
+                const uint32_t m = q < g1 ? mask[q - g0] : 0u;
+                if (m) {
 #pragma unroll
-                        for (int j = 0; j < 8; ++j) f[u][j] = m >> j & 1u ? neg_inf() : f[u][j];
-                    }
-                } else {
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) f[u][j] = neg_inf();
+                    for (int j = 0; j < 8; ++j) f[u][j] = m >> j & 1u ? neg_inf() : f[u][j];
                 }
-            }
-#pragma unroll
-            for (int u = 0; u < kU; ++u)
 #pragma unroll
                 for (int j = 0; j < 8; ++j) top = fmaxf(top, f[u][j]);
+            }
             asm volatile("redux.sync.max.f32 %0, %0, 0xffffffff;" : "+f"(top));
             if (top > sums.m) {
                 sums.s = sums.s == 0.f ? 0.f : sums.s * ex2((sums.m - top) * c);
                 sums.m = top;
             }
             const float from = ref_of(sums.m);
-            float e[4] = {};
+            const unsigned long long neg = pack2(-from, -from), c2 = pack2(c, c);
+            unsigned long long e[2] = {};
 #pragma unroll
             for (int u = 0; u < kU; ++u)
 #pragma unroll
-                for (int j = 0; j < 8; ++j) e[j & 3] += ex2((f[u][j] - from) * c);
-            sums.s += (e[0] + e[1]) + (e[2] + e[3]);
+                for (int j = 0; j < 8; j += 2) {
+                    const unsigned long long y = row::mul2(row::add2(pack2(f[u][j], f[u][j + 1]), neg), c2);
+                    e[j / 2 & 1] = row::add2(e[j / 2 & 1], pack2(ex2(lo_of(y)), ex2(hi_of(y))));
+                }
+            const unsigned long long both = row::add2(e[0], e[1]);
+            sums.s += lo_of(both) + hi_of(both);
         }
     }
 #pragma unroll
@@ -258,37 +280,33 @@ __global__ void __launch_bounds__(TPB) loss_kernel(const Args a)
     }
 }
 
-// ---- gradient: a block takes kU groups a thread of a row ----
-template <typename T, int TPB>
-__global__ void __launch_bounds__(TPB) gradient_kernel(const Args a)
+// ---- gradient: a warp takes one to four steps of 128 groups of a row by itself; the next step's logits are on their way while
+// it finds its listed ones, once for all steps (4096 x 50001 bf16, k = 64: 224 us where a block of 256 threads waited for
+// them, 180 with one step a warp) ----
+template <typename T>
+__global__ void __launch_bounds__(256) gradient_kernel(const Args a)
 {
-    constexpr int kU = 4;
-    const int t = threadIdx.x;
-    const int64_t n = blockIdx.x / a.chunks;
-    const int chunk = static_cast<int>(blockIdx.x % a.chunks);
+    constexpr int kU = 4, kOwn = kMaxListed / 32;
+    const int lane = threadIdx.x & 31;
+    const int64_t w = static_cast<int64_t>(blockIdx.x) * 8 + (threadIdx.x >> 5), n = w / a.chunks;
+    if (n >= a.N) return;
+    const int chunk = static_cast<int>(w - n * a.chunks);
     const T *x = static_cast<const T *>(a.x) + n * a.ldx;
     T *dx = static_cast<T *>(a.dx) + n * a.lddx;
-    const int s = shift_of(x), V = a.V, g0 = chunk * kU * TPB;
-    const int64_t lo = 8 * static_cast<int64_t>(g0) - s, hi = lo + 8 * kU * TPB;
+    const int s = shift_of(x), V = a.V, lo = chunk * a.steps * 256 * kU - s;
+    const int hi = lo + a.steps * 256 * kU < V ? lo + a.steps * 256 * kU : V;
     const float c = 1.f / a.T;
-    float f[kU][8];
+    row::Raw<T, 8> next[kU];
+    auto load = [&](int e0) {
 #pragma unroll
-    for (int u = 0; u < kU; ++u) {
-        const int64_t e = lo + 8 * (u * TPB + t);
-        if (e < V) load_group(x, static_cast<int>(e), V, f[u]);
-    }
+        for (int u = 0; u < kU; ++u) {
+            const int e = e0 + 8 * (32 * u + lane);
+            next[u] = load_group(x, e < V ? e : V, V);
+        }
+    };
+    load(lo);
     const float4 st = reinterpret_cast<const float4 *>(a.stats)[n];
     const float weight = a.dloss[n] / a.T, m = ref_of(st.x), log_s = st.y, log_rest = st.z;
-    // the listed logits of this block
-    constexpr int kOwn = kMaxListed / TPB < 1 ? 1 : kMaxListed / TPB;
-    int32_t at[kOwn];
-    float own[kOwn];
-#pragma unroll
-    for (int i = 0; i < kOwn; ++i) {
-        const int j = t + i * TPB;
-        at[i] = j < a.k ? a.idx[n * a.k + j] : -1;
-        if (at[i] < lo || at[i] >= hi || at[i] >= V) at[i] = -1;
-    }
     float whole, left = 0.f;  // Q, q_rest
     if (a.tail) {
         left = log_rest == neg_inf() ? 0.f : fmaxf(1.f - st.w, 0.f);
@@ -296,42 +314,59 @@ __global__ void __launch_bounds__(TPB) gradient_kernel(const Args a)
     } else {
         whole = st.w == neg_inf() ? 0.f : 1.f;  // nothing listed
     }
-    const bool empty = st.x == neg_inf();
+    // the listed logits among these, read before any of them is written: dx may be x
+    int at[kOwn];
+    float own[kOwn];
 #pragma unroll
     for (int i = 0; i < kOwn; ++i) {
+        const int j = lane + i * 32;
+        at[i] = j < a.k ? a.idx[n * a.k + j] : -1;
+        if (at[i] < lo || at[i] >= hi) at[i] = -1;
         if (at[i] >= 0) {
-            const float v = a.value[n * a.k + t + i * TPB];
+            const float v = a.value[n * a.k + j];
             const float q = a.tail ? expf(v) : (whole == 0.f ? 0.f : expf(v * c - st.w));
             const float p = expf(fmaf(row::to_f32(x[at[i]]), c, -m) - log_s);
-            own[i] = empty ? 0.f : (p * whole - q) * weight;
+            own[i] = st.x == neg_inf() ? 0.f : (p * whole - q) * weight;
         }
     }
     // off the list: coef exp(z - m - shift).  With a tail, relative to the sum over the unlisted
     const bool some = a.tail && log_rest != neg_inf();
     const float shift = some ? log_rest : log_s;
     const float coef = (some ? whole * expf(log_rest - log_s) - left : whole) * weight;
+    const unsigned long long c2 = pack2(c, c), neg = pack2(-m, -m), l2 = pack2(kLog2e, kLog2e), coef2 = pack2(coef, coef);
     const float minus = -shift * kLog2e;
-    __syncthreads();  // dx may be x: every listed logit has been read
     const bool words = shift_of(dx) == s;
+    __syncwarp();
+    for (int e0 = lo; e0 < hi; e0 += 256 * kU) {
+        row::Raw<T, 8> raw[kU];
 #pragma unroll
-    for (int u = 0; u < kU; ++u) {
-        const int64_t e64 = lo + 8 * (u * TPB + t);
-        if (e64 >= V) continue;
-        const int e = static_cast<int>(e64);
+        for (int u = 0; u < kU; ++u) raw[u] = next[u];
+        if (e0 + 256 * kU < hi) load(e0 + 256 * kU);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const float d = ex2(fmaf(fmaf(f[u][j], c, -m), kLog2e, minus)) * coef;
-            f[u][j] = empty ? 0.f : d;
-        }
-        if (words && e >= 0 && e + 8 <= V) {
-            row::store<T, 8>(dx + e, f[u]);
-        } else {
+        for (int u = 0; u < kU; ++u) {
+            const int e = e0 + 8 * (32 * u + lane);
+            if (e >= V) continue;
+            unsigned long long p[4];
+            row::unpack2<T, 8>(raw[u], p);
 #pragma unroll
-            for (int j = 0; j < 8; ++j)
-                if (e + j >= 0 && e + j < V) row::store<T, 1>(dx + e + j, f[u] + j);
+            for (int j = 0; j < 4; ++j) {
+                unsigned long long d = neg, y = pack2(minus, minus);
+                ffma2(d, p[j], c2);
+                ffma2(y, d, l2);
+                p[j] = row::mul2(pack2(ex2(lo_of(y)), ex2(hi_of(y))), coef2);
+            }
+            if (words && e >= 0 && e + 8 <= V) {
+                row::store2<T, 8>(dx + e, p);
+            } else {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const float v = j % 2 ? hi_of(p[j / 2]) : lo_of(p[j / 2]);
+                    if (e + j >= 0 && e + j < V) row::store<T, 1>(dx + e + j, &v);
+                }
+            }
         }
     }
-    __syncthreads();
+    __syncwarp();
 #pragma unroll
     for (int i = 0; i < kOwn; ++i)
         if (at[i] >= 0) row::store<T, 1>(dx + at[i], own + i);
@@ -369,13 +404,17 @@ cudaError_t launch_loss(Args a, cudaStream_t stream)
     return e == cudaSuccess ? cudaGetLastError() : e;
 }
 
-template <typename T, int TPB>
+template <typename T>
 cudaError_t launch_gradient(Args a, cudaStream_t stream)
 {
-    constexpr int64_t kLogits = 8 * 4 * TPB;
-    a.chunks = static_cast<int>((static_cast<int64_t>(a.V) + 7 + kLogits - 1) / kLogits);
-    if (a.N * a.chunks >= (int64_t(1) << 31)) return cudaErrorInvalidValue;
-    gradient_kernel<T, TPB><<<static_cast<unsigned>(a.N * a.chunks), TPB, 0, stream>>>(a);
+    // four steps a warp where that leaves several rounds of warps
+    const int64_t all = (a.V + 7 + 1023) / 1024;
+    a.steps = 4;
+    while (a.steps > 1 && a.N * ((all + a.steps - 1) / a.steps) < 4 * 24 * static_cast<int64_t>(row::sm_count())) a.steps /= 2;
+    a.chunks = static_cast<int>((all + a.steps - 1) / a.steps);
+    const int64_t blocks = (a.N * a.chunks + 7) / 8;
+    if (blocks >= (int64_t(1) << 31)) return cudaErrorInvalidValue;
+    gradient_kernel<T><<<static_cast<unsigned>(blocks), 256, 0, stream>>>(a);
     return cudaGetLastError();
 }
 
@@ -422,9 +461,7 @@ cudaError_t launch_distillation_backward(const float *dloss, const void *x, int 
     a.dloss = dloss;
     a.dx = dx;
     a.lddx = lddx;
-    if (dtype == CCI_F32)
-        return V <= kShort ? launch_gradient<float, 64>(a, stream) : launch_gradient<float, 256>(a, stream);
-    return V <= kShort ? launch_gradient<uint16_t, 64>(a, stream) : launch_gradient<uint16_t, 256>(a, stream);
+    return dtype == CCI_F32 ? launch_gradient<float>(a, stream) : launch_gradient<uint16_t>(a, stream);
 }
 
 }  // namespace cci
