@@ -103,6 +103,55 @@ struct Part {
     int bad;
 };
 
+// what a row's list says: the largest listed logit and the sum of exp((x - top) / T); the teacher's sum or its normaliser's
+// logarithm, as in stats; and - sum q_j (x_j - top) / T with the sum of those q_j
+struct Listed {
+    float top, sum, given, norm, off, share;
+};
+
+// by a warp, a lane's results those of all
+template <typename T>
+__device__ __forceinline__ Listed listed_of(const Args &a, const T *x, const int32_t *idx, const float *value, int lane)
+{
+    constexpr int kOwn = kMaxListed / 32;
+    int at[kOwn];
+    float z[kOwn], q[kOwn];
+    float top = neg_inf(), best = neg_inf();
+#pragma unroll
+    for (int i = 0; i < kOwn; ++i) {
+        const int j = lane + 32 * i;
+        at[i] = j < a.k ? idx[j] : -1;
+        q[i] = j < a.k ? value[j] : 0.f;
+        z[i] = at[i] >= 0 && at[i] < a.V ? row::to_f32(x[at[i]]) : neg_inf();
+        top = fmaxf(top, z[i]);
+        if (at[i] >= 0) best = fmaxf(best, q[i]);
+    }
+    top = row::warp_max(top);
+    best = row::warp_max(best);
+    Listed r{top, 0.f, 0.f, 0.f, 0.f, 0.f};
+    const float from = ref_of(top), best_from = ref_of(best);
+#pragma unroll
+    for (int i = 0; i < kOwn; ++i) {
+        q[i] = at[i] < 0 ? 0.f : (a.tail ? expf(q[i]) : expf((q[i] - best_from) / a.T));
+        z[i] = (z[i] - from) / a.T;
+        r.given += q[i];
+        if (at[i] >= 0) r.sum += expf(z[i]);
+    }
+    r.given = row::warp_sum(r.given);
+    r.sum = row::warp_sum(r.sum);
+    const float unit = a.tail || r.given == 0.f ? 1.f : 1.f / r.given;
+#pragma unroll
+    for (int i = 0; i < kOwn; ++i) {
+        const float share = q[i] * unit;
+        r.share += share;
+        if (share != 0.f) r.off -= share * z[i];
+    }
+    r.off = row::warp_sum(r.off);
+    r.share = row::warp_sum(r.share);
+    r.norm = a.tail ? r.given : (r.given == 0.f ? neg_inf() : logf(r.given) + best_from / a.T);
+    return r;
+}
+
 template <typename T, int TPB>
 __global__ void __launch_bounds__(TPB) loss_kernel(const Args a)
 {
@@ -116,29 +165,27 @@ __global__ void __launch_bounds__(TPB) loss_kernel(const Args a)
     const int part = static_cast<int>(blockIdx.x % a.parts);
     const T *x = static_cast<const T *>(a.x) + n * a.ldx;
     const int32_t *idx = a.idx + n * a.k;
-    const float *value = a.value + n * a.k;
     const float c = kLog2e / a.T;
     const int s = shift_of(x), V = a.V;
     const int groups = static_cast<int>((static_cast<int64_t>(V) + s + 7) / 8);
     const int each = ((groups + a.parts - 1) / a.parts + 31) / 32 * 32;
     const int first = part * each < groups ? part * each : groups, last = first + each < groups ? first + each : groups;
-    // the first block's: the listed logits and the teacher's values, on their way meanwhile
-    constexpr int kOwn = kMaxListed / 32;
-    int32_t at[kOwn];
-    float said[kOwn], listed[kOwn];
-    if (part == 0 && t < 32) {
-#pragma unroll
-        for (int i = 0; i < kOwn; ++i) {
-            const int j = lane + 32 * i;
-            at[i] = j < a.k ? idx[j] : -1;
-            said[i] = j < a.k ? value[j] : 0.f;
-            listed[i] = at[i] >= 0 && at[i] < V ? row::to_f32(x[at[i]]) : neg_inf();
-        }
-    }
     Sums sums{neg_inf(), 0.f};
+    Listed mine{};
     if (t == 0) bad_flag = 0;
     for (int g0 = first; g0 < last || g0 == first; g0 += kBits / 8) {
         const int g1 = g0 + kBits / 8 < last ? g0 + kBits / 8 : last;
+        // the first groups are on their way while the bits are set
+        row::Raw<T, 8> raw[kU];
+        auto load = [&](int g) {
+#pragma unroll
+            for (int u = 0; u < kU; ++u) {
+                const int q = g + u * TPB + lane;
+                raw[u] = load_group(x, q < g1 ? 8 * q - s : V, V);
+            }
+        };
+        int g = g0 + (t & ~31);
+        if (g < g1) load(g);
         __syncthreads();
         for (int i = t; i < (g1 - g0 + 3) / 4; i += TPB) bits[i] = 0u;
         __syncthreads();
@@ -153,18 +200,9 @@ __global__ void __launch_bounds__(TPB) loss_kernel(const Args a)
         }
         __syncthreads();
         const uint8_t *mask = reinterpret_cast<const uint8_t *>(bits);
+        if (g0 == first && part == 0 && t < 32) mine = listed_of(a, x, idx, a.value + n * a.k, lane);
         // the bounds are the same for a warp's lanes, so that they find their common maximum together; the next groups
         // are on their way while these are summed
-        row::Raw<T, 8> raw[kU];
-        auto load = [&](int g) {
-#pragma unroll
-            for (int u = 0; u < kU; ++u) {
-                const int q = g + u * TPB + lane;
-                raw[u] = load_group(x, q < g1 ? 8 * q - s : V, V);
-            }
-        };
-        int g = g0 + (t & ~31);
-        if (g < g1) load(g);
         for (; g < g1; g += kU * TPB) {
             float f[kU][8];
 #pragma unroll
@@ -225,59 +263,24 @@ __global__ void __launch_bounds__(TPB) loss_kernel(const Args a)
 #pragma unroll
             for (int o = 4; o > 0; o >>= 1)
                 sums = joined(sums, Sums{__shfl_xor_sync(0xffffffffu, sums.m, o), __shfl_xor_sync(0xffffffffu, sums.s, o)}, c);
-            sums.m = __shfl_sync(0xffffffffu, sums.m, 0);
-            sums.s = __shfl_sync(0xffffffffu, sums.s, 0);
         }
     }
-    if (t >= 32) return;
-    // the first warp: the listed join, and the teacher has its say
-    sums.m = __shfl_sync(0xffffffffu, sums.m, 0);
-    sums.s = __shfl_sync(0xffffffffu, sums.s, 0);
-    float top = neg_inf(), best = neg_inf();  // of the listed logits, of the teacher's values
-#pragma unroll
-    for (int i = 0; i < kOwn; ++i) {
-        top = fmaxf(top, listed[i]);
-        if (at[i] >= 0) best = fmaxf(best, said[i]);
-    }
-    top = row::warp_max(top);
-    best = row::warp_max(best);
-    const float m = fmaxf(sums.m, top), from = ref_of(m), best_from = ref_of(best);
-    float of_listed = 0.f, given = 0.f;
-    float q[kOwn];
-#pragma unroll
-    for (int i = 0; i < kOwn; ++i) {
-        q[i] = 0.f;
-        if (at[i] >= 0) {
-            of_listed += expf((listed[i] - from) / a.T);
-            q[i] = a.tail ? expf(said[i]) : expf((said[i] - best_from) / a.T);
-            given += q[i];
-        }
-    }
-    of_listed = row::warp_sum(of_listed);
-    given = row::warp_sum(given);
+    if (t > 0) return;
+    // the listed join, and the teacher has its say
+    const float m = fmaxf(sums.m, mine.top), from = ref_of(m);
     const float rest = sums.s == 0.f ? 0.f : sums.s * ex2((sums.m - from) * c);
-    const float sum = rest + of_listed;
+    const float sum = rest + (mine.sum == 0.f ? 0.f : mine.sum * ex2((mine.top - from) * c));
     const bool empty = m == neg_inf() && sum == 0.f;
     const float log_s = empty ? 0.f : logf(sum), log_rest = logf(rest);
-    const float unit = a.tail || given == 0.f ? 1.f : 1.f / given;
-    float loss = 0.f;
-#pragma unroll
-    for (int i = 0; i < kOwn; ++i)
-        if (at[i] >= 0 && q[i] != 0.f) loss -= q[i] * unit * ((listed[i] - from) / a.T - log_s);
-    loss = row::warp_sum(loss);
+    // no term is below 0: nothing cancels
+    float loss = mine.off + (mine.share == 0.f ? 0.f : mine.share * (log_s - (ref_of(mine.top) - from) / a.T));
     if (a.tail) {
-        const float left = rest == 0.f ? 0.f : fmaxf(1.f - given, 0.f);
+        const float left = rest == 0.f ? 0.f : fmaxf(1.f - mine.given, 0.f);
         if (left > 0.f) loss += left * (log_s - log_rest);
     }
-    if (lane == 0) {
-        if (bad) report(a.status, CCI_ERR_INDEX);
-        float *o = a.stats + 4 * n;
-        a.loss[n] = bad ? nan_f() : loss;
-        o[0] = bad ? nan_f() : m / a.T;
-        o[1] = log_s;
-        o[2] = log_rest;
-        o[3] = a.tail ? given : (given == 0.f ? neg_inf() : logf(given) + best_from / a.T);
-    }
+    if (bad) report(a.status, CCI_ERR_INDEX);
+    a.loss[n] = bad ? nan_f() : loss;
+    reinterpret_cast<float4 *>(a.stats)[n] = make_float4(bad ? nan_f() : m / a.T, log_s, log_rest, mine.norm);
 }
 
 // ---- gradient: a warp takes one to four steps of 128 groups of a row by itself; the next step's logits are on their way while
