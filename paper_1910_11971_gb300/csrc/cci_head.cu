@@ -14,9 +14,10 @@
 //
 // The tensor core cuts its running sum at every addition, always towards zero: 256 of them, at D = 4096, leave a logit
 // of 12 about 6e-5 off, and a confident token's loss, a difference of such logits, as much of itself and more.  So the
-// forward pass adds kChunk stages (256 reduction indices) at a time there and the chunks in registers, to the nearest, as fp32 does
-// throughout.  That takes eight output warps, each 32 tokens by half of a tile's columns.  P's own rounding
-// is larger than this by a hundred, so the bf16 backward pass keeps one running sum.
+// forward pass adds kChunk stages (512 reduction indices) at a time there and the chunks in registers, to the nearest, as
+// fp32 does throughout (1999 x 4096 x 50257 bf16: 421 us with one running sum, 437 so, 579 with chunks of 256).  That takes
+// eight output warps, each 32 tokens by half of a tile's columns.  P's own rounding is larger than this by a hundred, so the
+// bf16 backward pass keeps one running sum.
 //
 // Tiles: 256 tokens x 256 columns over a CTA pair, or for few tokens or columns 128 x 256 and 128 x 128 on one CTA.
 // Sixteen M tiles at a time pass over the vocabulary, so that W is read once for up to 4096 tokens.
@@ -33,7 +34,7 @@ using gated::stage_mma;
 using gated::term_planes;
 using gated::tile_desc;
 
-constexpr int kChunk = 4;       // stages that the tensor core adds up by itself
+constexpr int kChunk = 8;       // stages that the tensor core adds up by itself
 constexpr int kMTilesAtOnce = 16;
 
 // one launch: a piece of the vocabulary
@@ -61,7 +62,9 @@ template <int CG, int BN, bool PROBS>
 struct Cfg {
     static constexpr int kM = 128, kBRows = BN / CG;
     static constexpr int kABytes = kM * 128, kBBytes = kBRows * 128, kStage = kABytes + kBBytes;
-    static constexpr int kOut = kM * 128, kOuts = PROBS ? 2 : 0;  // a buffer of 64 columns for each four output warps
+    // buffers of 64 columns for each four output warps: two where five stages or more are left beside them
+    static constexpr int kOut = kM * 128, kBufs = 5 * kStage + 4 * kOut + 2048 <= static_cast<int>(kMaxSmemPerBlock) ? 2 : 1;
+    static constexpr int kOuts = PROBS ? 2 * kBufs : 0;
     static constexpr int kFit = (static_cast<int>(kMaxSmemPerBlock) - 2048 - kOuts * kOut) / kStage;
     static constexpr int kStages = kFit < 8 ? kFit : 8;
     static constexpr int kTmem = 2 * BN;
@@ -97,12 +100,33 @@ __device__ __forceinline__ void tmem_ld16_begin(uint32_t taddr, uint32_t (&v)[16
         : "r"(taddr));
 }
 
+// and waited for: they are operands, so that nothing takes them before
+__device__ __forceinline__ void tmem_ld16_end(uint32_t (&v)[16])
+{
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 : "+r"(v[0]), "+r"(v[1]), "+r"(v[2]), "+r"(v[3]), "+r"(v[4]), "+r"(v[5]), "+r"(v[6]), "+r"(v[7]),
+                   "+r"(v[8]), "+r"(v[9]), "+r"(v[10]), "+r"(v[11]), "+r"(v[12]), "+r"(v[13]), "+r"(v[14]), "+r"(v[15])
+                 :
+                 : "memory");
+}
+
 __device__ __forceinline__ void tile_at(const Params &p, int tile, int &mt, int &nt)
 {
     const int per = kMTilesAtOnce * p.n_tiles, g = tile / per, r = tile - g * per;
     const int left = p.m_tiles - kMTilesAtOnce * g, gm = left < kMTilesAtOnce ? left : kMTilesAtOnce;
     nt = r / gm;
     mt = kMTilesAtOnce * g + r - nt * gm;
+}
+
+// the upper halves of a and b as bf16 (a in the low half), which become what that leaves.  Cut, not rounded: eight
+// bits a plane, so that three hold all 24 (4 operations a value; to the nearest, with its care for the ends, took a 256 x 256
+// tile's output 15 us more)
+__device__ __forceinline__ uint32_t next_planes(float &a, float &b)
+{
+    const uint32_t x = __float_as_uint(a), y = __float_as_uint(b);
+    a -= __uint_as_float(x & 0xffff0000u);
+    b -= __uint_as_float(y & 0xffff0000u);
+    return __byte_perm(x, y, 0x7632);
 }
 
 template <int CG, int BN, bool PROBS>
@@ -253,8 +277,8 @@ __global__ void __launch_bounds__(Cfg<CG, BN, PROBS>::kThreads, 1)
         const int half = (warp - 4) >> 2, m = tid & 127, c0 = half * C::kCols;
         const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
         const uint32_t acc_empty0 = CG == 2 ? ws::map_to_rank(tc::smem_u32(&S->acc_empty[0]), 0) : 0u;
-        const uint32_t buf = outs + static_cast<uint32_t>(half) * C::kOut;
-        int t = 0;
+        const uint32_t bufs = outs + static_cast<uint32_t>(half * C::kBufs) * C::kOut;
+        int t = 0, stored = 0;
         bool ok = true;
         for (int tile = first; ok && tile < p.tiles; tile += step) {
             int mt, nt;
@@ -290,7 +314,7 @@ __global__ void __launch_bounds__(Cfg<CG, BN, PROBS>::kThreads, 1)
                 for (int q = 0; q < C::kCols; q += 16) {
                     uint32_t v[16];
                     tmem_ld16_begin(col + q, v);
-                    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+                    tmem_ld16_end(v);
                     if (chunk == 0) {
 #pragma unroll
                         for (int j = 0; j < 16; ++j) z[q + j] = __uint_as_float(v[j]);
@@ -348,7 +372,9 @@ __global__ void __launch_bounds__(Cfg<CG, BN, PROBS>::kThreads, 1)
                     for (int c = 0; c < C::kCols; c += 64) {
                         if (c < count) {
                             for (int plane = 0; plane < planes; ++plane) {
-                                if (m == 0) tc::bulk_wait_read<0>();
+                                const uint32_t buf = bufs + static_cast<uint32_t>(stored % C::kBufs) * C::kOut;
+                                ++stored;
+                                if (m == 0) tc::bulk_wait_read<C::kBufs - 1>();
                                 tc::named_sync(2 + half, 128);
 #pragma unroll
                                 for (int q = 0; q < 8; ++q) {
@@ -356,12 +382,7 @@ __global__ void __launch_bounds__(Cfg<CG, BN, PROBS>::kThreads, 1)
 #pragma unroll
                                     for (int j = 0; j < 4; ++j) {
                                         float &a = z[c + 8 * q + 2 * j], &b = z[c + 8 * q + 2 * j + 1];
-                                        if (planes == 1) {
-                                            w[j] = row::bf16x2(a, b);
-                                        } else {  // a plane, and what it leaves
-                                            const uint32_t x = gated::next_plane(a), y = gated::next_plane(b);
-                                            w[j] = x | y << 16;
-                                        }
+                                        w[j] = planes == 1 ? row::bf16x2(a, b) : next_planes(a, b);
                                     }
                                     ws::st_shared_v4(buf + ws::sw_chunk(m, q), w[0], w[1], w[2], w[3]);
                                 }
