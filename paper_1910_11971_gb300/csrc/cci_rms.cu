@@ -275,69 +275,13 @@ __global__ void __launch_bounds__(1024) rms_long_kernel(const Forward p)
 }
 
 // ---- backward ----
-template <typename T, int V, int NV, int TPR, bool MORE>
-__global__ void __launch_bounds__(block_threads(TPR), TPR <= 256 ? 2 : 1) rms_backward_kernel(const Backward p)
+// a block's columns of dw: each thread's, or the sum of its groups' in their order
+template <int V, int NV, int TPR>
+__device__ __forceinline__ void write_columns(const float (&dw)[NV][V], float *part, float *sums, int group, int t, int D)
 {
     constexpr int kGroups = block_threads(TPR) / TPR;
-    constexpr bool kHold = TPR < 1024;
-    __shared__ float buf[kGroups][2][TPR / 32];
-    extern __shared__ __align__(16) float sums[];  // [D] where a block has several groups
-    const int group = threadIdx.x / TPR, t = threadIdx.x % TPR, D = p.D;
-    const int64_t step = static_cast<int64_t>(gridDim.x) * kGroups;
-    const int64_t n0 = static_cast<int64_t>(blockIdx.x) * kGroups + group;
-    const T *dy = static_cast<const T *>(p.dy), *h = static_cast<const T *>(p.h), *dh = static_cast<const T *>(p.dh);
-    row::Raw<T, V> rdy[NV], rh[NV];
-    if (n0 < p.N) {
-        load_row<T, V, NV, TPR>(rdy, dy + n0 * p.lddy, t, D);
-        load_row<T, V, NV, TPR>(rh, h + n0 * p.ldh, t, D);
-    }
-    float w[kHold ? NV : 1][V], dw[NV][V];
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-        if constexpr (kHold) weight_at<V>(p.w, (i * TPR + t) * V, D, w[i]);
-#pragma unroll
-        for (int j = 0; j < V; ++j) dw[i][j] = 0.f;
-    }
-    int turn = 0;
-    for (int64_t n = n0; n < p.N; n += step, turn ^= 1) {
-        const float r = p.rstd[n];
-        float g[NV][V], v[NV][V], s[1] = {0.f};
-        row::Raw<T, V> more[MORE ? NV : 1];
-        if constexpr (MORE) load_row<T, V, NV, TPR>(more, dh + n * p.lddh, t, D);
-#pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            row::unpack<T, V>(rdy[i], g[i]);
-            row::unpack<T, V>(rh[i], v[i]);
-            if constexpr (!kHold) weight_at<V>(p.w, (i * TPR + t) * V, D, w[0]);
-#pragma unroll
-            for (int j = 0; j < V; ++j) {
-                v[i][j] *= r;
-                dw[i][j] = fmaf(g[i][j], v[i][j], dw[i][j]);
-                g[i][j] *= w[kHold ? i : 0][j];
-                s[0] = fmaf(g[i][j], v[i][j], s[0]);
-            }
-        }
-        if (n + step < p.N) {
-            load_row<T, V, NV, TPR>(rdy, dy + (n + step) * p.lddy, t, D);
-            load_row<T, V, NV, TPR>(rh, h + (n + step) * p.ldh, t, D);
-        }
-        row::group_sum<TPR>(s, buf[group][turn], group, t);
-        const float minus = -s[0] / static_cast<float>(D);
-#pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const int c = (i * TPR + t) * V;
-            float o[V];
-            if constexpr (MORE) row::unpack<T, V>(more[i], o);
-#pragma unroll
-            for (int j = 0; j < V; ++j) {
-                const float d = fmaf(v[i][j], minus, g[i][j]) * r;
-                o[j] = MORE ? o[j] + d : d;
-            }
-            if (c < D) row::store<T, V>(static_cast<T *>(p.dx) + n * D + c, o);
-        }
-    }
-    float *part = p.part + static_cast<int64_t>(blockIdx.x) * D;
     if constexpr (kGroups > 1) {
+        __syncthreads();  // sums may lie where rows were
         for (int g = 0; g < kGroups; ++g) {
             if (group == g) {
 #pragma unroll
@@ -359,6 +303,209 @@ __global__ void __launch_bounds__(block_threads(TPR), TPR <= 256 ? 2 : 1) rms_ba
             if (c < D) row::store<float, V>(part + c, dw[i]);
         }
     }
+}
+
+// 16 bytes to shared memory, not through registers; `left`: the newest copies that are not waited for
+__device__ __forceinline__ void copy_word(void *to, const void *from)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(tc::smem_u32(to)), "l"(from) : "memory");
+}
+__device__ __forceinline__ void copies_end() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int LEFT>
+__device__ __forceinline__ void copies_wait()
+{
+    asm volatile("cp.async.wait_group %0;" ::"n"(LEFT) : "memory");
+}
+
+// Rows on 16-byte words: each thread copies its own columns of dy, h and dh of the next rows into places of its own
+// in shared memory and reads them there, so that rows are on their way without registers and nobody waits for
+// anybody's copies but their own (16384 x 4096 bf16: 94 us with the next row in registers)
+template <typename T, int NV, int TPR, bool MORE>
+struct Ring {
+    static constexpr int kGroups = block_threads(TPR) / TPR, kArrays = MORE ? 3 : 2;
+    static constexpr int kWords = static_cast<int>(sizeof(T)) / 2;  // of eight elements
+    static constexpr int kBlocks = NV == 1 ? 3 : (TPR <= 256 ? 2 : 1);  // of an SM
+    static constexpr int kStage = kArrays * NV * kWords * TPR * 16; // a row of a group
+    static constexpr int kFit = 212 * 1024 / kBlocks / (kStage * kGroups);
+    static constexpr int kStages = kFit < 1 ? 1 : (kFit < 4 ? kFit : 4);
+    static constexpr int kBytes = kStages * kStage * kGroups;
+    static_assert(kBytes <= static_cast<int>(kMaxSmemPerBlock) - 1024 && kBytes >= NV * 8 * TPR * 4, "the groups' sums fit");
+};
+
+template <typename T, int NV, int TPR, bool MORE>
+__global__ void __launch_bounds__(block_threads(TPR), Ring<T, NV, TPR, MORE>::kBlocks) rms_backward_kernel(const Backward p)
+{
+    using R = Ring<T, NV, TPR, MORE>;
+    constexpr int kGroups = R::kGroups, kStages = R::kStages, kWords = R::kWords;
+    constexpr bool kHold = TPR < 1024;  // the weight, and a row's values between its two passes, in registers
+    extern __shared__ __align__(16) unsigned char ring_raw[];
+    __shared__ float buf[kGroups][2][TPR / 32];
+    const int group = threadIdx.x / TPR, t = threadIdx.x % TPR, D = p.D;
+    const int64_t step = static_cast<int64_t>(gridDim.x) * kGroups;
+    const int64_t n0 = static_cast<int64_t>(blockIdx.x) * kGroups + group;
+    // word `w` of this thread's eight i of array a in stage k
+    uint4 *ring = reinterpret_cast<uint4 *>(ring_raw + group * kStages * R::kStage) + t;
+    auto place = [&](int k, int a, int i, int w) { return ring + (((k * R::kArrays + a) * NV + i) * kWords + w) * TPR; };
+    auto copy = [&](int64_t n, int k) {
+#pragma unroll
+        for (int a = 0; a < R::kArrays; ++a) {
+            const T *x = a == 0 ? static_cast<const T *>(p.dy) + n * p.lddy
+                                : (a == 1 ? static_cast<const T *>(p.h) + n * p.ldh : static_cast<const T *>(p.dh) + n * p.lddh);
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                const int c = (i * TPR + t) * 8;
+                if (c < D) {
+#pragma unroll
+                    for (int w = 0; w < kWords; ++w) copy_word(place(k, a, i, w), reinterpret_cast<const uint4 *>(x + c) + w);
+                }
+            }
+        }
+    };
+    auto take = [&](int k, int a, int i, float (&f)[8]) {
+        row::Raw<T, 8> raw{};
+        if ((i * TPR + t) * 8 < D) {
+#pragma unroll
+            for (int w = 0; w < kWords; ++w) raw.w[w] = *place(k, a, i, w);
+        }
+        row::unpack<T, 8>(raw, f);
+    };
+#pragma unroll
+    for (int k = 0; k < kStages; ++k) {
+        if (n0 + k * step < p.N) copy(n0 + k * step, k);
+        copies_end();
+    }
+    float next_r = n0 < p.N ? p.rstd[n0] : 0.f;
+    float w[kHold ? NV : 1][8], dw[NV][8];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        if constexpr (kHold) weight_at<8>(p.w, (i * TPR + t) * 8, D, w[i]);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) dw[i][j] = 0.f;
+    }
+    int turn = 0, k = 0;
+    for (int64_t n = n0; n < p.N; n += step, turn ^= 1) {
+        const float r = next_r;
+        if (n + step < p.N) next_r = p.rstd[n + step];
+        copies_wait<kStages - 1>();
+        float g[kHold ? NV : 1][8], v[kHold ? NV : 1][8], s[1] = {0.f};
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            constexpr bool H = kHold;
+            const int at = H ? i : 0;
+            take(k, 0, i, g[at]);
+            take(k, 1, i, v[at]);
+            if constexpr (!kHold) weight_at<8>(p.w, (i * TPR + t) * 8, D, w[0]);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                v[at][j] *= r;
+                dw[i][j] = fmaf(g[at][j], v[at][j], dw[i][j]);
+                g[at][j] *= w[at][j];
+                s[0] = fmaf(g[at][j], v[at][j], s[0]);
+            }
+        }
+        row::group_sum<TPR>(s, buf[group][turn], group, t);
+        const float minus = -s[0] / static_cast<float>(D);
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int c = (i * TPR + t) * 8, at = kHold ? i : 0;
+            if constexpr (!kHold) {
+                take(k, 0, i, g[0]);
+                take(k, 1, i, v[0]);
+                weight_at<8>(p.w, c, D, w[0]);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    v[0][j] *= r;
+                    g[0][j] *= w[0][j];
+                }
+            }
+            float o[8];
+            if constexpr (MORE) take(k, 2, i, o);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const float d = fmaf(v[at][j], minus, g[at][j]) * r;
+                o[j] = MORE ? o[j] + d : d;
+            }
+            if (c < D) row::store<T, 8>(static_cast<T *>(p.dx) + n * D + c, o);
+        }
+        if (n + kStages * step < p.N) copy(n + kStages * step, k);  // what this thread has read
+        copies_end();
+        k = k + 1 == kStages ? 0 : k + 1;
+    }
+    copies_wait<0>();
+    write_columns<8, NV, TPR>(dw, p.part + static_cast<int64_t>(blockIdx.x) * D, reinterpret_cast<float *>(ring_raw), group, t, D);
+}
+
+// fp32 rows on words, of which shared memory holds too few (8000 x 4096: 85 us, 135 through it), and all rows off
+// them, element by element: the next row in registers.  dh is a row ahead for the latter alone (20000 x 777 bf16: 39 us, 63
+// with dh and rstd loaded when they are needed; fp32 on words has no registers left, 109)
+template <typename T, int V, int NV, int TPR, bool MORE>
+__global__ void __launch_bounds__(block_threads(TPR), TPR <= 256 ? 2 : 1) rms_backward_registers_kernel(const Backward p)
+{
+    constexpr int kGroups = block_threads(TPR) / TPR;
+    constexpr bool kHold = TPR < 1024, kAhead = V == 1;  // the weight in registers; dh a row ahead
+    __shared__ float buf[kGroups][2][TPR / 32];
+    extern __shared__ __align__(16) float sums[];  // [D] where a block has several groups
+    const int group = threadIdx.x / TPR, t = threadIdx.x % TPR, D = p.D;
+    const int64_t step = static_cast<int64_t>(gridDim.x) * kGroups;
+    const int64_t n0 = static_cast<int64_t>(blockIdx.x) * kGroups + group;
+    const T *dy = static_cast<const T *>(p.dy), *h = static_cast<const T *>(p.h), *dh = static_cast<const T *>(p.dh);
+    row::Raw<T, V> rdy[NV], rh[NV], more[MORE && kAhead ? NV : 1];
+    float next_r = 0.f;
+    auto load = [&](int64_t n) {
+        next_r = p.rstd[n];
+        load_row<T, V, NV, TPR>(rdy, dy + n * p.lddy, t, D);
+        load_row<T, V, NV, TPR>(rh, h + n * p.ldh, t, D);
+        if constexpr (MORE && kAhead) load_row<T, V, NV, TPR>(more, dh + n * p.lddh, t, D);
+    };
+    if (n0 < p.N) load(n0);
+    float w[kHold ? NV : 1][V], dw[NV][V];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        if constexpr (kHold) weight_at<V>(p.w, (i * TPR + t) * V, D, w[i]);
+#pragma unroll
+        for (int j = 0; j < V; ++j) dw[i][j] = 0.f;
+    }
+    int turn = 0;
+    for (int64_t n = n0; n < p.N; n += step, turn ^= 1) {
+        const float r = next_r;
+        float g[NV][V], v[NV][V], s[1] = {0.f};
+        row::Raw<T, V> now[MORE ? NV : 1];
+        if constexpr (MORE && kAhead) {
+#pragma unroll
+            for (int i = 0; i < NV; ++i) now[i] = more[i];
+        } else if constexpr (MORE) {
+            load_row<T, V, NV, TPR>(now, dh + n * p.lddh, t, D);
+        }
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            row::unpack<T, V>(rdy[i], g[i]);
+            row::unpack<T, V>(rh[i], v[i]);
+            if constexpr (!kHold) weight_at<V>(p.w, (i * TPR + t) * V, D, w[0]);
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                v[i][j] *= r;
+                dw[i][j] = fmaf(g[i][j], v[i][j], dw[i][j]);
+                g[i][j] *= w[kHold ? i : 0][j];
+                s[0] = fmaf(g[i][j], v[i][j], s[0]);
+            }
+        }
+        if (n + step < p.N) load(n + step);
+        row::group_sum<TPR>(s, buf[group][turn], group, t);
+        const float minus = -s[0] / static_cast<float>(D);
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int c = (i * TPR + t) * V;
+            float o[V];
+            if constexpr (MORE) row::unpack<T, V>(now[i], o);
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                const float d = fmaf(v[i][j], minus, g[i][j]) * r;
+                o[j] = MORE ? o[j] + d : d;
+            }
+            if (c < D) row::store<T, V>(static_cast<T *>(p.dx) + n * D + c, o);
+        }
+    }
+    write_columns<V, NV, TPR>(dw, p.part + static_cast<int64_t>(blockIdx.x) * D, sums, group, t, D);
 }
 
 // rows too long for registers: dx by two passes over each, dw's parts by columns (rows blockIdx.y, + parts, ...)
@@ -419,7 +566,9 @@ __global__ void __launch_bounds__(256) weight_kernel(const float *part, int part
 // host
 // ---------------------------------------------------------------------------
 
-constexpr int kLongest = 16384;   // columns that a row's registers hold
+// columns that a row's registers hold: on words, and off them (backward 749 x 10523 bf16: 57 us element by element in
+// registers, 46 by two passes)
+constexpr int kLongest = 16384, kLongestOff = 8192;
 
 // f(V, NV, TPR): vectors of V, NV of them a thread, TPR threads a row
 template <typename Fn>
@@ -434,7 +583,9 @@ cudaError_t with_layout(bool words, int64_t D, Fn f)
         CCI_RMS_CASE(1024, 8, 1, 128)
         CCI_RMS_CASE(2048, 8, 2, 128)
         CCI_RMS_CASE(4096, 8, 2, 256)
+        CCI_RMS_CASE(6144, 8, 2, 384)
         CCI_RMS_CASE(8192, 8, 2, 512)
+        CCI_RMS_CASE(12288, 8, 2, 768)
         CCI_RMS_CASE(16384, 8, 2, 1024)
     } else {
         CCI_RMS_CASE(256, 1, 8, 32)
@@ -442,7 +593,6 @@ cudaError_t with_layout(bool words, int64_t D, Fn f)
         CCI_RMS_CASE(2048, 1, 8, 256)
         CCI_RMS_CASE(4096, 1, 8, 512)
         CCI_RMS_CASE(8192, 1, 8, 1024)
-        CCI_RMS_CASE(16384, 1, 16, 1024)
     }
 #undef CCI_RMS_CASE
     return cudaErrorInvalidValue;
@@ -463,13 +613,13 @@ template <typename T, bool FP8>
 cudaError_t forward(const Forward &p, cudaStream_t stream)
 {
     constexpr int es = sizeof(T);
-    if (p.D > kLongest) {
-        rms_long_kernel<T, FP8><<<static_cast<unsigned>(p.N), 1024, 0, stream>>>(p);
-        return cudaGetLastError();
-    }
     const bool words = p.D % 8 == 0 && on_words(p.x, p.ldx, es) && on_words(p.residual, p.ldr, es) && on_words(p.w, 4, 4) &&
                        on_words(p.y, p.D, FP8 ? 2 : es) && on_words(p.h, p.D, es);
     if (FP8 && !words) return cudaErrorInvalidValue;
+    if (p.D > (words ? kLongest : kLongestOff)) {
+        rms_long_kernel<T, FP8><<<static_cast<unsigned>(p.N), 1024, 0, stream>>>(p);
+        return cudaGetLastError();
+    }
     return with_layout(words, p.D, [&](auto v, auto nv, auto tpr) {
         constexpr int V = decltype(v)::value, NV = decltype(nv)::value, TPR = decltype(tpr)::value;
         if constexpr (!FP8 || V == 8) {
@@ -486,7 +636,18 @@ cudaError_t forward(const Forward &p, cudaStream_t stream)
 }
 
 // blocks of the backward pass at most: their sums lie in the workspace
-int64_t most_parts(int64_t N) { return N < 2 * row::sm_count() ? N : 2 * row::sm_count(); }
+int64_t most_parts(int64_t N) { return N < 3 * row::sm_count() ? N : 3 * row::sm_count(); }
+
+template <typename T, int NV, int TPR, bool MORE>
+cudaError_t launch_ring(const Backward &p, unsigned blocks, cudaStream_t stream)
+{
+    using R = Ring<T, NV, TPR, MORE>;
+    static SmemAttrCache attr_cache;
+    const cudaError_t attr = smem_attr_once(rms_backward_kernel<T, NV, TPR, MORE>, R::kBytes, attr_cache);
+    if (attr != cudaSuccess) return attr;
+    rms_backward_kernel<T, NV, TPR, MORE><<<blocks, block_threads(TPR), R::kBytes, stream>>>(p);
+    return cudaGetLastError();
+}
 
 template <typename T>
 cudaError_t backward(const Backward &p, float *dw, cudaStream_t stream)
@@ -494,25 +655,29 @@ cudaError_t backward(const Backward &p, float *dw, cudaStream_t stream)
     constexpr int es = sizeof(T);
     unsigned parts = 0;
     cudaError_t e = cudaSuccess;
-    if (p.D > kLongest) {
+    const bool words = p.D % 8 == 0 && on_words(p.dy, p.lddy, es) && on_words(p.h, p.ldh, es) && on_words(p.dh, p.lddh, es) &&
+                       on_words(p.w, 4, 4) && on_words(p.dx, p.D, es);
+    if (p.D > (words ? kLongest : kLongestOff)) {
         rms_backward_long_kernel<T><<<static_cast<unsigned>(p.N), 1024, 0, stream>>>(p);
-        const int64_t most = most_parts(p.N);
-        parts = static_cast<unsigned>(most < 16 ? most : 16);
+        parts = static_cast<unsigned>(p.N < 32 ? p.N : 32);
         rms_columns_kernel<T><<<dim3(static_cast<unsigned>((p.D + 255) / 256), parts), 256, 0, stream>>>(p);
         e = cudaGetLastError();
     } else {
-        const bool words = p.D % 8 == 0 && on_words(p.dy, p.lddy, es) && on_words(p.h, p.ldh, es) &&
-                           on_words(p.dh, p.lddh, es) && on_words(p.w, 4, 4) && on_words(p.dx, p.D, es);
         e = with_layout(words, p.D, [&](auto v, auto nv, auto tpr) {
             constexpr int V = decltype(v)::value, NV = decltype(nv)::value, TPR = decltype(tpr)::value;
             constexpr int kGroups = block_threads(TPR) / TPR;
-            parts = blocks_of(p.N, kGroups, TPR <= 256 ? 2 : 1);
-            const size_t bytes = kGroups > 1 ? static_cast<size_t>(p.D) * sizeof(float) : 0;
-            if (p.dh)
-                rms_backward_kernel<T, V, NV, TPR, true><<<parts, block_threads(TPR), bytes, stream>>>(p);
-            else
-                rms_backward_kernel<T, V, NV, TPR, false><<<parts, block_threads(TPR), bytes, stream>>>(p);
-            return cudaGetLastError();
+            if constexpr (V == 8 && sizeof(T) == 2) {
+                parts = blocks_of(p.N, kGroups, Ring<T, NV, TPR, true>::kBlocks);
+                return p.dh ? launch_ring<T, NV, TPR, true>(p, parts, stream) : launch_ring<T, NV, TPR, false>(p, parts, stream);
+            } else {
+                parts = blocks_of(p.N, kGroups, TPR <= 256 ? 2 : 1);
+                const size_t bytes = kGroups > 1 ? static_cast<size_t>(p.D) * sizeof(float) : 0;
+                if (p.dh)
+                    rms_backward_registers_kernel<T, V, NV, TPR, true><<<parts, block_threads(TPR), bytes, stream>>>(p);
+                else
+                    rms_backward_registers_kernel<T, V, NV, TPR, false><<<parts, block_threads(TPR), bytes, stream>>>(p);
+                return cudaGetLastError();
+            }
         });
     }
     if (e != cudaSuccess || !dw) return e;
