@@ -123,3 +123,169 @@ def test_against_64_bits(dev, N, D, V, dtype):
     dX, dW = cci.linear_cross_entropy_backward(dloss.to(dev), *args, stats, status=status)
     check_backward(X, W, targets, stats, dloss, dX, dW, dtype)
     assert int(status.item()) == 0
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("N,D,V", [(20000, 16, 10000), (5000, 8, 60001)])
+def test_several_pieces(dev, N, D, V, dtype):
+    """Workspaces of a few pieces of the vocabulary: P's rows of 10000 entries are 400 MB, of 60001 600."""
+    X, W, targets, dloss = inputs(N, D, V, dtype, N)
+    args = X.to(dev), W.to(dev), targets.to(dev)
+    loss, stats = cci.linear_cross_entropy(*args)
+    dX, dW = cci.linear_cross_entropy_backward(dloss.to(dev), *args, stats)
+    some = torch.arange(0, N, 97)  # rows of dX and of the loss, all of dW by the formula on the GPU in 64 bits
+    z = args[0].double() @ args[1].double().t()
+    lse = torch.logsumexp(z, 1)
+    kept = args[2] != IGNORE
+    check_forward(X[some], W, targets[some], loss[some], stats[some], dtype)
+    P = torch.exp(z - lse[:, None]) * torch.where(kept, dloss.to(dev).double(), 0.0)[:, None]
+    P[torch.arange(N, device=dev)[kept], args[2][kept]] -= dloss.to(dev).double()[kept]
+    half = 2.0 ** -8 if dtype == "bf16" else 0.0
+    # A probability p is off by at most 512 u p: 36 u of sum |x w|, up to 10 here, for its logit and as much for the sum's;
+    # (4 + 3.4 * 20) u for its exponential, 70 u for the sum's additions.  The target's entry p - 1 is off by p's error, whatever
+    # is left of it: at p = 0.999 that is 1000 times as much of the entry itself, so the error goes with d (p + 1[v = t]), not
+    # with |P|.  The rounding of P and the products' sums go with |P|, as above
+    off = dloss.to(dev).double().abs()[:, None] * torch.exp(z - lse[:, None]) * kept[:, None]
+    rel = half + ((34 * 32 if dtype == "f32" else 34 * (max(N, V) // 16)) + 8) * U
+    for got, want, tol in ((dX, P @ args[1].double(), (512 * U * off + rel * P.abs()) @ args[1].double().abs()),
+                           (dW, P.t() @ args[0].double(), (512 * U * off + rel * P.abs()).t() @ args[0].double().abs())):
+        assert ((got.double() - want).abs() <= tol + half * want.abs()).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_only_what_is_asked_for(dev, dtype):
+    X, W, targets, dloss = (t.to(dev) for t in inputs(200, 64, 777, dtype, 1))
+    loss, stats = cci.linear_cross_entropy(X, W, targets)
+    dX, dW = cci.linear_cross_entropy_backward(dloss, X, W, targets, stats)
+    a, none = cci.linear_cross_entropy_backward(dloss, X, W, targets, stats, need_dw=False)
+    none2, b = cci.linear_cross_entropy_backward(dloss, X, W, targets, stats, need_dx=False)
+    assert none is None and none2 is None and torch.equal(a, dX) and torch.equal(b, dW)
+    assert cci.linear_cross_entropy_backward(dloss, X, W, targets, stats, need_dx=False, need_dw=False) == (None, None)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_the_same_call_gives_the_same_bits(dev, dtype):
+    X, W, targets, dloss = (t.to(dev) for t in inputs(300, 520, 3001, dtype, 2))
+    ref = None
+    for _ in range(3):
+        loss, stats = cci.linear_cross_entropy(X, W, targets)
+        got = (loss, stats, *cci.linear_cross_entropy_backward(dloss, X, W, targets, stats))
+        assert ref is None or all(torch.equal(a, b) for a, b in zip(got, ref))
+        ref = got
+
+
+def test_all_left_out(dev):
+    X, W, _, dloss = (t.to(dev) for t in inputs(40, 64, 300, "bf16", 3))
+    targets = torch.full((40,), IGNORE, device=dev)
+    loss, stats = cci.linear_cross_entropy(X, W, targets)
+    assert (loss == 0).all() and stats.isfinite().all()
+    dX, dW = cci.linear_cross_entropy_backward(dloss * float("nan"), X, W, targets, stats)
+    assert (dX == 0).all() and (dW == 0).all()
+    # another value to leave out by, a valid entry's too
+    loss, _ = cci.linear_cross_entropy(X, W, torch.full((40,), 7, device=dev), ignore_index=7)
+    assert (loss == 0).all()
+
+
+def test_no_rows(dev):
+    W = torch.ones((30, 16), device=dev)
+    X, t = torch.empty((0, 16), device=dev), torch.empty(0, dtype=torch.int64, device=dev)
+    loss, stats = cci.linear_cross_entropy(X, W, t)
+    dX, dW = cci.linear_cross_entropy_backward(loss, X, W, t, stats)
+    assert loss.shape == (0,) and stats.shape == (0, 2) and dX.shape == (0, 16) and (dW == 0).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_bad_targets_are_reported(dev, dtype):
+    X, W, targets, dloss = inputs(300, 64, 500, dtype, 4)
+    bad = torch.zeros(300, dtype=torch.bool)
+    for n, t in ((0, 500), (7, -1), (131, 2 ** 40), (299, -(2 ** 63))):
+        targets[n], bad[n] = t, True
+    args = X.to(dev), W.to(dev), targets.to(dev)
+    status = cci.new_status(dev)
+    loss, stats = cci.linear_cross_entropy(*args, status=status)
+    assert cci.read_status(status) == 10  # CCI_ERR_INDEX
+    assert (loss.cpu().isnan() == bad).all()
+    status = cci.new_status(dev)
+    dX, dW = cci.linear_cross_entropy_backward(dloss.to(dev), *args, stats, status=status)
+    assert cci.read_status(status) == 10
+    # as if they were left out
+    targets[bad] = IGNORE
+    check_backward(X, W, targets, stats, dloss, dX, dW, dtype)
+    assert (dX.cpu()[bad] == 0).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_nan_and_inf_keep_to_their_rows(dev, dtype):
+    X, W, targets, _ = inputs(300, 64, 500, dtype, 5)
+    good = cci.linear_cross_entropy(X.to(dev), W.to(dev), targets.to(dev))[0].cpu()
+    X[3, 5], X[200, 63] = float("nan"), float("inf")
+    loss = cci.linear_cross_entropy(X.to(dev), W.to(dev), targets.to(dev))[0].cpu()
+    bad = torch.zeros(300, dtype=torch.bool)
+    bad[3] = bad[200] = True
+    assert loss[bad].isnan().all() and torch.equal(loss[~bad], good[~bad])
+
+
+def test_confident_tokens_keep_their_loss(dev):
+    """Logits of 30 over thousands of indices whose sum grows all along: the loss is a difference of such sums."""
+    D, V = 4096, 300
+    g = torch.Generator().manual_seed(6)
+    W = torch.randn((V, D), generator=g).to(torch.bfloat16)
+    targets = torch.arange(0, V, 3)
+    X = ((30.0 / D) * W[targets].float() + 0.1 / D ** 0.5 * torch.randn((100, D), generator=g)).to(torch.bfloat16)
+    loss, stats = cci.linear_cross_entropy(X.to(dev), W.to(dev), targets.to(dev))
+    check_forward(X, W, targets, loss, stats, "bf16")
+    _, _, _, _, want = reference(X, W, targets)
+    # eight chunks of 512 indices, a logit of 3.75 each at most, 32 cuts of half a unit (2^-23 of up to 4) in the mean while
+    # the sum grows: 8 * 32 * 2^-23 / 2 * 4 / 2 = 3.1e-5 of the logit's difference, and as much of each token's chance to miss
+    assert ((loss.cpu().double() - want).abs() <= 6.2e-5 * (1 - torch.exp(-want)) + 1e-6 * want + 2 ** -24).all()
+
+
+def test_large_offsets(dev):
+    """Logits that all lie far from 0."""
+    N, D, V = 50, 64, 400
+    X, W, targets, dloss = inputs(N, D, V, "f32", 7)
+    X[:, 0], W[:, 0] = 100.0, 50.0
+    args = X.to(dev), W.to(dev), targets.to(dev)
+    loss, stats = cci.linear_cross_entropy(*args)
+    check_forward(X, W, targets, loss, stats, "f32")
+    dX, dW = cci.linear_cross_entropy_backward(dloss.to(dev), *args, stats)
+    check_backward(X, W, targets, stats, dloss, dX, dW, "f32")
+
+
+def test_gradient_against_differences(dev):
+    N, D, V = 3, 16, 20
+    X, W, targets, dloss = inputs(N, D, V, "f32", 8)
+    args = X.to(dev), W.to(dev), targets.to(dev)
+    loss, stats = cci.linear_cross_entropy(*args)
+    dX, dW = (t.cpu() for t in cci.linear_cross_entropy_backward(dloss.to(dev), *args, stats))
+    step = 1e-4
+    for which, grad in ((0, dX), (1, dW)):
+        for a, b in ((0, 3), (2, 15), (int(targets[0]) if which else 1, 7)):
+            ends = []
+            for sign in (1, -1):
+                t = [X.double(), W.double()]
+                t[which][a, b] += sign * step
+                ends.append(float((reference(t[0], t[1], targets)[4] * dloss.double()).sum()))
+            # third derivatives are below 10: |x|^3 and |w|^3 of a few
+            assert abs((ends[0] - ends[1]) / (2 * step) - float(grad[a, b])) <= 1e-6
+
+
+@pytest.mark.parametrize("call", [cci.HEAD_FORWARD, cci.HEAD_BACKWARD])
+def test_a_given_workspace_is_enough(dev, call):
+    N, D, V = 300, 64, 3001
+    X, W, targets, dloss = (t.to(dev) for t in inputs(N, D, V, "f32", 9))
+    ws = cci.head_workspace(call, torch.float32, N, D, V, dev)
+    room = torch.full((ws.numel() + 512,), 7, dtype=torch.uint8, device=dev)
+    at = room[256:256 + ws.numel()]
+    loss, stats = cci.linear_cross_entropy(X, W, targets)
+    if call == cci.HEAD_FORWARD:
+        got = cci.linear_cross_entropy(X, W, targets, workspace=at)
+        assert torch.equal(got[0], loss) and torch.equal(got[1], stats)
+    else:
+        want = cci.linear_cross_entropy_backward(dloss, X, W, targets, stats)
+        got = cci.linear_cross_entropy_backward(dloss, X, W, targets, stats, workspace=at)
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    assert (room[:256] == 7).all() and (room[256 + ws.numel():] == 7).all()
+    with pytest.raises(cci.CCIError):
+        cci.linear_cross_entropy(X, W, targets, workspace=at[:-256]) if call == cci.HEAD_FORWARD else \
+            cci.linear_cross_entropy_backward(dloss, X, W, targets, stats, workspace=at[:-256])
