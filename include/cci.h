@@ -781,7 +781,7 @@ cci_status cci_linear_cross_entropy(const void *X, cci_dtype dtype, int64_t N, i
  *   dX         device [N][D] of dtype (written), or NULL
  *   dW         device [V][D] of dtype (written; zeros for N = 0), or NULL
  *   workspace  cci_head_workspace_size(CCI_HEAD_BACKWARD, ...) bytes: about 256 MB for a piece, more
- *              only where a piece of 2048 entries takes more
+ *              only where a piece of 2048 entries, or of 128 times 128 / N for each SM, takes more
  * Errors: as cci_linear_cross_entropy.
  */
 cci_status cci_linear_cross_entropy_backward(const float *dloss, const void *X, cci_dtype dtype, int64_t N, int64_t D,

@@ -23,6 +23,7 @@
 // Sixteen M tiles at a time pass over the vocabulary, so that W is read once for up to 4096 tokens.
 // Every wait is bounded, as in the gated block's products.
 #include "cci_gated.cuh"
+#include "cci_head_few.cuh"
 
 namespace cci {
 namespace head {
@@ -118,17 +119,6 @@ __device__ __forceinline__ void tile_at(const Params &p, int tile, int &mt, int 
     mt = kMTilesAtOnce * g + r - nt * gm;
 }
 
-// the upper halves of a and b as bf16 (a in the low half), which become what that leaves.  Cut, not rounded: eight
-// bits a plane, so that three hold all 24 (4 operations a value; to the nearest, with its care for the ends, took a 256 x 256
-// tile's output 15 us more)
-__device__ __forceinline__ uint32_t next_planes(float &a, float &b)
-{
-    const uint32_t x = __float_as_uint(a), y = __float_as_uint(b);
-    a -= __uint_as_float(x & 0xffff0000u);
-    b -= __uint_as_float(y & 0xffff0000u);
-    return __byte_perm(x, y, 0x7632);
-}
-
 template <int CG, int BN, bool PROBS>
 __global__ void __launch_bounds__(Cfg<CG, BN, PROBS>::kThreads, 1)
     head_kernel(const Params p, const __grid_constant__ Maps maps)
@@ -181,6 +171,7 @@ __global__ void __launch_bounds__(Cfg<CG, BN, PROBS>::kThreads, 1)
     if constexpr (CG == 2) ws::cluster_sync();
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     const uint32_t tmem = S->tmem_base;
+    if constexpr (!PROBS) tc::launch_next_grid();  // the losses' launch, which waits for this one's end
 
     // output threads hold up to 128 sums each: 128 threads give up 96 of their 168 registers, and 256 take 48 more
     if (warp < 4) {
@@ -522,11 +513,13 @@ Shape shape_of(int64_t M, int64_t N, int64_t D, int terms)
 }
 
 // columns of a piece, at most: what a piece takes in the workspace, `bytes` a column, stays below `budget`, but for
-// pieces of 2048 columns.  Pieces are of like size
-int64_t piece_of(int64_t V, int64_t bytes, int64_t budget)
+// pieces of 2048 columns, or of a tile of 128 x 128 for each SM (64 fp32 tokens, 3688 x 15591: XX us in pieces of 4352, YY so).
+// Pieces are of like size
+int64_t piece_of(int64_t V, int64_t bytes, int64_t budget, int64_t N)
 {
-    int64_t most = budget / (bytes < 1 ? 1 : bytes) / 256 * 256;
-    if (most < 2048) most = 2048;
+    int64_t most = budget / (bytes < 1 ? 1 : bytes) / 256 * 256, least = 128 * ws::sm_count() / ((N + 127) / 128);
+    if (least < 2048) least = 2048;
+    if (most < least) most = (least + 255) / 256 * 256;
     const int64_t pieces = (V + most - 1) / most;
     const int64_t each = (V + pieces - 1) / pieces;
     return (each + 255) / 256 * 256;
@@ -547,6 +540,9 @@ struct Layout {
     size_t total;
 };
 
+// few fp32 tokens forward read the weights as they are (cci_head_few.cuh)
+bool few_tokens(int dtype, int64_t N, int call) { return call == CCI_HEAD_FORWARD && dtype == CCI_F32 && N <= kFewTokens; }
+
 Layout layout(int dtype, int64_t N, int64_t D, int64_t V, int call)
 {
     const bool f32 = dtype == CCI_F32;
@@ -559,15 +555,18 @@ Layout layout(int dtype, int64_t N, int64_t D, int64_t V, int call)
         return here;
     };
     if (call == CCI_HEAD_FORWARD)
-        l.piece = f32 ? piece_of(V, 6 * D, kForwardBudget) : V;
+        l.piece = f32 ? piece_of(V, 6 * D, kForwardBudget, N) : V;
     else
-        l.piece = piece_of(V, f32 ? 6 * (N + D) : 2 * N, kBackwardBudget);
+        l.piece = piece_of(V, f32 ? 6 * (N + D) : 2 * N, kBackwardBudget, N);
     if (l.piece > V) l.piece = V;
     if (f32) {
         l.x = take(6 * N * D);
-        l.w = take(6 * l.piece * D);
+        if (!few_tokens(dtype, N, call)) l.w = take(6 * l.piece * D);
     }
-    if (call == CCI_HEAD_FORWARD) {
+    if (few_tokens(dtype, N, call)) {
+        l.parts = take(few_blocks(V, ws::sm_count()) * N * static_cast<int64_t>(sizeof(float2)));
+        l.at_target = take(N * 4);
+    } else if (call == CCI_HEAD_FORWARD) {
         int64_t parts = 0;
         for (int64_t c = 0; c < V; c += l.piece) {
             const int64_t n = V - c < l.piece ? V - c : l.piece;
@@ -685,7 +684,14 @@ cudaError_t launch_head(const HeadArgs &a, cudaStream_t stream)
     int64_t count = 0;
     if (f32) e = planes(a.X, base + l.x, a.N * a.D, stream);
     const Operand x{f32 ? base + l.x : a.X, a.N, a.D, f32 ? 3 : 1};
-    for (int64_t c = 0; c < a.V && e == cudaSuccess; c += l.piece) {
+    const bool few = few_tokens(a.dtype, a.N, CCI_HEAD_FORWARD);
+    if (few && e == cudaSuccess) {
+        const FewParams f{static_cast<const uint16_t *>(x.data), static_cast<const float *>(a.W), static_cast<int>(a.N),
+                          static_cast<int>(a.D), a.V, 0, a.targets, a.ignore, parts, p.at_target};
+        e = launch_few(f, ws::sm_count(), stream);
+        count = few_blocks(a.V, ws::sm_count());
+    }
+    for (int64_t c = 0; !few && c < a.V && e == cudaSuccess; c += l.piece) {
         const int64_t n = a.V - c < l.piece ? a.V - c : l.piece;
         const void *w = rows_at(a, c);
         if (f32) {
