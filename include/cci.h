@@ -621,14 +621,18 @@ cci_status cci_token_logprobs_backward(const void *logits, cci_dtype dtype, int6
  *   temperature T > 0, finite
  *   loss       device fp32 [N]; stats device fp32 [N][4], 16-byte aligned (written)
  *   dev_status device uint32 or NULL
+ *   workspace  device, 16-byte aligned, cci_distillation_workspace_size(N, V) bytes (0 for many rows and for
+ *              short ones; it depends on the current device's number of SMs); overwritten
  * N = 0 is valid and enqueues nothing.
  * Errors: CCI_ERR_NULL, CCI_ERR_SHAPE (V < 1 or > 2^24, N >= 2^28, N rows of V / 2048 blocks or more than 2^31, ldx < V,
- *         k out of range), CCI_ERR_DTYPE, CCI_ERR_VALUE (temperature), CCI_ERR_ALIGN, CCI_ERR_CUDA.
+ *         k out of range), CCI_ERR_DTYPE, CCI_ERR_VALUE (temperature), CCI_ERR_ALIGN, CCI_ERR_WORKSPACE, CCI_ERR_CUDA.
  */
 #define CCI_MAX_TEACHER 128
+size_t cci_distillation_workspace_size(int64_t N, int64_t V);
 cci_status cci_distillation_loss(const void *logits, cci_dtype dtype, int64_t N, int64_t V, int64_t ldx,
                                  const int32_t *top_idx, const float *top_logp, int k, float temperature, int tail,
-                                 float *loss, float *stats, uint32_t *dev_status, cci_stream_t stream);
+                                 float *loss, float *stats, uint32_t *dev_status, void *workspace,
+                                 size_t workspace_bytes, cci_stream_t stream);
 
 /*
  * cci_distillation_loss_backward -- the gradient of cci_distillation_loss to the logits:

@@ -87,7 +87,9 @@ SIGNATURES = {
                                        ctypes.c_size_t, _P]),
     "cci_gated_linear_backward": (_I32, [_P, _P, _I32, _I64, _I64, _P, _P, _I64, _I32, _P, _P, _P, _P, _P, _U32P, _P,
                                          ctypes.c_size_t, _P]),
-    "cci_distillation_loss": (_I32, [_P, _I32, _I64, _I64, _I64, _P, _P, _I32, ctypes.c_float, _I32, _P, _P, _U32P, _P]),
+    "cci_distillation_workspace_size": (ctypes.c_size_t, [_I64, _I64]),
+    "cci_distillation_loss": (_I32, [_P, _I32, _I64, _I64, _I64, _P, _P, _I32, ctypes.c_float, _I32, _P, _P, _U32P, _P,
+                                     ctypes.c_size_t, _P]),
     "cci_distillation_loss_backward": (_I32, [_P, _P, _I32, _I64, _I64, _I64, _P, _P, _I32, ctypes.c_float, _I32, _P, _P,
                                               _I64, _P]),
     "cci_rms_norm": (_I32, [_P, _I32, _I64, _I64, _I64, _P, _I64, _P, ctypes.c_float, _P, _P, _P, _P]),
@@ -748,7 +750,7 @@ def token_logprobs_backward(logits: torch.Tensor, tokens: Optional[torch.Tensor]
 
 
 def distillation_loss(logits: torch.Tensor, top_idx: torch.Tensor, top_logp: torch.Tensor, *, temperature: float = 1.0,
-                      tail: bool = False, status: Optional[torch.Tensor] = None):
+                      tail: bool = False, status: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None):
     """(loss, stats) of a student's logits[N][V] against a teacher's top_idx (int32) and top_logp (fp32) [N][k]
     (``cci_distillation_loss``; the lists of ``token_logprobs(..., top=k)`` on the teacher's logits, k at most 128): the
     cross entropy of the teacher's listed probabilities, renormalised at the temperature or, with ``tail``, as they are
@@ -760,9 +762,12 @@ def distillation_loss(logits: torch.Tensor, top_idx: torch.Tensor, top_logp: tor
     ip, vp, k = _lists(top_idx, top_logp, N, index)
     loss = torch.empty(N, dtype=torch.float32, device=logits.device)
     stats = torch.empty((N, 4), dtype=torch.float32, device=logits.device)
+    if workspace is None:
+        workspace = _workspace(_distillation_bytes(N, V, index), logits.device)
+    wp, wb = (None, 0) if workspace is None else _space(workspace, index)
     _check(lib().cci_distillation_loss(logits.data_ptr(), _dtype_code(logits), N, V, ld, ip, vp, k, temperature, int(tail),
                                        loss.data_ptr(), stats.data_ptr(),
-                                       None if status is None else _status_word(status, index),
+                                       None if status is None else _status_word(status, index), wp, wb,
                                        torch._C._cuda_getCurrentRawStream(index)), "cci_distillation_loss")
     return loss, stats
 
@@ -784,6 +789,12 @@ def distillation_loss_backward(dloss: torch.Tensor, logits: torch.Tensor, top_id
                                                 torch._C._cuda_getCurrentRawStream(index)),
            "cci_distillation_loss_backward")
     return out
+
+
+@functools.lru_cache(maxsize=4096)
+def _distillation_bytes(N: int, V: int, device_index: int) -> int:
+    with torch.cuda.device(device_index):
+        return int(lib().cci_distillation_workspace_size(N, V))
 
 
 def _lists(top_idx: torch.Tensor, top_logp: torch.Tensor, N: int, index: int):

@@ -396,7 +396,7 @@ cci_status check_distillation(int dtype, int64_t N, int64_t V, const void *logit
 {
     if (!valid_dtype(dtype)) return CCI_ERR_DTYPE;
     if (N > 0 && (!logits || !idx || !value || !stats)) return CCI_ERR_NULL;
-    // a row takes up to eight blocks forward, and a block for 2048 logits or more backward
+    // eight rows take a block forward, and a warp for 1024 logits or more backward
     if (!rows_ok(N, V, ldx) || V > kMaxLogits || N >= kMaxRows / 8 || N * ((V + 2054) / 2048) >= kMaxRows || k < 1 ||
         k > CCI_MAX_TEACHER || k > V)
         return CCI_ERR_SHAPE;
@@ -410,17 +410,25 @@ cci_status check_distillation(int dtype, int64_t N, int64_t V, const void *logit
 
 extern "C" {
 
+size_t cci_distillation_workspace_size(int64_t N, int64_t V)
+{
+    return N < 1 || V < 1 || V > kMaxLogits || N >= kMaxRows / 8 ? 0 : distillation_workspace(N, V);
+}
+
 cci_status cci_distillation_loss(const void *logits, cci_dtype dtype, int64_t N, int64_t V, int64_t ldx,
                                  const int32_t *top_idx, const float *top_logp, int k, float temperature, int tail,
-                                 float *loss, float *stats, uint32_t *dev_status, cci_stream_t stream)
+                                 float *loss, float *stats, uint32_t *dev_status, void *workspace,
+                                 size_t workspace_bytes, cci_stream_t stream)
 {
     const cci_status st = check_distillation(dtype, N, V, logits, ldx, top_idx, top_logp, k, temperature, stats);
     if (st != CCI_OK) return st;
     if (N > 0 && !loss) return CCI_ERR_NULL;
     if (!aligned(loss, 4)) return CCI_ERR_ALIGN;
     if (N == 0) return CCI_OK;
+    const size_t need = distillation_workspace(N, V);
+    if (need > 0 && (!workspace || workspace_bytes < need || !aligned(workspace, 16))) return CCI_ERR_WORKSPACE;
     return to_status(launch_distillation(logits, dtype, N, V, ldx, top_idx, top_logp, k, temperature, tail != 0, loss,
-                                         stats, dev_status, as_stream(stream)));
+                                         stats, dev_status, workspace, as_stream(stream)));
 }
 
 cci_status cci_distillation_loss_backward(const float *dloss, const void *logits, cci_dtype dtype, int64_t N, int64_t V,

@@ -13,21 +13,22 @@
 // the factor log2(e) / T, which would overflow at the type's lowest value.
 //
 // Rows are walked in groups of eight logits on 16-byte words, whatever their first logit's place; the group at
-// either end is read one by one.  Where the rows alone would not fill the SMs, a cluster of blocks shares one
-// and joins in the first block's shared memory.
-#include <cooperative_groups.h>
-
+// either end is read one by one.  Forward, all rows' groups are cut evenly over as many blocks as the SMs hold, each with eight
+// warps that walk and one that sets the next row's bits, joins the last row's sums and leaves them for a second launch,
+// where a warp a row adds its listed tokens; that launch has read them before the first has ended.  Rows of up to 2048 logits
+// take a warp each, which does all of it.
 #include "cci_kernels.h"
 #include "cci_rowops.cuh"
+#include "cci_tc_common.cuh"
 
 namespace cci {
 namespace distill {
 
-namespace cg = cooperative_groups;
-
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kMaxListed = 128;
-constexpr int kBits = 262144;    // logits that a block has bits for at a time (32 KB)
+constexpr int kPiece = 32768;    // groups that a block has bits for at a time (32 KB, twice)
+// logits of a row that a warp takes by itself, and where there are rows enough for all SMs' warps
+constexpr int kShort = 2048, kShortOfMany = 32768;
 
 struct Args {
     const void *x;
@@ -41,7 +42,9 @@ struct Args {
     const float *dloss;
     void *dx;
     int64_t lddx;
-    int parts;            // blocks of a row, forward
+    // forward: a row's units of 32 groups, blocks that share all rows' units evenly, places for a row's sums
+    int units, blocks, places;
+    float2 *sums;         // [N][places]
     int chunks, steps;    // warps of a row, backward, and their steps of 1024 logits
 };
 
@@ -97,32 +100,39 @@ __device__ __forceinline__ Sums joined(Sums a, Sums b, float c)
     return Sums{m, u + v};
 }
 
-// what a block knows of its part
-struct Part {
-    Sums sums;
-    int bad;
-};
-
 // what a row's list says: the largest listed logit and the sum of exp((x - top) / T); the teacher's sum or its normaliser's
 // logarithm, as in stats; and - sum q_j (x_j - top) / T with the sum of those q_j
 struct Listed {
     float top, sum, given, norm, off, share;
 };
 
-// by a warp, a lane's results those of all
-template <typename T>
-__device__ __forceinline__ Listed listed_of(const Args &a, const T *x, const int32_t *idx, const float *value, int lane)
+// a lane's part of a row's list: indices (-1: none), the teacher's values
+constexpr int kOwn = kMaxListed / 32;
+
+__device__ __forceinline__ void read_list(const Args &a, int64_t n, int lane, int (&at)[kOwn])
 {
-    constexpr int kOwn = kMaxListed / 32;
-    int at[kOwn];
-    float z[kOwn], q[kOwn];
+#pragma unroll
+    for (int i = 0; i < kOwn; ++i) at[i] = lane + 32 * i < a.k ? a.idx[n * a.k + lane + 32 * i] : -1;
+}
+
+// the listed logits and the teacher's values
+template <typename T>
+__device__ __forceinline__ void read_listed(const Args &a, int64_t n, const T *x, int lane, const int (&at)[kOwn],
+                                            float (&z)[kOwn], float (&q)[kOwn])
+{
+#pragma unroll
+    for (int i = 0; i < kOwn; ++i) {
+        q[i] = lane + 32 * i < a.k ? a.value[n * a.k + lane + 32 * i] : 0.f;
+        z[i] = at[i] >= 0 && at[i] < a.V ? row::to_f32(x[at[i]]) : neg_inf();
+    }
+}
+
+// what they say, by a warp, to all its lanes
+__device__ __forceinline__ Listed listed_of(const Args &a, const int (&at)[kOwn], float (&z)[kOwn], float (&q)[kOwn])
+{
     float top = neg_inf(), best = neg_inf();
 #pragma unroll
     for (int i = 0; i < kOwn; ++i) {
-        const int j = lane + 32 * i;
-        at[i] = j < a.k ? idx[j] : -1;
-        q[i] = j < a.k ? value[j] : 0.f;
-        z[i] = at[i] >= 0 && at[i] < a.V ? row::to_f32(x[at[i]]) : neg_inf();
         top = fmaxf(top, z[i]);
         if (at[i] >= 0) best = fmaxf(best, q[i]);
     }
@@ -152,121 +162,133 @@ __device__ __forceinline__ Listed listed_of(const Args &a, const T *x, const int
     return r;
 }
 
-template <typename T, int TPB>
-__global__ void __launch_bounds__(TPB) loss_kernel(const Args a)
+// the bits of a row's listed logits in groups [g0, g1), by a warp; true: an index that is none, or that is listed twice
+__device__ __forceinline__ bool set_bits(uint32_t *bits, const Args &a, const int (&at)[kOwn], int s, int g0, int g1, int lane)
 {
-    constexpr int kU = 4;  // groups on their way a thread
-    extern __shared__ __align__(16) uint32_t bits[];
-    __shared__ Part warps[TPB / 32];
-    __shared__ Part parts[8];
-    __shared__ int bad_flag;
-    const int t = threadIdx.x, lane = t & 31;
-    const int64_t n = blockIdx.x / a.parts;
-    const int part = static_cast<int>(blockIdx.x % a.parts);
-    const T *x = static_cast<const T *>(a.x) + n * a.ldx;
-    const int32_t *idx = a.idx + n * a.k;
-    const float c = kLog2e / a.T;
-    const int s = shift_of(x), V = a.V;
-    const int groups = static_cast<int>((static_cast<int64_t>(V) + s + 7) / 8);
-    const int each = ((groups + a.parts - 1) / a.parts + 31) / 32 * 32;
-    const int first = part * each < groups ? part * each : groups, last = first + each < groups ? first + each : groups;
-    Sums sums{neg_inf(), 0.f};
-    Listed mine{};
-    if (t == 0) bad_flag = 0;
-    for (int g0 = first; g0 < last || g0 == first; g0 += kBits / 8) {
-        const int g1 = g0 + kBits / 8 < last ? g0 + kBits / 8 : last;
-        // the first groups are on their way while the bits are set
-        row::Raw<T, 8> raw[kU];
-        auto load = [&](int g) {
+    for (int i = lane; i < (g1 - g0 + 15) / 16; i += 32) reinterpret_cast<uint4 *>(bits)[i] = make_uint4(0u, 0u, 0u, 0u);
+    __syncwarp();
+    bool bad = false;
 #pragma unroll
-            for (int u = 0; u < kU; ++u) {
-                const int q = g + u * TPB + lane;
-                raw[u] = load_group(x, q < g1 ? 8 * q - s : V, V);
-            }
-        };
-        int g = g0 + (t & ~31);
-        if (g < g1) load(g);
-        __syncthreads();
-        for (int i = t; i < (g1 - g0 + 3) / 4; i += TPB) bits[i] = 0u;
-        __syncthreads();
-        for (int j = t; j < a.k; j += TPB) {
-            const int32_t v = idx[j];
-            if (v < -1 || v >= V) bad_flag = 1;
-            const int64_t b = static_cast<int64_t>(v) + s - 8 * static_cast<int64_t>(g0);
-            if (v >= 0 && v < V && b >= 0 && b < 8 * static_cast<int64_t>(g1 - g0)) {
-                const uint32_t bit = 1u << (b & 31);
-                if (atomicOr(&bits[b >> 5], bit) & bit) bad_flag = 1;
-            }
-        }
-        __syncthreads();
-        const uint8_t *mask = reinterpret_cast<const uint8_t *>(bits);
-        if (g0 == first && part == 0 && t < 32) mine = listed_of(a, x, idx, a.value + n * a.k, lane);
-        // the bounds are the same for a warp's lanes, so that they find their common maximum together; the next groups
-        // are on their way while these are summed
-        for (; g < g1; g += kU * TPB) {
-            float f[kU][8];
-#pragma unroll
-            for (int u = 0; u < kU; ++u) row::unpack<T, 8>(raw[u], f[u]);
-            if (g + kU * TPB < g1) load(g + kU * TPB);
-            float top = neg_inf();
-#pragma unroll
-            for (int u = 0; u < kU; ++u) {
-                const int q = g + u * TPB + lane;
-                const uint32_t m = q < g1 ? mask[q - g0] : 0u;
-                if (m) {
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) f[u][j] = m >> j & 1u ? neg_inf() : f[u][j];
-                }
-#pragma unroll
-                for (int j = 0; j < 8; ++j) top = fmaxf(top, f[u][j]);
-            }
-            asm volatile("redux.sync.max.f32 %0, %0, 0xffffffff;" : "+f"(top));
-            if (top > sums.m) {
-                sums.s = sums.s == 0.f ? 0.f : sums.s * ex2((sums.m - top) * c);
-                sums.m = top;
-            }
-            const float from = ref_of(sums.m);
-            const unsigned long long neg = pack2(-from, -from), c2 = pack2(c, c);
-            unsigned long long e[2] = {};
-#pragma unroll
-            for (int u = 0; u < kU; ++u)
-#pragma unroll
-                for (int j = 0; j < 8; j += 2) {
-                    const unsigned long long y = row::mul2(row::add2(pack2(f[u][j], f[u][j + 1]), neg), c2);
-                    e[j / 2 & 1] = row::add2(e[j / 2 & 1], pack2(ex2(lo_of(y)), ex2(hi_of(y))));
-                }
-            const unsigned long long both = row::add2(e[0], e[1]);
-            sums.s += lo_of(both) + hi_of(both);
+    for (int i = 0; i < kOwn; ++i) {
+        const int v = at[i];
+        if (v < -1 || v >= a.V) bad = true;
+        const int b = v + s - 8 * g0;
+        if (v >= 0 && v < a.V && b >= 0 && b < 8 * (g1 - g0)) {
+            const uint32_t bit = 1u << (b & 31);
+            if (atomicOr(&bits[b >> 5], bit) & bit) bad = true;
         }
     }
+    __syncwarp();
+    return __any_sync(0xffffffffu, bad);
+}
+
+// the largest of U groups as they lie in memory (NaN is no maximum)
+template <typename T, int U>
+__device__ __forceinline__ float largest(const row::Raw<T, 8> (&raw)[U])
+{
+    if constexpr (sizeof(T) == 2) {
+        uint32_t m = 0xff80ff80u;  // two at a time
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const uint32_t w[4] = {raw[u].w[0].x, raw[u].w[0].y, raw[u].w[0].z, raw[u].w[0].w};
+#pragma unroll
+            for (int j = 0; j < 4; ++j) asm("max.bf16x2 %0, %0, %1;" : "+r"(m) : "r"(w[j]));
+        }
+        return fmaxf(__uint_as_float(m << 16), __uint_as_float(m & 0xffff0000u));
+    } else {
+        float m = neg_inf();
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const uint4 w = raw[u].w[i];
+                asm("max.f32 %0, %0, %1, %2;" : "+f"(m) : "f"(__uint_as_float(w.x)), "f"(__uint_as_float(w.y)));
+                asm("max.f32 %0, %0, %1, %2;" : "+f"(m) : "f"(__uint_as_float(w.z)), "f"(__uint_as_float(w.w)));
+            }
+        return m;
+    }
+}
+
+// A warp's sums while it walks, c = log2(e) / T: s = sum of 2^(x c - r) with r the product m c as it is rounded.  One fused
+// operation takes a logit to its exponent, and its only rounding is that of the exponent, as if the difference x - m were
+// taken first: that r is not quite m c (`off` is what it lacks) is one factor for all, put right when the maximum moves and at the end.
+// Where m c overflows, at the type's lowest value, the difference does come first
+struct Walk {
+    float m, s, r, off;
+    __device__ __forceinline__ Walk() : m(neg_inf()), s(0.f), r(0.f), off(0.f) {}
+    __device__ __forceinline__ bool far() const { return !(fabsf(r) < 1e38f); }
+    __device__ __forceinline__ Sums sums() const { return Sums{m, s == 0.f ? 0.f : s * ex2(-off)}; }
+    __device__ __forceinline__ void raise(float top, float c)
+    {
+        s = s == 0.f ? 0.f : s * ex2(-off) * ex2((m - top) * c);
+        m = top;
+        r = top * c;
+        off = far() ? 0.f : fmaf(top, c, -r);
+        s *= ex2(off);
+    }
+};
+
+// adds U groups a lane to a warp's sums, without their listed logits (a bit each)
+template <typename T, int U>
+__device__ __forceinline__ void add_groups(Walk &walk, row::Raw<T, 8> (&raw)[U], const uint32_t (&listed)[U], float c)
+{
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        if (listed[u]) {
+            constexpr int kEach = 4 / static_cast<int>(sizeof(T));
+#pragma unroll
+            for (int i = 0; i < static_cast<int>(sizeof(T)) / 2; ++i) {
+                uint32_t w[4] = {raw[u].w[i].x, raw[u].w[i].y, raw[u].w[i].z, raw[u].w[i].w};
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const uint32_t m = listed[u] >> (4 * i + j) * kEach;
+                    if constexpr (sizeof(T) == 4) {
+                        w[j] = m & 1u ? 0xff800000u : w[j];
+                    } else {
+                        w[j] = m & 1u ? (w[j] & 0xffff0000u) | 0xff80u : w[j];
+                        w[j] = m & 2u ? (w[j] & 0xffffu) | 0xff800000u : w[j];
+                    }
+                }
+                raw[u].w[i] = make_uint4(w[0], w[1], w[2], w[3]);
+            }
+        }
+    }
+    float top = largest<T, U>(raw);
+    asm volatile("redux.sync.max.f32 %0, %0, 0xffffffff;" : "+f"(top));
+    if (top > walk.m) walk.raise(top, c);
+    float e[4] = {};
+    if (!walk.far()) {
+        const float minus = -walk.r;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            float f[8];
+            row::unpack<T, 8>(raw[u], f);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) e[j & 3] += ex2(fmaf(f[j], c, minus));
+        }
+    } else {
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            float f[8];
+            row::unpack<T, 8>(raw[u], f);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) e[j & 3] += ex2((f[j] - walk.m) * c);
+        }
+    }
+    walk.s += (e[0] + e[1]) + (e[2] + e[3]);
+}
+
+__device__ __forceinline__ Sums warp_joined(Sums a, float c)
+{
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1)
-        sums = joined(sums, Sums{__shfl_xor_sync(0xffffffffu, sums.m, o), __shfl_xor_sync(0xffffffffu, sums.s, o)}, c);
-    if (lane == 0) warps[t >> 5].sums = sums;
-    __syncthreads();
-    if (t < 32) {
-        sums = lane < TPB / 32 ? warps[lane].sums : Sums{neg_inf(), 0.f};
-#pragma unroll
-        for (int o = 4; o > 0; o >>= 1)
-            sums = joined(sums, Sums{__shfl_xor_sync(0xffffffffu, sums.m, o), __shfl_xor_sync(0xffffffffu, sums.s, o)}, c);
-    }
-    int bad = bad_flag;
-    if (a.parts > 1) {
-        cg::cluster_group cluster = cg::this_cluster();
-        if (t == 0) *cluster.map_shared_rank(&parts[part], 0) = Part{sums, bad};
-        cluster.sync();
-        if (part != 0) return;
-        if (t < 32) {
-            const Part p = lane < a.parts ? parts[lane] : Part{{neg_inf(), 0.f}, 0};
-            sums = p.sums;
-            bad = __any_sync(0xffffffffu, p.bad);
-#pragma unroll
-            for (int o = 4; o > 0; o >>= 1)
-                sums = joined(sums, Sums{__shfl_xor_sync(0xffffffffu, sums.m, o), __shfl_xor_sync(0xffffffffu, sums.s, o)}, c);
-        }
-    }
-    if (t > 0) return;
-    // the listed join, and the teacher has its say
+        a = joined(a, Sums{__shfl_xor_sync(0xffffffffu, a.m, o), __shfl_xor_sync(0xffffffffu, a.s, o)}, c);
+    return a;
+}
+
+// a row's loss and stats from the sums over what is not listed, and its list (one lane)
+__device__ __forceinline__ void finish(const Args &a, int64_t n, const Sums &sums, const Listed &mine, float c, bool bad)
+{
     const float m = fmaxf(sums.m, mine.top), from = ref_of(m);
     const float rest = sums.s == 0.f ? 0.f : sums.s * ex2((sums.m - from) * c);
     const float sum = rest + (mine.sum == 0.f ? 0.f : mine.sum * ex2((mine.top - from) * c));
@@ -281,6 +303,220 @@ __global__ void __launch_bounds__(TPB) loss_kernel(const Args a)
     if (bad) report(a.status, CCI_ERR_INDEX);
     a.loss[n] = bad ? nan_f() : loss;
     reinterpret_cast<float4 *>(a.stats)[n] = make_float4(bad ? nan_f() : m / a.T, log_s, log_rest, mine.norm);
+}
+
+// ---- short rows, or many: a warp each.  The argument: bytes of a row's bits ----
+template <typename T>
+__global__ void __launch_bounds__(256, 4) short_kernel(const Args a, int bytes)
+{
+    constexpr int kU = 8 / sizeof(T);
+    extern __shared__ __align__(16) unsigned char shared[];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int64_t n = static_cast<int64_t>(blockIdx.x) * 8 + warp;
+    if (n >= a.N) return;
+    unsigned char *bits = shared + warp * bytes;
+    const T *x = static_cast<const T *>(a.x) + n * a.ldx;
+    const float c = kLog2e / a.T;
+    const int s = shift_of(x), groups = (a.V + s + 7) / 8;
+    int at[kOwn];
+    float z[kOwn], q[kOwn];
+    read_list(a, n, lane, at);
+    row::Raw<T, 8> next[kU];
+    auto load = [&](int g) {
+#pragma unroll
+        for (int u = 0; u < kU; ++u) {
+            const int i = g + 32 * u + lane;
+            next[u] = load_group(x, i < groups ? 8 * i - s : a.V, a.V);
+        }
+    };
+    load(0);
+    read_listed(a, n, x, lane, at, z, q);
+    const bool bad = set_bits(reinterpret_cast<uint32_t *>(bits), a, at, s, 0, groups, lane);
+    Walk walk;
+    for (int g = 0; g < groups; g += 32 * kU) {
+        row::Raw<T, 8> raw[kU];
+        uint32_t listed[kU];
+#pragma unroll
+        for (int u = 0; u < kU; ++u) {
+            const int i = g + 32 * u + lane;
+            raw[u] = next[u];
+            listed[u] = i < groups ? bits[i] : 0u;
+        }
+        if (g + 32 * kU < groups) load(g + 32 * kU);
+        add_groups<T, kU>(walk, raw, listed, c);
+    }
+    const Listed mine = listed_of(a, at, z, q);
+    const Sums sums = warp_joined(walk.sums(), c);
+    if (lane == 0) finish(a, n, sums, mine, c, bad);
+}
+
+// ---- longer ones: the sums over what is not listed ----
+// of `all` units cut evenly over `blocks`, the block that holds unit u
+__device__ __forceinline__ int holder(int64_t u, int64_t all, int blocks)
+{
+    int b = static_cast<int>(u * blocks / all);
+    while (all * (b + 1) / blocks <= u) ++b;
+    return b;
+}
+
+// a block's units [u, end), piece by piece: groups [g0, g1) of row n
+struct Pieces {
+    int64_t u, end, n;
+    int unit;  // of the row, where the next piece begins
+    int g0, g1;
+    __device__ __forceinline__ Pieces(const Args &a, int64_t begin, int64_t end_) : u(begin), end(end_), n(begin / a.units)
+    {
+        unit = static_cast<int>(begin - n * a.units);
+        g1 = 0;
+    }
+    // the next piece (the first after a row's last is the next row's); false: there is none
+    __device__ __forceinline__ bool next(const Args &a)
+    {
+        if (u >= end) return false;
+        if (unit == a.units) {
+            unit = 0;
+            ++n;
+        }
+        int count = a.units - unit;
+        if (count > end - u) count = static_cast<int>(end - u);
+        if (count > kPiece / 32) count = kPiece / 32;
+        g0 = 32 * unit;
+        g1 = g0 + 32 * count;
+        unit += count;
+        u += count;
+        return true;
+    }
+};
+
+constexpr int kWalkers = 8;
+
+// The last argument: bytes of a piece's bits, of which there are two
+template <typename T>
+__global__ void __launch_bounds__(32 * (kWalkers + 1), 3) sums_kernel(const Args a, int bytes)
+{
+    constexpr int kU = 8 / sizeof(T), kStep = 32 * kWalkers;  // groups that a lane sums at a time
+    extern __shared__ __align__(16) unsigned char bits[];
+    __shared__ Sums warps[2][kWalkers];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int64_t all = a.N * a.units;
+    const int64_t begin = all * blockIdx.x / a.blocks, end = all * (blockIdx.x + 1) / a.blocks;
+    const float c = kLog2e / a.T;
+    const T *rows = static_cast<const T *>(a.x);
+    tc::launch_next_grid();  // the second launch, which waits for this one's end
+    Pieces p(a, begin, end);
+    if (warp < kWalkers) {
+        row::Raw<T, 8> next[kU];
+        const T *x = rows;
+        int s = 0;
+        auto load = [&](int g) {
+#pragma unroll
+            for (int u = 0; u < kU; ++u) {
+                const int q = g + u * kStep + lane;
+                next[u] = load_group(x, q < p.g1 ? 8 * q - s : a.V, a.V);
+            }
+        };
+        auto enter = [&]() {
+            if (!p.next(a)) return false;
+            x = rows + p.n * a.ldx;
+            s = shift_of(x);
+            if (p.g0 + 32 * warp < p.g1) load(p.g0 + 32 * warp);
+            return true;
+        };
+        enter();
+        for (int k = 0;; ++k) {
+            tc::named_sync(1, 32 * (kWalkers + 1));  // this piece's bits are set
+            const unsigned char *mask = bits + (k & 1) * bytes;
+            Walk walk;
+            // the bounds are the same for a warp's lanes, so that they find their common maximum together; the next groups
+            // are on their way while these are summed
+            for (int g = p.g0 + 32 * warp; g < p.g1; g += kU * kStep) {
+                row::Raw<T, 8> raw[kU];
+                uint32_t listed[kU];
+#pragma unroll
+                for (int u = 0; u < kU; ++u) {
+                    const int q = g + u * kStep + lane;
+                    raw[u] = next[u];
+                    listed[u] = q < p.g1 ? mask[q - p.g0] : 0u;
+                }
+                if (g + kU * kStep < p.g1) load(g + kU * kStep);
+                add_groups<T, kU>(walk, raw, listed, c);
+            }
+            const bool more = enter();
+            const Sums sums = warp_joined(walk.sums(), c);
+            if (lane == 0) warps[k & 1][warp] = sums;
+            if (!more) break;
+        }
+        tc::named_sync(1, 32 * (kWalkers + 1));
+    } else {
+        // the warp beside them: two pieces ahead with the list, one with its bits, one behind with the sums
+        int at[kOwn];
+        Pieces list = p, last = p;
+        bool bad = false, next_bad = false;
+        bool more = list.next(a);
+        read_list(a, list.n, lane, at);
+        Sums sums{neg_inf(), 0.f};
+        auto prepare = [&](int k) {  // the bits of the piece whose list is at hand, then the next list
+            p = list;
+            next_bad = set_bits(reinterpret_cast<uint32_t *>(bits + (k & 1) * bytes), a, at, shift_of(rows + p.n * a.ldx), p.g0, p.g1, lane);
+            more = list.next(a);
+            if (more) read_list(a, list.n, lane, at);
+        };
+        auto join = [&](int k, bool final) {
+            sums = joined(sums, warp_joined(lane < kWalkers ? warps[k & 1][lane] : Sums{neg_inf(), 0.f}, c), c);
+            if (final || last.g1 == 32 * a.units) {
+                if (lane == 0) {
+                    // a row that begins here is the first block's
+                    const int64_t first = last.n * a.units;
+                    const int place = first >= begin ? 0 : static_cast<int>(blockIdx.x) - holder(first, all, a.blocks);
+                    a.sums[last.n * a.places + place] = make_float2(sums.m, bad ? nan_f() : sums.s);
+                    if (bad) report(a.status, CCI_ERR_INDEX);
+                }
+                sums = Sums{neg_inf(), 0.f};
+                bad = false;
+            }
+        };
+        prepare(0);
+        for (int k = 0;; ++k) {
+            const Pieces now = p;
+            const bool now_bad = next_bad, left = more;
+            tc::named_sync(1, 32 * (kWalkers + 1));
+            if (k > 0) join(k - 1, false);
+            bad = bad || now_bad;  // of the row that `now` is of
+            last = now;
+            if (left) {
+                prepare(k + 1);
+            } else {
+                tc::named_sync(1, 32 * (kWalkers + 1));
+                join(k, true);
+                break;
+            }
+        }
+    }
+}
+
+// a row's loss from its sums and its list, a warp a row.  The list is read while the sums are taken
+template <typename T>
+__global__ void __launch_bounds__(256) loss_kernel(const Args a)
+{
+    const int lane = threadIdx.x & 31;
+    const int64_t n = static_cast<int64_t>(blockIdx.x) * 8 + (threadIdx.x >> 5), all = a.N * a.units;
+    if (n >= a.N) return;
+    const T *x = static_cast<const T *>(a.x) + n * a.ldx;
+    const float c = kLog2e / a.T;
+    int at[kOwn];
+    float z[kOwn], q[kOwn];
+    read_list(a, n, lane, at);
+    read_listed(a, n, x, lane, at, z, q);
+    const Listed mine = listed_of(a, at, z, q);
+    const int count = holder(n * a.units + a.units - 1, all, a.blocks) - holder(n * a.units, all, a.blocks) + 1;
+    tc::wait_prior_grid();
+    Sums sums{neg_inf(), 0.f};
+    for (int i = lane; i < count; i += 32) {
+        const float2 part = a.sums[n * a.places + i];
+        sums = joined(sums, Sums{part.x, part.y}, c);
+    }
+    sums = warp_joined(sums, c);
+    if (lane == 0) finish(a, n, sums, mine, c, false);
 }
 
 // ---- gradient: a warp takes one to four steps of 128 groups of a row by itself; the next step's logits are on their way while
@@ -379,31 +615,60 @@ __global__ void __launch_bounds__(256) gradient_kernel(const Args a)
 // host
 // ---------------------------------------------------------------------------
 
-constexpr int kShort = 2048;  // rows of up to so many logits take two warps
-
-template <typename T, int TPB>
-cudaError_t launch_loss(Args a, cudaStream_t stream)
+// a warp a row (bf16 8192 x 4096: 25 us, 62 where eight warps share each; 8192 x 16384: 58 and 88)
+bool by_warps(int64_t N, int64_t V)
 {
-    // blocks of a row: about 1024 blocks in all, each with 4096 logits or more
-    int parts = 1;
-    while (parts < 8 && a.N * parts < 1024 && a.V / (2 * parts) >= 4096) parts *= 2;
-    a.parts = parts;
-    const int64_t groups = (static_cast<int64_t>(a.V) + 14) / 8;
-    const int64_t each = ((groups + parts - 1) / parts + 31) / 32 * 32;
-    const size_t bytes = static_cast<size_t>(each < kBits / 8 ? each : kBits / 8) + 16;
+    return V <= kShort || (V <= kShortOfMany && N >= 24 * static_cast<int64_t>(row::sm_count()));
+}
+
+// how a forward call's rows are cut otherwise
+struct Cut {
+    int units, blocks, places;
+};
+
+Cut cut_of(int64_t N, int64_t V)
+{
+    Cut c{};
+    if (N < 1 || by_warps(N, V)) return c;
+    const int64_t units = ((V + 14) / 8 + 31) / 32, most = 3 * static_cast<int64_t>(row::sm_count());
+    int64_t blocks = N * units / kWalkers;  // a unit for each warp at least
+    if (blocks > most) blocks = most;
+    c.units = static_cast<int>(units);
+    c.blocks = static_cast<int>(blocks < 1 ? 1 : blocks);
+    c.places = static_cast<int>((c.blocks + N - 1) / N) + 1;  // blocks that a row's units lie with
+    return c;
+}
+
+template <typename T>
+cudaError_t launch_loss(Args a, float2 *workspace, cudaStream_t stream)
+{
+    if (by_warps(a.N, a.V)) {
+        const int bytes = ((a.V + 14) / 8 + 15) / 16 * 16;
+        short_kernel<T><<<static_cast<unsigned>((a.N + 7) / 8), 256, static_cast<size_t>(8 * bytes), stream>>>(a, bytes);
+        return cudaGetLastError();
+    }
+    const Cut cut = cut_of(a.N, a.V);
+    a.units = cut.units;
+    a.blocks = cut.blocks;
+    a.places = cut.places;
+    a.sums = cut.places <= 2 ? reinterpret_cast<float2 *>(a.stats) : workspace;  // two fit where the stats come later
+    const int bits = 32 * a.units < kPiece ? 32 * a.units : kPiece;
+    static SmemAttrCache attr_cache;
+    const cudaError_t attr = smem_attr_once(sums_kernel<T>, 2 * kPiece, attr_cache);
+    if (attr != cudaSuccess) return attr;
+    sums_kernel<T><<<static_cast<unsigned>(a.blocks), 32 * (kWalkers + 1), static_cast<size_t>(2 * bits), stream>>>(a, bits);
+    cudaError_t e = cudaGetLastError();
+    if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(static_cast<unsigned>(a.N * parts));
-    cfg.blockDim = dim3(TPB);
-    cfg.dynamicSmemBytes = (bytes + 15) / 16 * 16;
+    cfg.gridDim = dim3(static_cast<unsigned>((a.N + 7) / 8));
+    cfg.blockDim = dim3(256);
     cfg.stream = stream;
     cudaLaunchAttribute la[1];
-    la[0].id = cudaLaunchAttributeClusterDimension;
-    la[0].val.clusterDim.x = static_cast<unsigned>(parts);
-    la[0].val.clusterDim.y = 1;
-    la[0].val.clusterDim.z = 1;
+    la[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    la[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = la;
-    cfg.numAttrs = parts > 1 ? 1 : 0;
-    const cudaError_t e = cudaLaunchKernelEx(&cfg, loss_kernel<T, TPB>, static_cast<const Args>(a));
+    cfg.numAttrs = 1;
+    e = cudaLaunchKernelEx(&cfg, loss_kernel<T>, static_cast<const Args>(a));
     return e == cudaSuccess ? cudaGetLastError() : e;
 }
 
@@ -423,9 +688,15 @@ cudaError_t launch_gradient(Args a, cudaStream_t stream)
 
 }  // namespace distill
 
+size_t distillation_workspace(int64_t N, int64_t V)
+{
+    const distill::Cut c = distill::cut_of(N, V);
+    return c.places <= 2 ? 0 : static_cast<size_t>(N) * c.places * sizeof(float2);
+}
+
 cudaError_t launch_distillation(const void *x, int dtype, int64_t N, int64_t V, int64_t ldx, const int32_t *idx,
                                 const float *value, int k, float T, int tail, float *loss, float *stats,
-                                uint32_t *status, cudaStream_t stream)
+                                uint32_t *status, void *workspace, cudaStream_t stream)
 {
     using namespace distill;
     Args a{};
@@ -441,8 +712,8 @@ cudaError_t launch_distillation(const void *x, int dtype, int64_t N, int64_t V, 
     a.loss = loss;
     a.stats = stats;
     a.status = status;
-    if (dtype == CCI_F32) return V <= kShort ? launch_loss<float, 64>(a, stream) : launch_loss<float, 256>(a, stream);
-    return V <= kShort ? launch_loss<uint16_t, 64>(a, stream) : launch_loss<uint16_t, 256>(a, stream);
+    float2 *w = static_cast<float2 *>(workspace);
+    return dtype == CCI_F32 ? launch_loss<float>(a, w, stream) : launch_loss<uint16_t>(a, w, stream);
 }
 
 cudaError_t launch_distillation_backward(const float *dloss, const void *x, int dtype, int64_t N, int64_t V, int64_t ldx,

@@ -94,10 +94,11 @@ size_t gated_workspace(int dtype, int64_t N, int64_t D, int64_t F, int call);
 cudaError_t launch_gated(const GatedArgs &a, cudaStream_t stream);
 cudaError_t launch_gated_backward(const GatedArgs &a, cudaStream_t stream);
 
-// distillation from a teacher's top logits (cci_distill.cu)
+// distillation from a teacher's top logits (cci_distill.cu); workspace: distillation_workspace bytes
+size_t distillation_workspace(int64_t N, int64_t V);
 cudaError_t launch_distillation(const void *x, int dtype, int64_t N, int64_t V, int64_t ldx, const int32_t *idx,
                                 const float *value, int k, float T, int tail, float *loss, float *stats,
-                                uint32_t *status, cudaStream_t stream);
+                                uint32_t *status, void *workspace, cudaStream_t stream);
 cudaError_t launch_distillation_backward(const float *dloss, const void *x, int dtype, int64_t N, int64_t V, int64_t ldx,
                                          const int32_t *idx, const float *value, int k, float T, int tail,
                                          const float *stats, void *dx, int64_t lddx, cudaStream_t stream);

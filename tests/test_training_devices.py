@@ -39,7 +39,7 @@ CALLS = {
 }
 TYPES = {"targets": i64, "top_idx": i32}
 STATUS = ("linear_cross_entropy", "linear_cross_entropy_backward", "distillation_loss")
-WORKSPACE = ("rms_norm_backward", "linear_cross_entropy", "linear_cross_entropy_backward")
+WORKSPACE = ("rms_norm_backward", "linear_cross_entropy", "linear_cross_entropy_backward", "distillation_loss")
 
 
 def names(call):

@@ -37,8 +37,8 @@ def ce_back(lib, dl=P, x=P, dt=1, N=4, D=64, w=P, V=100, t=P, stats=P, dx=P, dw=
     return lib.cci_linear_cross_entropy_backward(dl, x, dt, N, D, w, V, t, -100, stats, dx, dw, None, ws, wb, None)
 
 
-def kd(lib, x=P, dt=1, N=4, V=100, ld=100, i=P, v=P, k=5, T=1.0, tail=0, loss=P, stats=P):
-    return lib.cci_distillation_loss(x, dt, N, V, ld, i, v, k, T, tail, loss, stats, None, None)
+def kd(lib, x=P, dt=1, N=4, V=100, ld=100, i=P, v=P, k=5, T=1.0, tail=0, loss=P, stats=P, ws=P, wb=1 << 30):
+    return lib.cci_distillation_loss(x, dt, N, V, ld, i, v, k, T, tail, loss, stats, None, ws, wb, None)
 
 
 def kd_back(lib, dl=P, x=P, dt=1, N=4, V=100, ld=100, i=P, v=P, k=5, T=1.0, tail=0, stats=P, dx=P, ldd=100):
@@ -92,7 +92,11 @@ KD = [(dict(x=0), NULL), (dict(i=0), NULL), (dict(v=0), NULL), (dict(stats=0), N
       (dict(T=float("inf")), VALUE), (dict(x=P + 1), ALIGN), (dict(i=P + 2), ALIGN), (dict(v=P + 2), ALIGN), (dict(stats=P + 8), ALIGN)]
 
 
-@pytest.mark.parametrize("change,want", KD + [(dict(loss=0), NULL), (dict(loss=P + 2), ALIGN)])
+LONG = dict(N=1, V=1 << 24, ld=1 << 24)  # one row for many blocks
+
+
+@pytest.mark.parametrize("change,want", KD + [(dict(loss=0), NULL), (dict(loss=P + 2), ALIGN), (dict(ws=0, **LONG), WORKSPACE),
+                                              (dict(ws=P + 8, **LONG), WORKSPACE), (dict(wb=8, **LONG), WORKSPACE)])
 def test_distillation(lib, change, want):
     assert kd(lib, **change) == want
 
@@ -106,7 +110,7 @@ def test_nothing_to_do_needs_no_device(lib):
     assert rms(lib, N=0, x=0, y=0, h=0, r=0) == OK
     assert rms8(lib, N=0, x=0, q=0, scales=0, h=0, r=0) == OK
     assert ce(lib, N=0, x=0, t=0, loss=0, stats=0, ws=0, wb=0) == OK
-    assert kd(lib, N=0, x=0, i=0, v=0, loss=0, stats=0) == OK
+    assert kd(lib, N=0, x=0, i=0, v=0, loss=0, stats=0, ws=0, wb=0) == OK
     assert kd_back(lib, N=0, x=0, i=0, v=0, stats=0, dx=0, dl=0) == OK
     assert rms_back(lib, N=0, dy=0, h=0, dh=0, rstd=0, dx=0, dw=0, ws=0, wb=0) == OK
     assert ce_back(lib, N=0, x=0, t=0, dl=0, stats=0, dx=0, dw=0, ws=0, wb=0) == OK
@@ -115,6 +119,9 @@ def test_nothing_to_do_needs_no_device(lib):
 def test_workspace_sizes(lib):
     assert lib.cci_rms_norm_workspace_size(0, 64) == 0 and lib.cci_rms_norm_workspace_size(4, 0) == 0
     assert lib.cci_rms_norm_workspace_size(1, 64) == 256
+    for N, V in ((0, 100000), (1, 0), (1, (1 << 24) + 1), (5, 2048), (100000, 50000)):
+        assert lib.cci_distillation_workspace_size(N, V) == 0
+    assert lib.cci_distillation_workspace_size(1, 1 << 24) >= 8
     for call in (cci.HEAD_FORWARD, cci.HEAD_BACKWARD):
         for bad in ((2, 4, 64, 100), (1, 0, 64, 100), (1, 4, 0, 100), (1, 4, 64, 0), (1, 1 << 30, 64, 100)):
             assert lib.cci_head_workspace_size(call, *bad) == 0
