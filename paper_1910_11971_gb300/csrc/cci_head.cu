@@ -540,8 +540,8 @@ struct Layout {
     size_t total;
 };
 
-// few fp32 tokens forward read the weights as they are (cci_head_few.cuh)
-bool few_tokens(int dtype, int64_t N, int call) { return call == CCI_HEAD_FORWARD && dtype == CCI_F32 && N <= kFewTokens; }
+// few fp32 tokens read the weights as they are (cci_head_few.cuh)
+bool few_tokens(int dtype, int64_t N) { return dtype == CCI_F32 && N <= kFewTokens; }
 
 Layout layout(int dtype, int64_t N, int64_t D, int64_t V, int call)
 {
@@ -561,9 +561,12 @@ Layout layout(int dtype, int64_t N, int64_t D, int64_t V, int call)
     if (l.piece > V) l.piece = V;
     if (f32) {
         l.x = take(6 * N * D);
-        if (!few_tokens(dtype, N, call)) l.w = take(6 * l.piece * D);
+        if (!few_tokens(dtype, N)) l.w = take(6 * l.piece * D);
     }
-    if (few_tokens(dtype, N, call)) {
+    if (few_tokens(dtype, N) && call == CCI_HEAD_BACKWARD) {
+        l.p = take(4 * V * few_pitch(N));
+        l.products = take(4 * few_slices(N, D, V, ws::sm_count()) * N * D);
+    } else if (few_tokens(dtype, N)) {
         l.parts = take(few_blocks(V, ws::sm_count()) * N * static_cast<int64_t>(sizeof(float2)));
         l.at_target = take(N * 4);
     } else if (call == CCI_HEAD_FORWARD) {
@@ -656,6 +659,20 @@ const void *rows_at(const HeadArgs &a, int64_t c)
     return static_cast<const char *>(a.W) + c * a.D * (a.dtype == CCI_F32 ? 4 : 2);
 }
 
+FewParams few_params(const HeadArgs &a, const void *x_planes)
+{
+    FewParams f{};
+    f.x = static_cast<const uint16_t *>(x_planes);
+    f.w = static_cast<const float *>(a.W);
+    f.N = static_cast<int>(a.N);
+    f.D = static_cast<int>(a.D);
+    f.V = a.V;
+    f.targets = a.targets;
+    f.ignore = a.ignore;
+    f.status = a.status;
+    return f;
+}
+
 }  // namespace head
 
 size_t head_workspace(int dtype, int64_t N, int64_t D, int64_t V, int call)
@@ -684,11 +701,12 @@ cudaError_t launch_head(const HeadArgs &a, cudaStream_t stream)
     int64_t count = 0;
     if (f32) e = planes(a.X, base + l.x, a.N * a.D, stream);
     const Operand x{f32 ? base + l.x : a.X, a.N, a.D, f32 ? 3 : 1};
-    const bool few = few_tokens(a.dtype, a.N, CCI_HEAD_FORWARD);
+    const bool few = few_tokens(a.dtype, a.N);
     if (few && e == cudaSuccess) {
-        const FewParams f{static_cast<const uint16_t *>(x.data), static_cast<const float *>(a.W), static_cast<int>(a.N),
-                          static_cast<int>(a.D), a.V, 0, a.targets, a.ignore, parts, p.at_target};
-        e = launch_few(f, ws::sm_count(), stream);
+        FewParams f = few_params(a, x.data);
+        f.parts = parts;
+        f.at_target = p.at_target;
+        e = launch_few<false>(f, ws::sm_count(), stream);
         count = few_blocks(a.V, ws::sm_count());
     }
     for (int64_t c = 0; !few && c < a.V && e == cudaSuccess; c += l.piece) {
@@ -748,6 +766,18 @@ cudaError_t launch_head_backward(const HeadArgs &a, cudaStream_t stream)
     const bool sums = !f32 && l.piece < a.V;  // dX in fp32 until the last piece
     if (f32) e = planes(a.X, base + l.x, a.N * a.D, stream);
     const Operand x{f32 ? base + l.x : a.X, a.N, a.D, np};
+    if (few_tokens(a.dtype, a.N)) {
+        if (e != cudaSuccess) return e;
+        FewParams f = few_params(a, x.data);
+        f.stats = a.stats;
+        f.dloss = a.dloss;
+        f.probs = reinterpret_cast<float *>(base + l.p);
+        e = launch_few<true>(f, ws::sm_count(), stream);
+        if (e != cudaSuccess) return e;
+        const FewGradients g{static_cast<const float *>(a.X), f.w, f.probs, f.N, f.D, a.V, 0, static_cast<float *>(a.dW),
+                             a.dX ? reinterpret_cast<float *>(base + l.products) : nullptr};
+        return launch_few_gradients(g, ws::sm_count(), static_cast<float *>(a.dX), stream);
+    }
     for (int64_t c = 0; c < a.V && e == cudaSuccess; c += l.piece) {
         const int64_t n = a.V - c < l.piece ? a.V - c : l.piece;
         const void *w = rows_at(a, c);

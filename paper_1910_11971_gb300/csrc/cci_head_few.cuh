@@ -1,4 +1,4 @@
-// cci_head_few.cuh -- the cross entropy of up to 32 tokens from a head's fp32 inputs.
+// cci_head_few.cuh -- the cross entropy of up to 32 tokens from a head's fp32 inputs, and its gradients.
 //
 // The head's weights are all that is read, once, as they are: writing W's planes first, as for more tokens
 // (cci_head.cu), moves four times its bytes (2 tokens, 3392 x 4076: 96 us, 26 so; 16 tokens, 4096 x 65536 fp32 240 us of
@@ -8,6 +8,11 @@
 // bits each; the six products of planes are those of cci_gated.cuh.  The warps' sums meet in shared memory, where each
 // token's maximum and sum of exponentials are taken.  bf16 tokens, however few, go by the tiles of cci_head.cu, whose copies
 // keep more on its way (1 token, 4096 x 131072: 203 us through here, 166 so).
+//
+// Backward the same walk gives P [V][tokens] in fp32, and one pass over the weights takes both gradients from it with
+// fused multiply-adds: a thread holds its columns of X and of dX for all tokens, reads a weight, adds P times it to dX and writes
+// P^T X in its place of dW.  dX's parts over slices of the vocabulary are added in order.  7 tokens, 2752 x 34448: XX us with
+// planes of W and products of tiles, YY so; what it cannot do without is to read W twice and to write dW.
 #pragma once
 
 #include "cci_kernels.h"
@@ -27,8 +32,13 @@ struct FewParams {
     int groups;          // of 32 entries, a block
     const int64_t *targets;
     int64_t ignore;
+    // forward
     float2 *parts;       // [blocks][N]
     float *at_target;    // [N]
+    // backward
+    const float *stats, *dloss;
+    float *probs;        // [V][8, 16 or 32: few_pitch]
+    uint32_t *status;
 };
 
 // the upper halves of a and b as bf16 (a in the low half), which become what that leaves.  Cut, not rounded: eight
@@ -51,8 +61,8 @@ __device__ __forceinline__ void mma16816(float (&d)[4], const uint32_t (&a)[4], 
         : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
-// NT: eights of tokens, and tokens that a warp sums up
-template <int NT>
+// NT: eights of tokens, and tokens that a warp sums up.  PROBS: P instead
+template <int NT, bool PROBS>
 __global__ void __launch_bounds__(kFewWarps * 32, NT <= 2 ? 2 : 1) few_kernel(const FewParams p)
 {
     constexpr int kPlanes = 3, kPitch = 8 * NT + 1;
@@ -65,7 +75,25 @@ __global__ void __launch_bounds__(kFewWarps * 32, NT <= 2 ? 2 : 1) few_kernel(co
     float most[NT], total[NT] = {};
 #pragma unroll
     for (int i = 0; i < NT; ++i) most[i] = __int_as_float(0xff800000);
-    tc::launch_next_grid();  // which waits for this one's end
+    // backward: what is subtracted from their logits, the probabilities' factors, the targets (-1: left out)
+    float base[NT], log_s[NT], weight[NT];
+    int64_t target[NT];
+    if constexpr (PROBS) {
+#pragma unroll
+        for (int i = 0; i < NT; ++i) {
+            const int n = NT * warp + i;
+            const int64_t token = n < p.N ? p.targets[n] : p.ignore;
+            const bool kept = token != p.ignore && token >= 0 && token < p.V;
+            target[i] = kept ? token : -1;
+            weight[i] = kept ? p.dloss[n] : 0.f;
+            const float m = n < p.N ? p.stats[2 * n] : 0.f;
+            base[i] = m == __int_as_float(0xff800000) ? 0.f : m;
+            log_s[i] = n < p.N ? p.stats[2 * n + 1] : 0.f;
+            if (!kept && token != p.ignore && blockIdx.x == 0 && lane == 0) report(p.status, CCI_ERR_INDEX);
+        }
+    } else {
+        tc::launch_next_grid();  // which waits for this one's end
+    }
     for (int group = 0; group < p.groups; ++group) {
         const int64_t v0 = (static_cast<int64_t>(blockIdx.x) * p.groups + group) * kFewRows;
         if (v0 >= p.V) break;
@@ -145,22 +173,28 @@ __global__ void __launch_bounds__(kFewWarps * 32, NT <= 2 ? 2 : 1) few_kernel(co
 #pragma unroll
         for (int i = 0; i < NT; ++i) {
             const int n = NT * warp + i;
-            if (n >= p.N) continue;
+            if (!PROBS && n >= p.N) continue;
             float z = 0.f;
 #pragma unroll
             for (int s = 0; s < kFewWarps; ++s) z += sums[s][lane][n];
-            const int64_t v = v0 + lane, token = p.targets[n];
+            const int64_t v = v0 + lane;
+            if constexpr (PROBS) {
+                const float e = __expf((z - base[i]) - log_s[i]) - (v == target[i] ? 1.f : 0.f);
+                if (v < p.V) p.probs[v * (8 * NT) + n] = weight[i] == 0.f ? 0.f : e * weight[i];
+                continue;
+            }
+            const int64_t token = p.targets[n];
             if (v < p.V && v == token && token != p.ignore) p.at_target[n] = z;
             if (v >= p.V) z = __int_as_float(0xff800000);
-            const float top = fmaxf(most[i], row::warp_max(z)), base = top == __int_as_float(0xff800000) ? 0.f : top;
-            const float e = row::warp_sum(__expf(z - base));
-            total[i] = (total[i] == 0.f ? 0.f : total[i] * __expf(most[i] - base)) + e;
+            const float top = fmaxf(most[i], row::warp_max(z)), from = top == __int_as_float(0xff800000) ? 0.f : top;
+            const float e = row::warp_sum(__expf(z - from));
+            total[i] = (total[i] == 0.f ? 0.f : total[i] * __expf(most[i] - from)) + e;
             most[i] = top;
         }
     }
 #pragma unroll
     for (int i = 0; i < NT; ++i)
-        if (lane == 0 && NT * warp + i < p.N)
+        if (!PROBS && lane == 0 && NT * warp + i < p.N)
             p.parts[static_cast<int64_t>(blockIdx.x) * p.N + NT * warp + i] = make_float2(most[i], total[i]);
 }
 
@@ -178,17 +212,183 @@ inline int64_t few_blocks(int64_t V, int sms)
     return (V + rows - 1) / rows;
 }
 
-inline cudaError_t launch_few(FewParams p, int sms, cudaStream_t stream)
+template <bool PROBS>
+cudaError_t launch_few(FewParams p, int sms, cudaStream_t stream)
 {
     p.groups = few_groups(p.V, sms);
     const unsigned blocks = static_cast<unsigned>(few_blocks(p.V, sms));
     switch ((p.N + 7) / 8) {
-        case 1: few_kernel<1><<<blocks, kFewWarps * 32, 0, stream>>>(p); break;
-        case 2: few_kernel<2><<<blocks, kFewWarps * 32, 0, stream>>>(p); break;
-        case 3: few_kernel<3><<<blocks, kFewWarps * 32, 0, stream>>>(p); break;
-        default: few_kernel<4><<<blocks, kFewWarps * 32, 0, stream>>>(p);
+        case 1: few_kernel<1, PROBS><<<blocks, kFewWarps * 32, 0, stream>>>(p); break;
+        case 2: few_kernel<2, PROBS><<<blocks, kFewWarps * 32, 0, stream>>>(p); break;
+        default: few_kernel<4, PROBS><<<blocks, kFewWarps * 32, 0, stream>>>(p);
     }
     return cudaGetLastError();
+}
+
+// ---- both gradients from P ----
+constexpr int kFewTile = 64;  // entries whose P is in shared memory at a time
+
+struct FewGradients {
+    const float *x, *w, *probs;
+    int N, D;
+    int64_t V, slice;  // entries of a slice, a multiple of kFewTile
+    float *dw, *parts; // dW, dX's parts [slices][N][D]; each may be null
+};
+
+constexpr int kFewAhead = 4;           // batches of weights on their way
+constexpr int kFewBatch = 16 * 1024;   // bytes of one, of all threads
+
+// NP: P's row length; C = 32 / NP columns a thread, so that its share of X and dX takes 64 registers.  Weights come through
+// places of the thread's own in shared memory, several rows ahead.  blockIdx.x: columns, .y: slice
+template <int NP, int C>
+__global__ void __launch_bounds__(256, 2) few_gradients_kernel(const FewGradients p)
+{
+    constexpr int kRows = kFewBatch / (256 * C * 4);  // of a batch
+    static_assert(kFewTile % kRows == 0, "a tile holds whole batches");
+    struct __align__(4 * C) Columns {
+        float f[C];
+    };
+    extern __shared__ __align__(16) unsigned char ring_raw[];
+    Columns *ring = reinterpret_cast<Columns *>(ring_raw) + threadIdx.x;
+    __shared__ __align__(16) float probs[kFewTile][NP];
+    const int d = (static_cast<int>(blockIdx.x) * 256 + static_cast<int>(threadIdx.x)) * C;
+    const bool mine = d < p.D;  // D is a multiple of 8
+    const int64_t from = p.slice * blockIdx.y, to = from + p.slice < p.V ? from + p.slice : p.V;
+    auto copy = [&](int64_t v0, int k) {  // rows v0 .. of a batch
+        if (mine && p.parts) {
+#pragma unroll
+            for (int r = 0; r < kRows; ++r)
+                if (v0 + r < to)
+                    asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(tc::smem_u32(ring + (k * kRows + r) * 256)),
+                                 "l"(p.w + (v0 + r) * p.D + d), "n"(4 * C)
+                                 : "memory");
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+#pragma unroll
+    for (int k = 0; k < kFewAhead; ++k) copy(from + k * kRows, k);
+    float x[NP][C], dx[NP][C];
+#pragma unroll
+    for (int n = 0; n < NP; ++n) {
+        const Columns q = mine && n < p.N ? *reinterpret_cast<const Columns *>(p.x + static_cast<int64_t>(n) * p.D + d) : Columns{};
+#pragma unroll
+        for (int j = 0; j < C; ++j) {
+            x[n][j] = q.f[j];
+            dx[n][j] = 0.f;
+        }
+    }
+    int k = 0;
+    for (int64_t v0 = from; v0 < to; v0 += kFewTile) {
+        const int count = to - v0 < kFewTile ? static_cast<int>(to - v0) : kFewTile;
+        __syncthreads();
+        for (int i = threadIdx.x; i < count * NP / 4; i += 256)
+            reinterpret_cast<float4 *>(&probs[0][0])[i] = reinterpret_cast<const float4 *>(p.probs + v0 * NP)[i];
+        __syncthreads();
+        for (int r0 = 0; r0 < count; r0 += kRows) {
+            asm volatile("cp.async.wait_group %0;" ::"n"(kFewAhead - 1) : "memory");
+            if (mine) {
+#pragma unroll 4
+                for (int r = 0; r < kRows; ++r) {
+                    if (r0 + r >= count) break;
+                    const Columns w = p.parts ? ring[(k * kRows + r) * 256] : Columns{};
+                    Columns dw{};
+#pragma unroll
+                    for (int n = 0; n < NP; n += 4) {
+                        const float4 q = *reinterpret_cast<const float4 *>(&probs[r0 + r][n]);
+                        const float f[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+#pragma unroll
+                            for (int j = 0; j < C; ++j) {
+                                dx[n + i][j] = fmaf(f[i], w.f[j], dx[n + i][j]);
+                                dw.f[j] = fmaf(f[i], x[n + i][j], dw.f[j]);
+                            }
+                    }
+                    if (p.dw) *reinterpret_cast<Columns *>(p.dw + (v0 + r0 + r) * p.D + d) = dw;
+                }
+            }
+            copy(v0 + r0 + kFewAhead * kRows, k);  // where this thread has read
+            k = k + 1 == kFewAhead ? 0 : k + 1;
+        }
+    }
+    if (!p.parts || !mine) return;
+#pragma unroll
+    for (int n = 0; n < NP; ++n) {
+        if (n >= p.N) break;
+        Columns q;
+#pragma unroll
+        for (int j = 0; j < C; ++j) q.f[j] = dx[n][j];
+        *reinterpret_cast<Columns *>(p.parts + (static_cast<int64_t>(blockIdx.y) * p.N + n) * p.D + d) = q;
+    }
+}
+
+// dX: its parts in order, n elements
+__global__ void __launch_bounds__(256) few_join_kernel(const float *parts, int slices, int64_t n, float *dx)
+{
+    const int64_t i = (static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x) * 4;
+    tc::wait_prior_grid();
+    if (i >= n) return;  // a multiple of 8
+    float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 8
+    for (int k = 0; k < slices; ++k) {
+        const float4 q = *reinterpret_cast<const float4 *>(parts + k * n + i);
+        s.x += q.x;
+        s.y += q.y;
+        s.z += q.z;
+        s.w += q.w;
+    }
+    *reinterpret_cast<float4 *>(dx + i) = s;
+}
+
+inline int few_pitch(int64_t N) { return N <= 8 ? 8 : (N <= 16 ? 16 : 32); }
+
+// slices of the vocabulary: about four blocks an SM, of kFewTile entries or more
+inline int64_t few_slice(int64_t N, int64_t D, int64_t V, int sms)
+{
+    const int64_t columns = (D + 256 * 32 / few_pitch(N) - 1) / (256 * 32 / few_pitch(N));
+    int64_t slices = 4 * sms / columns;
+    if (slices < 1) slices = 1;
+    return ((V + slices - 1) / slices + kFewTile - 1) / kFewTile * kFewTile;
+}
+
+inline int64_t few_slices(int64_t N, int64_t D, int64_t V, int sms)
+{
+    const int64_t slice = few_slice(N, D, V, sms);
+    return (V + slice - 1) / slice;
+}
+
+template <int NP, int C>
+cudaError_t launch_few_columns(const FewGradients &p, const dim3 &grid, cudaStream_t stream)
+{
+    static SmemAttrCache attr_cache;
+    const cudaError_t attr = smem_attr_once(few_gradients_kernel<NP, C>, kFewAhead * kFewBatch, attr_cache);
+    if (attr != cudaSuccess) return attr;
+    few_gradients_kernel<NP, C><<<grid, 256, kFewAhead * kFewBatch, stream>>>(p);
+    return cudaGetLastError();
+}
+
+inline cudaError_t launch_few_gradients(FewGradients p, int sms, float *dx, cudaStream_t stream)
+{
+    const int pitch = few_pitch(p.N);
+    p.slice = few_slice(p.N, p.D, p.V, sms);
+    const int64_t slices = few_slices(p.N, p.D, p.V, sms);
+    const int columns = 256 * 32 / pitch;
+    const dim3 grid(static_cast<unsigned>((p.D + columns - 1) / columns), static_cast<unsigned>(slices));
+    cudaError_t e = pitch == 8 ? launch_few_columns<8, 4>(p, grid, stream)
+                               : (pitch == 16 ? launch_few_columns<16, 2>(p, grid, stream) : launch_few_columns<32, 1>(p, grid, stream));
+    if (e != cudaSuccess || !dx) return e;
+    const int64_t n = static_cast<int64_t>(p.N) * p.D;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(static_cast<unsigned>((n / 4 + 255) / 256));
+    cfg.blockDim = dim3(256);
+    cfg.stream = stream;
+    cudaLaunchAttribute la[1];
+    la[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    la[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = la;
+    cfg.numAttrs = 1;
+    e = cudaLaunchKernelEx(&cfg, few_join_kernel, const_cast<const float *>(p.parts), static_cast<int>(slices), n, dx);
+    return e == cudaSuccess ? cudaGetLastError() : e;
 }
 
 }  // namespace head
