@@ -913,6 +913,10 @@ inline Plan plan(Mode mode, int64_t M, int64_t N, int64_t K, int terms)
         const bool can = (mode != kForward || terms > 1) && rest > 0 && shares > rest && rest * stages >= 8 * shares;
         double cut = static_cast<double>(tiles) / static_cast<double>(can ? shares : units) * tile +
                      static_cast<double>(rounds) * 4000.0 + 20000.0;
+        // A head's products have long reductions, of which the cut shares each read another part: what one share
+        // brings into L2 no other uses (dX of 4096 tokens, 2048 wide, from 32768 entries: 359 us and 1.7 GB read with 52 of 128
+        // tiles cut, 299 whole)
+        if (mode == kDxAdd || mode == kDwOne) cut += 0.6 * static_cast<double>(rest) / static_cast<double>(units) * tile;
         if (!can) cut = whole;
         const double cost = cut < whole ? cut : whole;
         if (best.cg == 0 || cost < least) {

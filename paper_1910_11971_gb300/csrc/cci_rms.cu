@@ -542,22 +542,22 @@ __global__ void __launch_bounds__(256) rms_columns_kernel(const Backward p)
     p.part[static_cast<int64_t>(blockIdx.y) * p.D + c] = s;
 }
 
-// dw from the blocks' sums, in block order over eight shares, whose sums are added in order.  A block takes 32 columns
-__global__ void __launch_bounds__(256) weight_kernel(const float *part, int parts, int D, float *dw)
+// dw from the blocks' sums, in block order over 32 shares, whose sums are added in order.  A block takes 32 columns
+__global__ void __launch_bounds__(1024) weight_kernel(const float *part, int parts, int D, float *dw)
 {
-    __shared__ float share[8][32];
+    __shared__ float share[32][33];
     const int x = threadIdx.x & 31, y = threadIdx.x >> 5, c = blockIdx.x * 32 + x;
     float s = 0.f;
     tc::wait_prior_grid();
     if (c < D) {
 #pragma unroll 8
-        for (int i = y; i < parts; i += 8) s += part[static_cast<int64_t>(i) * D + c];
+        for (int i = y; i < parts; i += 32) s += part[static_cast<int64_t>(i) * D + c];
     }
     share[y][x] = s;
     __syncthreads();
     if (y == 0 && c < D) {
 #pragma unroll
-        for (int i = 1; i < 8; ++i) s += share[i][x];
+        for (int i = 1; i < 32; ++i) s += share[i][x];
         dw[c] = s;
     }
 }
@@ -683,7 +683,7 @@ cudaError_t backward(const Backward &p, float *dw, cudaStream_t stream)
     if (e != cudaSuccess || !dw) return e;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(static_cast<unsigned>((p.D + 31) / 32));
-    cfg.blockDim = dim3(256);
+    cfg.blockDim = dim3(1024);
     cfg.stream = stream;
     cudaLaunchAttribute la[1];
     la[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
