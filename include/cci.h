@@ -778,7 +778,9 @@ cci_status cci_linear_cross_entropy(const void *X, cci_dtype dtype, int64_t N, i
  *   P[n][v] = dloss[n] * (softmax(z)[v] - 1[v = t]),  dX = P W,  dW = P^T X
  * in pieces of the vocabulary, whose logits are computed again.  P is rounded to bf16 for the products (fp32:
  * split into planes); sums are fp32 in a fixed order, each gradient rounded once to dtype.  Rows whose
- * target is `ignore_index`, or outside [0, V) (which sets CCI_ERR_INDEX), or whose dloss is 0 have P = 0.
+ * target is `ignore_index`, or outside [0, V) (which sets CCI_ERR_INDEX), or whose dloss is 0 have P = 0; they
+ * take part in dW as zeros, so their X has to be finite.  Up to 32 tokens of fp32 take the sums in another order than
+ * more do.
  *
  *   dloss      device fp32 [N];  X, W, targets as in the forward call
  *   stats      as the forward call wrote them

@@ -14,7 +14,7 @@
 //
 // The tensor core cuts its running sum at every addition, always towards zero: 256 of them, at D = 4096, leave a logit
 // of 12 about 6e-5 off, and a confident token's loss, a difference of such logits, as much of itself and more.  So the
-// forward pass adds kChunk stages (512 reduction indices) at a time there and the chunks in registers, to the nearest, as
+// forward pass adds about eight stages (512 reduction indices) at a time there and the chunks in registers, to the nearest, as
 // fp32 does throughout (1999 x 4096 x 50257 bf16: 421 us with one running sum, 437 so, 579 with chunks of 256).  That takes
 // eight output warps, each 32 tokens by half of a tile's columns.  P's own rounding is larger than this by a hundred, so the
 // bf16 backward pass keeps one running sum.
@@ -35,7 +35,12 @@ using gated::stage_mma;
 using gated::term_planes;
 using gated::tile_desc;
 
-constexpr int kChunk = 8;       // stages that the tensor core adds up by itself
+// stages that the tensor core adds up by itself, of a tile's n: about eight, eleven at most
+inline int chunk_of(int n)
+{
+    const int chunks = n < 12 ? 1 : (n + 4) / 8;
+    return (n + chunks - 1) / chunks;
+}
 constexpr int kMTilesAtOnce = 16;
 
 // one launch: a piece of the vocabulary
@@ -87,8 +92,34 @@ static_assert(sizeof(Smem) <= 1024, "barriers");
 
 __device__ __forceinline__ float neg_inf() { return __int_as_float(0xff800000); }
 
+constexpr float kLog2e = 1.4426950408889634f;
+
+__device__ __forceinline__ float ex2(float x)
+{
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+
 // exp(x) for x <= 0 or so: the difference from the maximum is taken before, in fp32
 __device__ __forceinline__ float exp_of(float x) { return __expf(x); }
+
+// z to z log2(e) - r with r the product m log2(e) as it is rounded: one fused operation, whose only rounding is that of the
+// exponent, as if the difference z - m were taken first.  What r lacks of m log2(e) is returned, one factor for all.  Where
+// r overflows the difference does come first
+template <int N>
+__device__ __forceinline__ float to_exponents(float (&z)[N], float m)
+{
+    const float r = m * kLog2e;
+    if (!(fabsf(r) < 1e38f)) {
+#pragma unroll
+        for (int j = 0; j < N; ++j) z[j] = (z[j] - m) * kLog2e;
+        return 0.f;
+    }
+#pragma unroll
+    for (int j = 0; j < N; ++j) z[j] = fmaf(z[j], kLog2e, -r);
+    return fmaf(m, kLog2e, -r);
+}
 
 // sixteen columns of this warp's TMEM lanes, without waiting for them
 __device__ __forceinline__ void tmem_ld16_begin(uint32_t taddr, uint32_t (&v)[16])
@@ -278,25 +309,19 @@ __global__ void __launch_bounds__(Cfg<CG, BN, PROBS>::kThreads, 1)
             const int64_t n0 = static_cast<int64_t>(nt) * BN + c0;
             const int64_t left_cols = p.N - n0;
             const int count = left_cols < 0 ? 0 : (left_cols < C::kCols ? static_cast<int>(left_cols) : C::kCols);
-            // the row's target among these columns, or -1; what its probabilities are multiplied by
-            int target = -1;
+            // the row's: on their way while the products are, and looked at after them
+            const int64_t token = r < p.M ? p.targets[r] : p.ignore;
             float top = 0.f, log_s = 0.f, weight = 0.f;
-            if (r < p.M) {
-                const int64_t token = p.targets[r];
-                const bool kept = token != p.ignore && token >= 0 && token < p.V;
-                const int64_t at = kept ? token - p.col0 - n0 : -1;
-                if (at >= 0 && at < count) target = static_cast<int>(at);
-                if constexpr (PROBS) {
-                    top = p.stats[2 * r];
-                    log_s = p.stats[2 * r + 1];
-                    if (kept) weight = p.dloss[r];
-                    if (!kept && token != p.ignore && nt == 0 && half == 0) report(p.status, CCI_ERR_INDEX);
-                }
+            if (PROBS && r < p.M) {
+                top = p.stats[2 * r];
+                log_s = p.stats[2 * r + 1];
+                weight = p.dloss[r];
             }
             float z[C::kCols];
             for (int left = per_tile, chunk = 0; left > 0 && ok; left -= p.chunk, ++chunk) {
                 ok = tc::mbar_wait(&S->acc_full[t & 1], (t >> 1) & 1, abort, p.status);
-                ok = tc::named_and(1, 256, ok);
+                // the output warps that wait for one another below leave together
+                ok = PROBS ? tc::named_and(1, 256, ok) : __all_sync(0xffffffffu, ok) != 0;
                 if (!ok) break;
                 __syncwarp();
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
@@ -325,6 +350,10 @@ __global__ void __launch_bounds__(Cfg<CG, BN, PROBS>::kThreads, 1)
                 ++t;
             }
             if (!ok) break;
+            // the target among these columns, or -1
+            const bool kept = token != p.ignore && token >= 0 && token < p.V;
+            const int64_t at = kept ? token - p.col0 - n0 : -1;
+            const int target = at >= 0 && at < count ? static_cast<int>(at) : -1;
             if constexpr (!PROBS) {
                 if (count < C::kCols) {
 #pragma unroll
@@ -336,21 +365,25 @@ __global__ void __launch_bounds__(Cfg<CG, BN, PROBS>::kThreads, 1)
                     for (int j = 0; j < C::kCols; ++j) x = j == target ? z[j] : x;
                     p.at_target[r] = x;
                 }
-                float most[4] = {neg_inf(), neg_inf(), neg_inf(), neg_inf()}, sum[4] = {};
+                float most[2] = {neg_inf(), neg_inf()}, sum[4] = {};
 #pragma unroll
-                for (int j = 0; j < C::kCols; ++j) most[j & 3] = fmaxf(most[j & 3], z[j]);
-                const float high = fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3]));
-                const float from = high == neg_inf() ? 0.f : high;  // -inf - -inf would be NaN
+                for (int j = 0; j < C::kCols; j += 4) {
+                    asm("max.f32 %0, %0, %1, %2;" : "+f"(most[0]) : "f"(z[j]), "f"(z[j + 1]));
+                    asm("max.f32 %0, %0, %1, %2;" : "+f"(most[1]) : "f"(z[j + 2]), "f"(z[j + 3]));
+                }
+                const float high = fmaxf(most[0], most[1]);
+                const float off = to_exponents(z, high == neg_inf() ? 0.f : high);  // -inf - -inf would be NaN
 #pragma unroll
-                for (int j = 0; j < C::kCols; ++j) sum[j & 3] += exp_of(z[j] - from);
-                if (r < p.M)
-                    p.parts[(2 * static_cast<int64_t>(nt) + half) * p.M + r] =
-                        make_float2(high, (sum[0] + sum[1]) + (sum[2] + sum[3]));
+                for (int j = 0; j < C::kCols; ++j) sum[j & 3] += ex2(z[j]);
+                float total = ((sum[0] + sum[1]) + (sum[2] + sum[3])) * ex2(-off);
+                if (high > neg_inf() && total < 1.f) total = 1.f;  // the largest's own is 1: no loss is below 0.  NaN stays
+                if (r < p.M) p.parts[(2 * static_cast<int64_t>(nt) + half) * p.M + r] = make_float2(high, total);
             } else {
-                const float from = top == neg_inf() ? 0.f : top;
-                const bool none = weight == 0.f;  // left out: 0 whatever the logits
+                if (!kept && token != p.ignore && nt == 0 && half == 0) report(p.status, CCI_ERR_INDEX);
+                const bool none = !kept || weight == 0.f;  // left out: 0 whatever the logits
+                const float off = to_exponents(z, top == neg_inf() ? 0.f : top), minus = -fmaf(log_s, kLog2e, off);
 #pragma unroll
-                for (int j = 0; j < C::kCols; ++j) z[j] = exp_of((z[j] - from) - log_s);
+                for (int j = 0; j < C::kCols; ++j) z[j] = ex2(z[j] + minus);
                 if (target >= 0) {
 #pragma unroll
                     for (int j = 0; j < C::kCols; ++j) z[j] = j == target ? z[j] - 1.f : z[j];
@@ -513,8 +546,8 @@ Shape shape_of(int64_t M, int64_t N, int64_t D, int terms)
 }
 
 // columns of a piece, at most: what a piece takes in the workspace, `bytes` a column, stays below `budget`, but for
-// pieces of 2048 columns, or of a tile of 128 x 128 for each SM (64 fp32 tokens, 3688 x 15591: XX us in pieces of 4352, YY so).
-// Pieces are of like size
+// pieces of 2048 columns, or of a tile of 128 x 128 for each SM, which fewer columns would leave idle.  Pieces are of like
+// size
 int64_t piece_of(int64_t V, int64_t bytes, int64_t budget, int64_t N)
 {
     int64_t most = budget / (bytes < 1 ? 1 : bytes) / 256 * 256, least = 128 * ws::sm_count() / ((N + 127) / 128);
@@ -692,7 +725,7 @@ cudaError_t launch_head(const HeadArgs &a, cudaStream_t stream)
     p.V = a.V;
     p.k_stages = static_cast<int>((a.D + 63) / 64);
     p.terms = f32 ? 6 : 1;
-    p.chunk = kChunk;
+    p.chunk = chunk_of(p.k_stages * p.terms);
     p.targets = a.targets;
     p.ignore = a.ignore;
     p.at_target = reinterpret_cast<float *>(base + l.at_target);
@@ -755,7 +788,7 @@ cudaError_t launch_head_backward(const HeadArgs &a, cudaStream_t stream)
     p.V = a.V;
     p.k_stages = static_cast<int>((a.D + 63) / 64);
     p.terms = f32 ? 6 : 1;
-    p.chunk = f32 ? kChunk : p.k_stages;
+    p.chunk = f32 ? chunk_of(p.k_stages * p.terms) : p.k_stages;
     p.targets = a.targets;
     p.ignore = a.ignore;
     p.stats = a.stats;

@@ -658,9 +658,10 @@ cudaError_t backward(const Backward &p, float *dw, cudaStream_t stream)
     const bool words = p.D % 8 == 0 && on_words(p.dy, p.lddy, es) && on_words(p.h, p.ldh, es) && on_words(p.dh, p.lddh, es) &&
                        on_words(p.w, 4, 4) && on_words(p.dx, p.D, es);
     if (p.D > (words ? kLongest : kLongestOff)) {
-        rms_backward_long_kernel<T><<<static_cast<unsigned>(p.N), 1024, 0, stream>>>(p);
-        parts = static_cast<unsigned>(p.N < 32 ? p.N : 32);
+        const int64_t most = most_parts(p.N);
+        parts = static_cast<unsigned>(most < 32 ? most : 32);
         rms_columns_kernel<T><<<dim3(static_cast<unsigned>((p.D + 255) / 256), parts), 256, 0, stream>>>(p);
+        rms_backward_long_kernel<T><<<static_cast<unsigned>(p.N), 1024, 0, stream>>>(p);
         e = cudaGetLastError();
     } else {
         e = with_layout(words, p.D, [&](auto v, auto nv, auto tpr) {

@@ -2,8 +2,8 @@
 
 Tolerances, with u = 2^-24.
   Logits: the tensor core adds blocks of 16 products to a running sum and cuts what it aligns, at most 17 cuts of 2 u of
-      the magnitudes' sum A = sum |x w| a block; forward, and in fp32, no more than 512 indices at a time (32 blocks), whose sums are
-      added with one rounding each.  So ez = (34 * min(32, D / 16) + D * terms / 512 + 2) u A, and for the bf16 gradient's
+      the magnitudes' sum A = sum |x w| a block; forward, and in fp32, no more than 704 indices at a time (44 blocks), whose sums are
+      added with one rounding each.  So ez = (34 * min(44, D / 16) + D * terms / 320 + 2) u A, and for the bf16 gradient's
       logits 34 * D / 16 + 2.  fp32 operands leave out 2^-25 of A, within the 2.
   Loss: twice the logits' ez (of the target, of the others), and for log s of s = sum exp(z - m): each exponential within
       2 + 1.17 |z - m| units of 2 u and the rounding of its argument, u |z - m|; 32 additions in a thread, 4 joins in it,
@@ -54,7 +54,7 @@ def logit_error(X, W, dtype, chunked):
     D, terms = X.shape[1], 6 if dtype == "f32" else 1
     A = X.double().abs() @ W.double().abs().t()
     blocks = (D + 15) // 16
-    return (34 * (min(32, blocks) if chunked else blocks) + D * terms / 512 + 2) * U * A
+    return (34 * (min(44, blocks) if chunked else blocks) + D * terms / 320 + 2) * U * A
 
 
 def softmax_error(z, m, ez, p, V):
