@@ -621,8 +621,8 @@ cci_status cci_token_logprobs_backward(const void *logits, cci_dtype dtype, int6
  *   temperature T > 0, finite
  *   loss       device fp32 [N]; stats device fp32 [N][4], 16-byte aligned (written)
  *   dev_status device uint32 or NULL
- *   workspace  device, 16-byte aligned, cci_distillation_workspace_size(N, V) bytes (0 for many rows and for
- *              short ones; it depends on the current device's number of SMs); overwritten
+ *   workspace  device, 16-byte aligned, cci_distillation_workspace_size(N, V) bytes (0 for many rows, for few and
+ *              for short ones; it depends on the current device's number of SMs); overwritten
  * N = 0 is valid and enqueues nothing.
  * Errors: CCI_ERR_NULL, CCI_ERR_SHAPE (V < 1 or > 2^24, N >= 2^28, N rows of V / 2048 blocks or more than 2^31, ldx < V,
  *         k out of range), CCI_ERR_DTYPE, CCI_ERR_VALUE (temperature), CCI_ERR_ALIGN, CCI_ERR_WORKSPACE, CCI_ERR_CUDA.

@@ -10,7 +10,7 @@
 //             fp32, rounded once.
 //
 // What bounds it: 2 N D V operations forward and 6 N D V backward on the tensor cores for many tokens, one read of W
-// forward for few.  P is rounded to bf16 (2^-9 of each of its values) because it is an operand of the tensor core.
+// forward for few.  P is rounded to bf16 (2^-8 of each of its values at most) because it is an operand of the tensor core.
 //
 // The tensor core cuts its running sum at every addition, always towards zero: 256 of them, at D = 4096, leave a logit
 // of 12 about 6e-5 off, and a confident token's loss, a difference of such logits, as much of itself and more.  So the

@@ -163,6 +163,14 @@ def test_rows_longer_than_a_block_has_bits_for(dev):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("N,V,k", [(57, 5000, 20), (58, 5000, 20), (200, 9001, 5), (456, 3000, 64), (500, 4097, 20), (3648, 2100, 7), (3647, 2100, 7), (2, 300001, 128),
+                                   (130, 40000, 9), (40, 140000, 20)])
+def test_rows_that_share_blocks(dev, N, V, k, dtype):
+    """On both sides of what takes a cluster a row, a warp a row, or blocks that cut the rows evenly."""
+    both(dev, N, V, k, dtype, 1.0, True)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("tail", [False, True])
 def test_masked_logits(dev, tail, dtype):
     """-inf and the type's lowest value take no part; a listed token that is masked has no chance."""

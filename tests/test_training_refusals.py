@@ -92,7 +92,7 @@ KD = [(dict(x=0), NULL), (dict(i=0), NULL), (dict(v=0), NULL), (dict(stats=0), N
       (dict(T=float("inf")), VALUE), (dict(x=P + 1), ALIGN), (dict(i=P + 2), ALIGN), (dict(v=P + 2), ALIGN), (dict(stats=P + 8), ALIGN)]
 
 
-LONG = dict(N=1, V=1 << 24, ld=1 << 24)  # one row for many blocks
+LONG = dict(N=1, V=1 << 24, ld=1 << 24)  # one row for many blocks, too long for a cluster
 
 
 @pytest.mark.parametrize("change,want", KD + [(dict(loss=0), NULL), (dict(loss=P + 2), ALIGN), (dict(ws=0, **LONG), WORKSPACE),
