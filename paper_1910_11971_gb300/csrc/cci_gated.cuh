@@ -900,7 +900,8 @@ inline Plan plan(Mode mode, int64_t M, int64_t N, int64_t K, int terms)
     const int shapes[3][3] = {{2, 256, 512}, {1, 128, 256}, {1, 64, 192}};
     for (const auto &shape : shapes) {
         const int cg = shape[0], bn = shape[1];
-        if (terms > 1 && cg == 2) continue;  // fp32: the output warps hold a tile's sums
+        // fp32: the output warps hold a tile's sums, four of them (a head's products: eight, cci_wide.cuh)
+        if (terms > 1 && cg == 2 && mode != kDxAdd && mode != kDwOne) continue;
         if (cg > sms) continue;              // no device: sizes and refusals are still answered
         const int64_t n = mode == kForward ? bn / 2 : bn, units = sms / cg;
         const int64_t tiles = (M + 128 * cg - 1) / (128 * cg) * outs * ((N + n - 1) / n);
