@@ -233,10 +233,12 @@ __global__ void __launch_bounds__(Cfg<CG, BN, PROBS>::kThreads, 1)
                             s = 0;
                             ph ^= 1u;
                         }
-                        if (++ks == p.k_stages) {
-                            ks = 0;
-                            term_planes(++t, p.terms, pa, pb);
+                        // all terms of a stage one after the other: what they share comes from L2
+                        if (++t == p.terms) {
+                            t = 0;
+                            ++ks;
                         }
+                        term_planes(t, p.terms, pa, pb);
                     }
                 }
                 // no copy is in flight when the block ends, nor a commit, also after an abort (as in the gated block's products)

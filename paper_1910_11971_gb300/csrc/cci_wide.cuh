@@ -98,7 +98,8 @@ __global__ void __launch_bounds__(WideCfg::kThreads, 1) wide_kernel(const Params
                     tile_at(p, work.tile, p.m_tiles, mt, nt);
                     const int m0 = (mt * 2 + static_cast<int>(rank)) * C::kM;
                     const int n0 = nt * C::kBN + static_cast<int>(rank) * 128;
-                    int ks = work.s0 % p.k_stages, t = work.s0 / p.k_stages, pa, pb;
+                    // all terms of a stage one after the other: what they share comes from L2
+                    int ks = work.s0 / p.terms, t = work.s0 % p.terms, pa, pb;
                     term_planes(t, p.terms, pa, pb);
                     for (int i = 0; i < work.n; ++i, ++it) {
                         ok = tc::mbar_wait(&S->empty[s], ph, abort, p.status);
@@ -119,10 +120,11 @@ __global__ void __launch_bounds__(WideCfg::kThreads, 1) wide_kernel(const Params
                             s = 0;
                             ph ^= 1u;
                         }
-                        if (++ks == p.k_stages) {
-                            ks = 0;
-                            term_planes(++t, p.terms, pa, pb);
+                        if (++t == p.terms) {
+                            t = 0;
+                            ++ks;
                         }
+                        term_planes(t, p.terms, pa, pb);
                     }
                 }
                 // no copy is in flight when the block ends, nor a commit, also after an abort (as in product_kernel)
