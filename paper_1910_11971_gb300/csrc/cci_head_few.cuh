@@ -12,9 +12,9 @@
 // Backward the same walk gives P [V][tokens] in fp32, and one pass over the weights takes both gradients from it with
 // fused multiply-adds: a thread holds its columns of X and of dX for all tokens, reads a weight, adds P times it to dX and writes
 // P^T X in its place of dW.  dX's parts over slices of the vocabulary are added in order.  7 tokens, 2752 x 34448,
-// both passes: 845 us with planes of W and products of tiles, 327 so, of 224 to read W three times and write dW.  25 to
-// 100 tokens are past what fused multiply-adds here, or planes there, do well: 25 tokens 774 us, of which elementary fp32 products
-// take 590.
+// both passes: 845 us with planes of W and products of tiles, 327 so, of 224 to read W three times and write dW.  What bounds
+// that pass is P, a broadcast load from shared memory for four multiply-adds of each gradient.  17 to about 80 tokens are past what this,
+// or planes, do well: 25 tokens 772 us, where elementary fp32 products take 591.
 #pragma once
 
 #include "cci_kernels.h"
