@@ -608,7 +608,8 @@ cci_status cci_token_logprobs_backward(const void *logits, cci_dtype dtype, int6
  * gradient.  The lists are those of cci_token_logprobs on the teacher's logits.  It is not multiplied
  * by T^2: the gradient's dloss is the place for that.
  *   stats[n] = (max z, log sum exp(z - max), log of that sum over what is not listed,
- *               tail: sum q, else: log sum exp(t_j / T))
+ *               tail: sum q, else: log sum exp(t_j / T));  where |max z| is 64 or more and its rounding loses
+ *               something of max x, the first two are max x and the logarithm with its sign set
  * An index of -1 lists nothing, whatever its t; a row that lists nothing has loss 0 and no gradient.  t_j may
  * be -inf (q_j = 0, and listed).  A listed logit of -inf with q_j > 0 makes the loss inf.  Where no unlisted logit is
  * above -inf, the rest takes no part (q_rest counts as 0).  NaN or +inf in a row makes its loss NaN.  Any other
@@ -618,7 +619,7 @@ cci_status cci_token_logprobs_backward(const void *logits, cci_dtype dtype, int6
  *   logits     device, N rows of V of dtype, row stride ldx
  *   top_idx    device int32 [N][k]; top_logp device fp32 [N][k]
  *   k          1 .. min(V, CCI_MAX_TEACHER)
- *   temperature T > 0, finite
+ *   temperature T > 0, T and log2(e) / T finite
  *   loss       device fp32 [N]; stats device fp32 [N][4], 16-byte aligned (written)
  *   dev_status device uint32 or NULL
  *   workspace  device, 16-byte aligned, cci_distillation_workspace_size(N, V) bytes (0 for many rows, for few and

@@ -400,7 +400,8 @@ cci_status check_distillation(int dtype, int64_t N, int64_t V, const void *logit
     if (!rows_ok(N, V, ldx) || V > kMaxLogits || N >= kMaxRows / 8 || N * ((V + 2054) / 2048) >= kMaxRows || k < 1 ||
         k > CCI_MAX_TEACHER || k > V)
         return CCI_ERR_SHAPE;
-    if (!(temperature > 0.0f) || temperature > 3.4e38f) return CCI_ERR_VALUE;  // also NaN
+    // also NaN; below, the kernels' factor log2(e) / T is infinite
+    if (!(temperature >= 4.3e-39f) || temperature > 3.4e38f) return CCI_ERR_VALUE;
     if (!aligned(logits, elem_size(dtype)) || !aligned(idx, 4) || !aligned(value, 4) || !aligned(stats, 16))
         return CCI_ERR_ALIGN;
     return CCI_OK;

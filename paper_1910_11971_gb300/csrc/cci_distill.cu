@@ -35,6 +35,10 @@ constexpr int kPiece = 32768;    // groups that a block has bits for at a time (
 // logits of a row that a warp takes by itself, and where there are rows enough for all SMs' warps
 constexpr int kShort = 2048, kShortOfMany = 32768;
 
+// beyond it fp32 rounds a number by 2^-18 and more, and as much of its exponential: those maxima and normalisers are not taken from
+// their quotients by T
+constexpr float kFar = 64.f;
+
 struct Args {
     const void *x;
     int64_t ldx, N;
@@ -218,11 +222,11 @@ __device__ __forceinline__ float largest(const row::Raw<T, 8> (&raw)[U])
 // A warp's sums while it walks, c = log2(e) / T: s = sum of 2^(x c - r) with r the product m c as it is rounded.  One fused
 // operation takes a logit to its exponent, and its only rounding is that of the exponent, as if the difference x - m were
 // taken first: that r is not quite m c (`off` is what it lacks) is one factor for all, put right when the maximum moves and at the end.
-// Where m c overflows, at the type's lowest value, the difference does come first
+// Far from 0 (a row that is masked by large negative numbers) that factor would leave the range, and the difference does come first
 struct Walk {
     float m, s, r, off;
     __device__ __forceinline__ Walk() : m(neg_inf()), s(0.f), r(0.f), off(0.f) {}
-    __device__ __forceinline__ bool far() const { return !(fabsf(r) < 1e38f); }
+    __device__ __forceinline__ bool far() const { return !(fabsf(r) < 16777216.f); }  // below, off is 1/2 at most
     __device__ __forceinline__ Sums sums() const { return Sums{m, s == 0.f ? 0.f : s * ex2(-off)}; }
     __device__ __forceinline__ void raise(float top, float c)
     {
@@ -308,7 +312,12 @@ __device__ __forceinline__ void finish(const Args &a, int64_t n, const Sums &sum
     }
     if (bad) report(a.status, CCI_ERR_INDEX);
     a.loss[n] = bad ? nan_f() : loss;
-    reinterpret_cast<float4 *>(a.stats)[n] = make_float4(bad ? nan_f() : m / a.T, log_s, log_rest, mine.norm);
+    // The gradient takes differences from the maximum.  Where the rounding of m / T says too little of it (a masked row's, say),
+    // it is left as it is, and the logarithm, which is 0 at least, has its sign set
+    const float high = m / a.T;
+    const bool as_is = fabsf(high) >= kFar && high * a.T != m;
+    reinterpret_cast<float4 *>(a.stats)[n] =
+        make_float4(bad ? nan_f() : (as_is ? m : high), as_is ? -log_s : log_s, log_rest, mine.norm);
 }
 
 // ---- short rows, or many: a warp each.  The argument: bytes of a row's bits ----
@@ -607,7 +616,7 @@ __global__ void __launch_bounds__(256) gradient_kernel(const Args a)
     T *dx = static_cast<T *>(a.dx) + n * a.lddx;
     const int s = shift_of(x), V = a.V, lo = chunk * a.steps * 256 * kU - s;
     const int hi = lo + a.steps * 256 * kU < V ? lo + a.steps * 256 * kU : V;
-    const float c = 1.f / a.T;
+    const float unit = 1.f / a.T, c = kLog2e / a.T;
     row::Raw<T, 8> next[kU];
     auto load = [&](int e0) {
 #pragma unroll
@@ -618,13 +627,25 @@ __global__ void __launch_bounds__(256) gradient_kernel(const Args a)
     };
     load(lo);
     const float4 st = reinterpret_cast<const float4 *>(a.stats)[n];
-    const float weight = a.dloss[n] / a.T, m = ref_of(st.x), log_s = st.y, log_rest = st.z;
-    float whole, left = 0.f;  // Q, q_rest
+    const float weight = a.dloss[n] / a.T, log_s = fabsf(st.y), log_rest = st.z;
+    const float m = ref_of(signbit(st.y) ? st.x : st.x * a.T);
+    float whole, left = 0.f;        // Q, q_rest
+    float best = 0.f, norm = st.w;  // of the teacher's values: q_j = exp((t_j - best) / T - norm)
     if (a.tail) {
         left = log_rest == neg_inf() ? 0.f : fmaxf(1.f - st.w, 0.f);
         whole = st.w + left;
     } else {
-        whole = st.w == neg_inf() ? 0.f : 1.f;  // nothing listed
+        if (fabsf(norm) >= kFar) {
+            best = neg_inf();
+            for (int j = lane; j < a.k; j += 32)
+                if (a.idx[n * a.k + j] >= 0) best = fmaxf(best, a.value[n * a.k + j]);
+            best = ref_of(row::warp_max(best));
+            norm = 0.f;
+            for (int j = lane; j < a.k; j += 32)
+                if (a.idx[n * a.k + j] >= 0) norm += expf((a.value[n * a.k + j] - best) / a.T);
+            norm = logf(row::warp_sum(norm));
+        }
+        whole = norm == neg_inf() ? 0.f : 1.f;  // nothing listed
     }
     // the listed logits among these, read before any of them is written: dx may be x
     int at[kOwn];
@@ -636,8 +657,8 @@ __global__ void __launch_bounds__(256) gradient_kernel(const Args a)
         if (at[i] < lo || at[i] >= hi) at[i] = -1;
         if (at[i] >= 0) {
             const float v = a.value[n * a.k + j];
-            const float q = a.tail ? expf(v) : (whole == 0.f ? 0.f : expf(v * c - st.w));
-            const float p = expf(fmaf(row::to_f32(x[at[i]]), c, -m) - log_s);
+            const float q = a.tail ? expf(v) : (whole == 0.f ? 0.f : expf((v - best) * unit - norm));
+            const float p = expf((row::to_f32(x[at[i]]) - m) * unit - log_s);
             own[i] = st.x == neg_inf() ? 0.f : (p * whole - q) * weight;
         }
     }
@@ -645,7 +666,7 @@ __global__ void __launch_bounds__(256) gradient_kernel(const Args a)
     const bool some = a.tail && log_rest != neg_inf();
     const float shift = some ? log_rest : log_s;
     const float coef = (some ? whole * expf(log_rest - log_s) - left : whole) * weight;
-    const unsigned long long c2 = pack2(c, c), neg = pack2(-m, -m), l2 = pack2(kLog2e, kLog2e), coef2 = pack2(coef, coef);
+    const unsigned long long c2 = pack2(c, c), neg = pack2(-m, -m), coef2 = pack2(coef, coef);
     const float minus = -shift * kLog2e;
     const bool words = shift_of(dx) == s;
     __syncwarp();
@@ -662,9 +683,8 @@ __global__ void __launch_bounds__(256) gradient_kernel(const Args a)
             row::unpack2<T, 8>(raw[u], p);
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                unsigned long long d = neg, y = pack2(minus, minus);
-                ffma2(d, p[j], c2);
-                ffma2(y, d, l2);
+                unsigned long long y = pack2(minus, minus);
+                ffma2(y, row::add2(p[j], neg), c2);
                 p[j] = row::mul2(pack2(ex2(lo_of(y)), ex2(hi_of(y))), coef2);
             }
             if (words && e >= 0 && e + 8 <= V) {

@@ -105,13 +105,13 @@ __device__ __forceinline__ float ex2(float x)
 __device__ __forceinline__ float exp_of(float x) { return __expf(x); }
 
 // z to z log2(e) - r with r the product m log2(e) as it is rounded: one fused operation, whose only rounding is that of the
-// exponent, as if the difference z - m were taken first.  What r lacks of m log2(e) is returned, one factor for all.  Where
-// r overflows the difference does come first
+// exponent, as if the difference z - m were taken first.  What r lacks of m log2(e) is returned, one factor for all, 1/2 at most:
+// for larger logits than that leaves, the difference does come first
 template <int N>
 __device__ __forceinline__ float to_exponents(float (&z)[N], float m)
 {
     const float r = m * kLog2e;
-    if (!(fabsf(r) < 1e38f)) {
+    if (!(fabsf(r) < 16777216.f)) {
 #pragma unroll
         for (int j = 0; j < N; ++j) z[j] = (z[j] - m) * kLog2e;
         return 0.f;

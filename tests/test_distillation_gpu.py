@@ -198,6 +198,84 @@ def test_masked_logits(dev, tail, dtype):
     assert abs(float(loss[5]) - float(f["loss"])) <= 1e-5 * float(f["loss"])
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("tail", [False, True])
+@pytest.mark.parametrize("T", [0.5, 2.0 ** -10, 2.0 ** -127])
+@pytest.mark.parametrize("N,V", [(6, 900), (6, 20000), (300, 5000)])
+def test_maxima_beyond_32_bits(dev, N, V, T, tail, dtype):
+    """Rows whose maximum is the type's lowest value, or its largest, divided by a temperature below 1.  What is not at the maximum is
+    at least 2^-24 of it below, more than any exponent: the formula's result is that of 0 at the maximum and -inf elsewhere.
+    So it is of a teacher's values."""
+    k, info = 8, torch.finfo(DTYPES[dtype])
+    g = torch.Generator().manual_seed(V)
+    at_most = torch.rand((N, V), generator=g) < 0.3
+    at_most[:, :4] = True
+    at_most[N - 1] = True                                # nothing but the maximum
+    high = torch.full((N, 1), info.min)
+    high[1] = info.max
+    lower = torch.where(high < 0, -INF, torch.randn((N, V), generator=g))
+    x = torch.where(at_most, high, lower).to(DTYPES[dtype])
+    idx = torch.stack([torch.randperm(V, generator=g)[:k] for _ in range(N)]).to(torch.int32)
+    idx[0, :3] = torch.tensor([0, 1, 2])
+    idx[2] = -1
+    value = torch.full((N, k), -2.0)
+    if not tail:                                         # alike far down, but for one lower
+        value[:] = torch.finfo(torch.float32).min * 0.9
+        value[:, 1] = torch.finfo(torch.float32).min
+    chance = at_most.gather(1, idx.clamp(min=0).long())  # the listed have to have one, or the loss is infinite
+    idx = torch.where(chance, idx, -1)
+    most = torch.where(idx >= 0, value, -INF).max(1, keepdim=True).values
+    same = value if tail else torch.where(value == most, 0.0, -INF)
+    dloss = torch.rand(N, generator=g) * min(T, 1.0)
+    f = reference(torch.where(at_most, 0.0, -INF), idx, same, 1.0, tail)
+    logits, lists = x.to(dev), (idx.to(dev), value.to(dev))
+    check_shifted(logits, lists, dloss, T, tail, dtype, f)
+
+
+def check_shifted(logits, lists, dloss, T, tail, dtype, f):
+    """Against the formula of logits and a teacher's values less their rows' largest, which is the same."""
+    N, V = logits.shape
+    m = logits.cpu().double().max(1).values
+    loss, stats = cci.distillation_loss(logits, *lists, temperature=T, tail=tail)
+    shown = stats.cpu().double()
+    as_is = torch.signbit(shown[:, 1])
+    assert (shown[as_is, 0] == m[as_is]).all() and ((shown[:, 0] - m / T).abs() <= 2 * U * (m / T).abs())[~as_is].all()
+    shown[:, 0], shown[:, 1] = 0.0, shown[:, 1].abs()
+    if not tail:
+        shown[:, 3] = f["given"]
+    check_forward(loss, shown, f, tail)
+    # the gradient takes maxima and normalisers of up to 64 from their quotients by T, whose roundings count as above
+    t = (torch.where(f["valid"], lists[1].cpu().double(), 0.0) / T).abs().max(1, keepdim=True).values
+    f = dict(f, m=torch.where(as_is | ((m / T).abs() >= 64), 0.0, m / T))
+    if not tail:
+        f["e_q"] = f["e_q"] + 4 * U * torch.where(t < 68, t, 0.0)
+    dloss_on = dloss.to(logits.device)
+    dx = cci.distillation_loss_backward(dloss_on, logits, *lists, stats, temperature=T, tail=tail)
+    check_backward(dx, f, dloss, T, V, dtype)
+    assert cci.distillation_loss_backward(dloss_on, logits, *lists, stats, temperature=T, tail=tail, out=logits) is logits
+    assert torch.equal(logits, dx)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("tail", [False, True])
+@pytest.mark.parametrize("T", [0.7, 1.0, 1.5, 3.0])
+@pytest.mark.parametrize("mask", [-50.0, -1e4, -1e6, -1e9, -1e30, -1e38, 1e5])
+@pytest.mark.parametrize("N,V", [(6, 900), (6, 20000), (300, 5000)])
+def test_rows_that_lie_far_from_0(dev, N, V, mask, T, tail, dtype):
+    """Every logit of a row, and the teacher's values, with the same number added: as a mask that covers all of a row does.  The
+    type keeps what it has room for of their differences."""
+    k, t = 8, DTYPES[dtype]
+    g = torch.Generator().manual_seed(V)
+    x = (torch.randn((N, V), generator=g) * 3 + mask).to(t)
+    idx = torch.stack([torch.randperm(V, generator=g)[:k] for _ in range(N)]).to(torch.int32)
+    value = torch.log(torch.full((N, k), 0.08)) if tail else torch.randn((N, k), generator=g) + mask
+    value = value.contiguous()
+    apart = (x.double() - x.double().max(1, keepdim=True).values) / T
+    value_apart = value.double() if tail else (value.double() - value.double().max(1, keepdim=True).values) / T
+    dloss = torch.randn(N, generator=g)
+    check_shifted(x.to(dev), (idx.to(dev), value.to(dev)), dloss, T, tail, dtype, reference(apart, idx, value_apart, 1.0, tail))
+
+
 def test_nan_and_inf_keep_to_their_rows(dev):
     N, V, k = 5, 5000, 6
     _, x, idx, value, dloss = inputs(N, V, k, "f32", 4, 1.0, True)

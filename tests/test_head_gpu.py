@@ -252,6 +252,38 @@ def test_large_offsets(dev):
     check_backward(X, W, targets, stats, dloss, dX, dW, "f32")
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("scale", [10, 12, 16, 50])
+@pytest.mark.parametrize("N", [5, 40, 200])
+def test_logits_of_any_size(dev, N, scale, dtype):
+    """Two values of logits, 2^20 to 2^100 and further apart than any exponent: p is 1 / c at the larger, c of them.  Sums as above:
+    100 units of u for s (V / 500 and what its exponentials, all 1, leave), P's rounding, and the products' cuts."""
+    D, V = 64, 301
+    g = torch.Generator().manual_seed(N)
+    X, W = torch.zeros((N, D)), torch.zeros((V, D))
+    X[:, 3] = 1.5859375 * 2.0 ** scale * torch.where(torch.arange(N) % 2 > 0, -1.0, 1.0)
+    W[:, 3] = 1.5703125 * 2.0 ** scale * torch.where(torch.rand(V, generator=g) < 0.4, 0.5, 1.0)
+    z = X.double() @ W.double().t()
+    top = z == z.max(1, keepdim=True).values
+    c = top.sum(1).double()
+    targets = torch.multinomial(top.double(), 1, generator=g)[:, 0]
+    dloss = torch.randn(N, generator=g) / N
+    args = X.to(DTYPES[dtype]).to(dev), W.to(DTYPES[dtype]).to(dev), targets.to(dev)
+    loss, stats = cci.linear_cross_entropy(*args)
+    assert ((loss.cpu().double() - torch.log(c)).abs() <= 100 * U * (1 + torch.log(c))).all()
+    d = dloss.double()[:, None]
+    p = top / c[:, None]
+    P = d * p
+    P[torch.arange(N), targets] -= dloss.double()
+    half = 2.0 ** -8 if dtype == "bf16" else 0.0
+    eP = 200 * U * d.abs() * p + (half + 4 * U) * P.abs()
+    sums = 34 * 32 * U
+    dX, dW = cci.linear_cross_entropy_backward(dloss.to(dev), *args, stats)
+    for got, want, tol in ((dX, P @ W.double(), (eP + sums * P.abs()) @ W.double().abs()),
+                           (dW, P.t() @ X.double(), (eP + sums * P.abs()).t() @ X.double().abs())):
+        assert ((got.cpu().double() - want).abs() <= tol + (half + 2 * U) * want.abs()).all()
+
+
 def test_gradient_against_differences(dev):
     N, D, V = 3, 16, 20
     X, W, targets, dloss = inputs(N, D, V, "f32", 8)

@@ -92,6 +92,9 @@ KD = [(dict(x=0), NULL), (dict(i=0), NULL), (dict(v=0), NULL), (dict(stats=0), N
       (dict(T=float("inf")), VALUE), (dict(x=P + 1), ALIGN), (dict(i=P + 2), ALIGN), (dict(v=P + 2), ALIGN), (dict(stats=P + 8), ALIGN)]
 
 
+KD += [(dict(T=4e-39), VALUE), (dict(T=1e-45), VALUE)]  # log2(e) / T is infinite
+
+
 LONG = dict(N=1, V=1 << 24, ld=1 << 24)  # one row for many blocks, too long for a cluster
 
 
