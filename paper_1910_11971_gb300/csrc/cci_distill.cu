@@ -626,6 +626,19 @@ __global__ void __launch_bounds__(256) gradient_kernel(const Args a)
         }
     };
     load(lo);
+    // the listed logits among these, read before any of them is written (dx may be x), and what the teacher says of them
+    int at[kOwn];
+    float z[kOwn], own[kOwn];
+#pragma unroll
+    for (int i = 0; i < kOwn; ++i) {
+        const int j = lane + i * 32;
+        at[i] = j < a.k ? a.idx[n * a.k + j] : -1;
+        if (at[i] < lo || at[i] >= hi) at[i] = -1;
+        if (at[i] >= 0) {
+            z[i] = row::to_f32(x[at[i]]);
+            own[i] = a.value[n * a.k + j];
+        }
+    }
     const float4 st = reinterpret_cast<const float4 *>(a.stats)[n];
     const float weight = a.dloss[n] / a.T, log_s = fabsf(st.y), log_rest = st.z;
     const float m = ref_of(signbit(st.y) ? st.x : st.x * a.T);
@@ -647,18 +660,11 @@ __global__ void __launch_bounds__(256) gradient_kernel(const Args a)
         }
         whole = norm == neg_inf() ? 0.f : 1.f;  // nothing listed
     }
-    // the listed logits among these, read before any of them is written: dx may be x
-    int at[kOwn];
-    float own[kOwn];
 #pragma unroll
     for (int i = 0; i < kOwn; ++i) {
-        const int j = lane + i * 32;
-        at[i] = j < a.k ? a.idx[n * a.k + j] : -1;
-        if (at[i] < lo || at[i] >= hi) at[i] = -1;
         if (at[i] >= 0) {
-            const float v = a.value[n * a.k + j];
-            const float q = a.tail ? expf(v) : (whole == 0.f ? 0.f : expf((v - best) * unit - norm));
-            const float p = expf((row::to_f32(x[at[i]]) - m) * unit - log_s);
+            const float q = a.tail ? expf(own[i]) : (whole == 0.f ? 0.f : expf((own[i] - best) * unit - norm));
+            const float p = expf((z[i] - m) * unit - log_s);
             own[i] = st.x == neg_inf() ? 0.f : (p * whole - q) * weight;
         }
     }
