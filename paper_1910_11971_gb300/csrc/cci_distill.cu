@@ -110,10 +110,10 @@ __device__ __forceinline__ Sums joined(Sums a, Sums b, float c)
     return Sums{m, u + v};
 }
 
-// what a row's list says: the largest listed logit and the sum of exp((x - top) / T); the teacher's sum or its normaliser's
-// logarithm, as in stats; and - sum q_j (x_j - top) / T with the sum of those q_j
+// what a row's list says: the largest listed logit and the sum of exp((x - top) / T) but for the largest's own 1; the teacher's
+// sum or its normaliser's logarithm, as in stats; and - sum q_j (x_j - top) / T with the sum of those q_j
 struct Listed {
-    float top, sum, given, norm, off, share;
+    float top, others, given, norm, off, share;
 };
 
 // a lane's part of a row's list: indices (-1: none), the teacher's values
@@ -150,15 +150,20 @@ __device__ __forceinline__ Listed listed_of(const Args &a, const int (&at)[kOwn]
     best = row::warp_max(best);
     Listed r{top, 0.f, 0.f, 0.f, 0.f, 0.f};
     const float from = ref_of(top), best_from = ref_of(best);
+    int largest = 0;  // how many are
 #pragma unroll
     for (int i = 0; i < kOwn; ++i) {
         q[i] = at[i] < 0 ? 0.f : (a.tail ? expf(q[i]) : expf((q[i] - best_from) / a.T));
         z[i] = (z[i] - from) / a.T;
         r.given += q[i];
-        if (at[i] >= 0) r.sum += expf(z[i]);
+        if (z[i] == 0.f)
+            ++largest;
+        else if (at[i] >= 0)
+            r.others += expf(z[i]);
     }
+    largest = __reduce_add_sync(0xffffffffu, largest);
     r.given = row::warp_sum(r.given);
-    r.sum = row::warp_sum(r.sum);
+    r.others = row::warp_sum(r.others) + (largest > 1 ? static_cast<float>(largest - 1) : 0.f);
     const float unit = a.tail || r.given == 0.f ? 1.f : 1.f / r.given;
 #pragma unroll
     for (int i = 0; i < kOwn; ++i) {
@@ -301,14 +306,16 @@ __device__ __forceinline__ void finish(const Args &a, int64_t n, const Sums &sum
 {
     const float m = fmaxf(sums.m, mine.top), from = ref_of(m);
     const float rest = sums.s == 0.f ? 0.f : sums.s * ex2((sums.m - from) * c);
-    const float sum = rest + (mine.sum == 0.f ? 0.f : mine.sum * ex2((mine.top - from) * c));
+    const bool some = mine.top != neg_inf();
+    const float listed = some ? (1.f + mine.others) * ex2((mine.top - from) * c) : mine.others, sum = rest + listed;
     const bool empty = m == neg_inf() && sum == 0.f;
-    const float log_s = empty ? 0.f : logf(sum), log_rest = logf(rest);
-    // no term is below 0: nothing cancels
+    // A sure student's loss is what others add to the 1 of a listed token, a small rest's what the listed add to it: neither
+    // is left to the rounding of a sum that is mostly something else.  No term below is negative: nothing cancels
+    const float log_s = empty ? 0.f : (some && mine.top >= sums.m ? log1pf(mine.others + rest) : logf(sum)), log_rest = logf(rest);
     float loss = mine.off + (mine.share == 0.f ? 0.f : mine.share * (log_s - (ref_of(mine.top) - from) / a.T));
     if (a.tail) {
         const float left = rest == 0.f ? 0.f : fmaxf(1.f - mine.given, 0.f);
-        if (left > 0.f) loss += left * (log_s - log_rest);
+        if (left > 0.f) loss += left * (listed < rest ? log1pf(listed / rest) : log_s - log_rest);
     }
     if (bad) report(a.status, CCI_ERR_INDEX);
     a.loss[n] = bad ? nan_f() : loss;

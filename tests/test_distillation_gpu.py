@@ -322,6 +322,28 @@ def test_bad_indices_are_reported(dev, V):
     assert dx[bad].isnan().all() and dx[~bad].isfinite().all()
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("N,V", [(6, 300), (6, 20000), (300, 5000)])
+def test_small_losses(dev, N, V, dtype):
+    """Relative to themselves: a student's that is sure of what its teacher says, and what a few tokens of a small chance
+    take from the rest.  An exponential is off by (8 + 4 * 33) u, the sums by V / 4096 + 60 units of u, q by (8 + 4 * 9) u, the
+    rest's share of the teacher, 0.99 at least, by as much of 0.01, three logarithms and products by 4 u each: 300 u."""
+    g = torch.Generator().manual_seed(V)
+    x = torch.rand((N, V), generator=g).to(DTYPES[dtype])
+    idx = torch.stack([torch.randperm(V, generator=g)[:3] for _ in range(N)]).to(torch.int32)
+    sure = x.clone()
+    sure[torch.arange(N), idx[:, 0].long()] = 32.0
+    value = torch.tensor([0.0, -INF, -INF]).repeat(N, 1)
+    loss, _ = cci.distillation_loss(sure.to(dev), idx.to(dev), value.to(dev))
+    # 1 + 6e-12 is off by 2^-53 in 64 bits too, 1.8e-5 of the loss: what is added to the 1 by itself
+    want = torch.log1p(torch.exp(sure.double() - 32.0).scatter(1, idx[:, :1].long(), 0.0).sum(1))
+    assert want.max() < 1e-8 and ((loss.cpu().double() - want).abs() <= 300 * U * want).all()
+    value = torch.tensor([-9.0, -7.0, -INF]).repeat(N, 1)
+    loss, _ = cci.distillation_loss(x.to(dev), idx.to(dev), value.to(dev), tail=True)
+    want = reference(x, idx, value, 1.0, True)["loss"]
+    assert want.max() < 0.1 and ((loss.cpu().double() - want).abs() <= 300 * U * want).all()
+
+
 def test_gradient_against_differences(dev):
     N, V, k = 2, 30, 4
     for T, tail in ((1.5, False), (1.0, True)):
