@@ -240,6 +240,36 @@ def test_confident_tokens_keep_their_loss(dev):
     assert ((loss.cpu().double() - want).abs() <= 6.2e-5 * (1 - torch.exp(-want)) + 1e-6 * want + 2 ** -24).all()
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("N", [3, 30, 100])
+def test_sure_tokens_keep_their_gradient(dev, N, dtype):
+    """Chances of 1 - 3e-4 or so: what is left of p - 1 is as right as that of the others.  A difference of logits is off by 2 ez of
+    the chunks, which goes with p (1 - p); log s and the difference from it round to 8 u, whatever is left; the exponentials' and
+    the sum's errors and the rounding of P as above."""
+    D, V = 4096, 300
+    g = torch.Generator().manual_seed(6)
+    W = torch.randn((V, D), generator=g).to(DTYPES[dtype])
+    targets = torch.randperm(V, generator=g)[:N]
+    X = ((14.0 / D) * W[targets].float() + 0.1 / D ** 0.5 * torch.randn((N, D), generator=g)).to(DTYPES[dtype])
+    dloss = torch.randn(N, generator=g)
+    args = X.to(dev), W.to(dev), targets.to(dev)
+    loss, stats = cci.linear_cross_entropy(*args)
+    dX, dW = cci.linear_cross_entropy_backward(dloss.to(dev), *args, stats)
+    z = X.double() @ W.double().t()
+    m = z.max(1, keepdim=True).values
+    p = torch.softmax(z, 1)
+    assert 2e-5 < float((1 - p.max(1).values).min()) and float((1 - p.max(1).values).max()) < 1e-3
+    P = p.scatter(1, targets[:, None], 0.0)
+    P.scatter_(1, targets[:, None], -P.sum(1, keepdim=True))  # not by p - 1
+    P = dloss.double()[:, None] * P
+    half = 2.0 ** -8 if dtype == "bf16" else 0.0
+    ez = logit_error(X, W, dtype, True).max(1, keepdim=True).values
+    eP = P.abs() * (half + 2 * ez + (60 + V / 500 + 3.4 * (m - z)) * U) + 8 * U * dloss.double().abs()[:, None] * torch.maximum(p, p > 0.5)
+    for got, want, mags in ((dX, P @ W.double(), W.double().abs()), (dW, P.t() @ X.double(), X.double().abs())):
+        a, e = (P.abs(), eP) if got is dX else (P.abs().t(), eP.t())
+        assert ((got.cpu().double() - want).abs() <= (e + 34 * 32 * U * a) @ mags + (half + 2 * U) * want.abs()).all()
+
+
 def test_large_offsets(dev):
     """Logits that all lie far from 0."""
     N, D, V = 50, 64, 400
