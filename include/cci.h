@@ -504,8 +504,8 @@ cci_status cci_layer_norm_backward_ex(const void *dy, int64_t lddy, const void *
  *              themselves, packed
  *   rstd       device fp32 [N] (written; the backward pass reads it) or NULL
  * N = 0 is valid and enqueues nothing.  eps must be >= 0 (CCI_ERR_VALUE; NaN too).
- * Errors: CCI_ERR_NULL, CCI_ERR_SHAPE (D < 1 or >= 2^30, N >= 2^31, ldx or ldr < D), CCI_ERR_DTYPE, CCI_ERR_ALIGN,
- *         CCI_ERR_VALUE, CCI_ERR_CUDA.
+ * Errors: CCI_ERR_NULL, CCI_ERR_SHAPE (D < 1 or >= 2^30, N >= 2^31, ldx or ldr < D, h in the place of rows that are
+ *         not packed), CCI_ERR_DTYPE, CCI_ERR_ALIGN, CCI_ERR_VALUE, CCI_ERR_CUDA.
  */
 cci_status cci_rms_norm(const void *x, cci_dtype dtype, int64_t N, int64_t D, int64_t ldx, const void *residual,
                         int64_t ldr, const float *weight, float eps, void *y, void *h, float *rstd,
@@ -646,7 +646,7 @@ cci_status cci_distillation_loss(const void *logits, cci_dtype dtype, int64_t N,
  *   dlogits    device, N rows of V of dtype, row stride lddx (written; may be the logits themselves, with
  *              the same stride).  Rows at the same offset from a 16-byte boundary as the logits' are
  *              written in whole vectors
- * Errors: as cci_distillation_loss; CCI_ERR_SHAPE also for lddx < V.
+ * Errors: as cci_distillation_loss; CCI_ERR_SHAPE also for lddx < V, and in place with another stride.
  */
 cci_status cci_distillation_loss_backward(const float *dloss, const void *logits, cci_dtype dtype, int64_t N, int64_t V,
                                           int64_t ldx, const int32_t *top_idx, const float *top_logp, int k,

@@ -314,6 +314,12 @@ cci_status cci_linear_cross_entropy_backward(const float *dloss, const void *X, 
 
 namespace {
 
+// whether the sums, which are packed, may go where they do: over no other row of x or the residual
+bool in_place_ok(int64_t N, int64_t D, const void *x, int64_t ldx, const void *residual, int64_t ldr, const void *h)
+{
+    return !h || N < 2 || ((h != x || ldx == D) && (h != residual || ldr == D));
+}
+
 // sizes and pointers of both forward forms of the root-mean-square norm
 cci_status check_rms(int dtype, int64_t N, int64_t D, const void *x, int64_t ldx, const void *residual, int64_t ldr,
                      const float *weight, float eps, const void *y, const void *h, const float *rstd)
@@ -339,6 +345,7 @@ cci_status cci_rms_norm(const void *x, cci_dtype dtype, int64_t N, int64_t D, in
     const cci_status st = check_rms(dtype, N, D, x, ldx, residual, ldr, weight, eps, y, h, rstd);
     if (st != CCI_OK) return st;
     if (!aligned(y, elem_size(dtype))) return CCI_ERR_ALIGN;
+    if (!in_place_ok(N, D, x, ldx, residual, ldr, h)) return CCI_ERR_SHAPE;
     if (N == 0) return CCI_OK;
     return to_status(launch_rms_norm(x, ldx, residual, ldr, dtype, N, D, weight, eps, y, h, rstd, nullptr, 0,
                                      as_stream(stream)));
@@ -357,6 +364,7 @@ cci_status cci_rms_norm_fp8(const void *x, cci_dtype dtype, int64_t N, int64_t D
     if (!aligned(x, 16) || ldx * es % 16 != 0 || !aligned(residual, 16) || (residual && ldr * es % 16 != 0) ||
         !aligned(h, 16) || !aligned(weight, 16) || !aligned(q, 16) || !aligned(scales, 4))
         return CCI_ERR_ALIGN;
+    if (!in_place_ok(N, D, x, ldx, residual, ldr, h)) return CCI_ERR_SHAPE;
     if (N == 0) return CCI_OK;
     const int groups = group == 0 ? 1 : static_cast<int>((D + 127) / 128);
     return to_status(launch_rms_norm(x, ldx, residual, ldr, dtype, N, D, weight, eps, q, h, rstd, scales, groups,
@@ -440,7 +448,7 @@ cci_status cci_distillation_loss_backward(const float *dloss, const void *logits
     const cci_status st = check_distillation(dtype, N, V, logits, ldx, top_idx, top_logp, k, temperature, stats);
     if (st != CCI_OK) return st;
     if (N > 0 && (!dloss || !dlogits)) return CCI_ERR_NULL;
-    if (!rows_ok(N, V, lddx)) return CCI_ERR_SHAPE;
+    if (!rows_ok(N, V, lddx) || (dlogits == logits && N > 1 && lddx != ldx)) return CCI_ERR_SHAPE;
     if (!aligned(dloss, 4) || !aligned(dlogits, elem_size(dtype))) return CCI_ERR_ALIGN;
     if (N == 0) return CCI_OK;
     return to_status(launch_distillation_backward(dloss, logits, dtype, N, V, ldx, top_idx, top_logp, k, temperature,

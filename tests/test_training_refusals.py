@@ -95,6 +95,17 @@ KD = [(dict(x=0), NULL), (dict(i=0), NULL), (dict(v=0), NULL), (dict(stats=0), N
 KD += [(dict(T=4e-39), VALUE), (dict(T=1e-45), VALUE)]  # log2(e) / T is infinite
 
 
+@pytest.mark.parametrize("call", [rms, rms8])
+def test_sums_go_over_no_other_row(lib, call):
+    """In place of rows that are not packed."""
+    assert call(lib, ldx=128) == SHAPE and call(lib, ldr=72) == SHAPE
+    assert call(lib, x=0, N=0, ldx=128, h=0) == OK
+
+
+def test_gradients_go_over_no_other_row(lib):
+    assert kd_back(lib, ldd=101) == SHAPE and kd_back(lib, ld=101) == SHAPE
+
+
 LONG = dict(N=1, V=1 << 24, ld=1 << 24)  # one row for many blocks, too long for a cluster
 
 
