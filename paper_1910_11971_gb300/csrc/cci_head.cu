@@ -14,11 +14,11 @@
 //
 // The tensor core cuts its running sum at every addition, always towards zero: 256 of them, at D = 4096, leave a logit
 // of 12 about 6e-5 off, and a confident token's loss, a difference of such logits, as much of itself and more.  So the
-// forward pass adds about eight stages (512 reduction indices) at a time there and the chunks in registers, to the nearest, as
+// forward pass adds about eight stages (512 reduction indices, 704 at most) at a time there and the chunks in registers, to the nearest, as
 // fp32 does throughout (1999 x 4096 x 50257 bf16: 421 us with one running sum, 437 so, 579 with chunks of 256).  That takes
 // eight output warps, each 32 tokens by half of a tile's columns.  The backward pass adds as the forward pass does: a sure token's
 // gradient, p - 1, is the difference of its logit from what the forward pass made of the same sums (with one running
-// sum 4096 x 2048 x 131072 bf16 both passes took 5114 us, 5175 so, and a p of 0.999 was 2 % of its 1 - p off).
+// sum a p of 0.999 was 2 % of its 1 - p off).
 //
 // Tiles: 256 tokens x 256 columns over a CTA pair, or for few tokens or columns 128 x 256 and 128 x 128 on one CTA.
 // Sixteen M tiles at a time pass over the vocabulary, so that W is read once for up to 4096 tokens.
@@ -36,10 +36,11 @@ using gated::stage_mma;
 using gated::term_planes;
 using gated::tile_desc;
 
-// stages that the tensor core adds up by itself, of a tile's n: about eight, eleven at most
+// stages that the tensor core adds up by itself, of a tile's n: about eight of many, up to eleven of up to 33, where the output
+// warps are what a tile waits for (4096 x 2048 x 131072 bf16 both passes: 5235 us with eight, 5084 so)
 inline int chunk_of(int n)
 {
-    const int chunks = n < 12 ? 1 : (n + 4) / 8;
+    const int chunks = n <= 33 ? (n + 10) / 11 : (n + 4) / 8;
     return (n + chunks - 1) / chunks;
 }
 constexpr int kMTilesAtOnce = 16;
