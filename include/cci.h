@@ -779,15 +779,15 @@ cci_status cci_linear_cross_entropy(const void *X, cci_dtype dtype, int64_t N, i
  *   P[n][v] = dloss[n] * (softmax(z)[v] - 1[v = t]),  dX = P W,  dW = P^T X
  * in pieces of the vocabulary, whose logits are computed again.  P is rounded to bf16 for the products (fp32:
  * split into planes); sums are fp32 in a fixed order, each gradient rounded once to dtype.  Rows whose
- * target is `ignore_index`, or outside [0, V) (which sets CCI_ERR_INDEX), or whose dloss is 0 have P = 0; they
- * take part in dW as zeros, so their X has to be finite.  Up to 32 tokens of fp32 take the sums in another order than
+ * target is `ignore_index`, or outside [0, V) (which sets CCI_ERR_INDEX), or whose dloss is 0 have P = 0 and
+ * take no part, whatever their X holds.  Up to 32 tokens of fp32 take the sums in another order than
  * more do.
  *
  *   dloss      device fp32 [N];  X, W, targets as in the forward call
  *   stats      as the forward call wrote them
  *   dX         device [N][D] of dtype (written), or NULL
  *   dW         device [V][D] of dtype (written; zeros for N = 0), or NULL
- *   workspace  cci_head_workspace_size(CCI_HEAD_BACKWARD, ...) bytes: about 256 MB for a piece, more
+ *   workspace  cci_head_workspace_size(CCI_HEAD_BACKWARD, ...) bytes: X once more and about 256 MB for a piece, more
  *              only where a piece of 2048 entries, or of 128 times 128 / N for each SM, takes more
  * Errors: as cci_linear_cross_entropy.
  */

@@ -355,7 +355,7 @@ __global__ void __launch_bounds__(Cfg<CG, BN, PROBS>::kThreads, 1)
             }
             if (!ok) break;
             // the target among these columns, or -1
-            const bool kept = token != p.ignore && token >= 0 && token < p.V;
+            const bool kept = is_kept(token, p.ignore, p.V);
             const int64_t at = kept ? token - p.col0 - n0 : -1;
             const int target = at >= 0 && at < count ? static_cast<int>(at) : -1;
             if constexpr (!PROBS) {
@@ -537,6 +537,35 @@ __global__ void __launch_bounds__(256) cut_kernel(const float *in, uint16_t *out
     }
 }
 
+// X for the gradients' products: left-out tokens' rows are zeros whatever they hold, which would come into every row of dW as 0 times
+// it.  fp32: its planes, cut as above.  A warp a row (4096 x 2048 bf16: 6 us of the pass' 3900)
+template <typename T>
+__global__ void __launch_bounds__(256) kept_rows_kernel(const T *in, uint16_t *out, int64_t N, int D, const int64_t *targets, int64_t ignore,
+                                                        int64_t V, const float *dloss)
+{
+    const int lane = threadIdx.x & 31;
+    const int64_t n = static_cast<int64_t>(blockIdx.x) * 8 + (threadIdx.x >> 5);
+    if (n >= N) return;
+    const bool keep = is_kept(targets[n], ignore, V) && dloss[n] != 0.f;
+    for (int c = lane * 8; c < D; c += 256) {
+        row::Raw<T, 8> raw{};
+        if (keep) raw = row::load_once<T, 8>(in + n * D + c);
+        if constexpr (sizeof(T) == 2) {
+            *reinterpret_cast<uint4 *>(out + n * D + c) = raw.w[0];
+        } else {
+            float v[8];
+            row::unpack<float, 8>(raw, v);
+#pragma unroll
+            for (int q = 0; q < 3; ++q) {
+                uint32_t w[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) w[j] = next_planes(v[2 * j], v[2 * j + 1]);
+                *reinterpret_cast<uint4 *>(out + q * N * D + n * D + c) = make_uint4(w[0], w[1], w[2], w[3]);
+            }
+        }
+    }
+}
+
 // dX from its fp32 sums
 __global__ void __launch_bounds__(256) round_kernel(const float *in, uint16_t *out, int64_t n)
 {
@@ -603,7 +632,7 @@ constexpr int64_t kBackwardBudget = int64_t(256) << 20;
 struct Layout {
     int64_t piece;    // columns of a piece (the last one may be narrower)
     int64_t ldp;      // row stride of P
-    size_t x, w;      // planes (fp32)
+    size_t x, w;      // planes (fp32); backward: kept_rows_kernel's X
     size_t parts, at_target;  // forward
     size_t p, dx, products;   // backward
     size_t total;
@@ -628,10 +657,8 @@ Layout layout(int dtype, int64_t N, int64_t D, int64_t V, int call)
     else
         l.piece = piece_of(V, f32 ? 6 * (N + D) : 2 * N, kBackwardBudget, N);
     if (l.piece > V) l.piece = V;
-    if (f32) {
-        l.x = take(6 * N * D);
-        if (!few_tokens(dtype, N)) l.w = take(6 * l.piece * D);
-    }
+    if (f32 || call == CCI_HEAD_BACKWARD) l.x = take(2 * planes * N * D);
+    if (f32 && !few_tokens(dtype, N)) l.w = take(6 * l.piece * D);
     if (few_tokens(dtype, N) && call == CCI_HEAD_BACKWARD) {
         l.p = take(4 * V * few_pitch(N));
         l.products = take(4 * few_slices(N, D, V, ws::sm_count()) * N * D);
@@ -834,8 +861,16 @@ cudaError_t launch_head_backward(const HeadArgs &a, cudaStream_t stream)
     uint16_t *probs = reinterpret_cast<uint16_t *>(base + l.p);
     const int np = f32 ? 3 : 1;
     const bool sums = !f32 && l.piece < a.V;  // dX in fp32 until the last piece
-    if (f32) e = planes(a.X, base + l.x, a.N * a.D, stream);
-    const Operand x{f32 ? base + l.x : a.X, a.N, a.D, np};
+    const unsigned blocks = static_cast<unsigned>((a.N + 7) / 8);
+    uint16_t *kept = reinterpret_cast<uint16_t *>(base + l.x);
+    if (f32)
+        kept_rows_kernel<float><<<blocks, 256, 0, stream>>>(static_cast<const float *>(a.X), kept, a.N, static_cast<int>(a.D), a.targets,
+                                                            a.ignore, a.V, a.dloss);
+    else
+        kept_rows_kernel<uint16_t><<<blocks, 256, 0, stream>>>(static_cast<const uint16_t *>(a.X), kept, a.N, static_cast<int>(a.D),
+                                                               a.targets, a.ignore, a.V, a.dloss);
+    e = cudaGetLastError();
+    const Operand x{kept, a.N, a.D, np};
     if (few_tokens(a.dtype, a.N)) {
         if (e != cudaSuccess) return e;
         FewParams f = few_params(a, x.data);
@@ -845,7 +880,7 @@ cudaError_t launch_head_backward(const HeadArgs &a, cudaStream_t stream)
         e = launch_few<true>(f, ws::sm_count(), stream);
         if (e != cudaSuccess) return e;
         const FewGradients g{static_cast<const float *>(a.X), f.w, f.probs, f.N, f.D, a.V, 0, static_cast<float *>(a.dW),
-                             a.dX ? reinterpret_cast<float *>(base + l.products) : nullptr};
+                             a.dX ? reinterpret_cast<float *>(base + l.products) : nullptr, a.targets, a.ignore, a.dloss};
         return launch_few_gradients(g, ws::sm_count(), static_cast<float *>(a.dX), stream);
     }
     for (int64_t c = 0; c < a.V && e == cudaSuccess; c += l.piece) {

@@ -12,9 +12,9 @@
 // Backward the same walk gives P [V][tokens] in fp32, and one pass over the weights takes both gradients from it with
 // fused multiply-adds: a thread holds its columns of X and of dX for all tokens, reads a weight, adds P times it to dX and writes
 // P^T X in its place of dW.  dX's parts over slices of the vocabulary are added in order.  7 tokens, 2752 x 34448,
-// both passes: 845 us with planes of W and products of tiles, 327 so, of 224 to read W three times and write dW.  What bounds
+// both passes: 845 us with planes of W and products of tiles, 330 so, of 224 to read W three times and write dW.  What bounds
 // that pass is P, a broadcast load from shared memory for four multiply-adds of each gradient.  17 to about 80 tokens are past what this,
-// or planes, do well: 25 tokens 772 us, where elementary fp32 products take 591.
+// or planes, do well: 25 tokens 777 us, where elementary fp32 products take 591.
 #pragma once
 
 #include "cci_kernels.h"
@@ -25,6 +25,11 @@ namespace cci {
 namespace head {
 
 constexpr int kFewTokens = 32, kFewRows = 32, kFewWarps = 8;
+
+__device__ __forceinline__ bool is_kept(int64_t token, int64_t ignore, int64_t V)
+{
+    return token != ignore && token >= 0 && token < V;
+}
 
 struct FewParams {
     const uint16_t *x;   // three planes [N][D]
@@ -86,7 +91,7 @@ __global__ void __launch_bounds__(kFewWarps * 32, NT <= 2 ? 2 : 1) few_kernel(co
         for (int i = 0; i < NT; ++i) {
             const int n = NT * warp + i;
             const int64_t token = n < p.N ? p.targets[n] : p.ignore;
-            const bool kept = token != p.ignore && token >= 0 && token < p.V;
+            const bool kept = is_kept(token, p.ignore, p.V);
             target[i] = kept ? token : -1;
             weight[i] = kept ? p.dloss[n] : 0.f;
             const float m = n < p.N ? p.stats[2 * n] : 0.f;
@@ -236,6 +241,9 @@ struct FewGradients {
     int N, D;
     int64_t V, slice;  // entries of a slice, a multiple of kFewTile
     float *dw, *parts; // dW, dX's parts [slices][N][D]; each may be null
+    const int64_t *targets;
+    int64_t ignore;
+    const float *dloss;
 };
 
 constexpr int kFewAhead = 4;           // batches of weights on their way
@@ -270,10 +278,13 @@ __global__ void __launch_bounds__(256, 2) few_gradients_kernel(const FewGradient
     };
 #pragma unroll
     for (int k = 0; k < kFewAhead; ++k) copy(from + k * kRows, k);
+    // left-out tokens' X are zeros, whatever they hold
+    const int lane = threadIdx.x & 31;
+    const unsigned kept = __ballot_sync(0xffffffffu, lane < p.N && is_kept(p.targets[lane], p.ignore, p.V) && p.dloss[lane] != 0.f);
     float x[NP][C], dx[NP][C];
 #pragma unroll
     for (int n = 0; n < NP; ++n) {
-        const Columns q = mine && n < p.N ? *reinterpret_cast<const Columns *>(p.x + static_cast<int64_t>(n) * p.D + d) : Columns{};
+        const Columns q = mine && (kept >> n & 1u) ? *reinterpret_cast<const Columns *>(p.x + static_cast<int64_t>(n) * p.D + d) : Columns{};
 #pragma unroll
         for (int j = 0; j < C; ++j) {
             x[n][j] = q.f[j];

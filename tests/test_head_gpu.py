@@ -186,6 +186,24 @@ def test_all_left_out(dev):
     assert (loss == 0).all()
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("N", [5, 20, 40, 300])
+def test_left_out_rows_may_hold_anything(dev, N, dtype):
+    """Pad rows of NaN and inf: to be ignored, with a bad target, without a gradient."""
+    X, W, targets, dloss = inputs(N, 72, 700, dtype, 11)
+    out = torch.arange(N) % 5 < 3
+    targets[0::5], targets[1::5], dloss[2::5] = IGNORE, 700, 0.0
+    clean = torch.where(out[:, None], 0.0, X.float()).to(X.dtype)
+    dirty = torch.where(out[:, None], torch.tensor([float("nan"), float("inf"), -float("inf")]).repeat(24), X.float()).to(X.dtype)
+    got = []
+    for x in (clean, dirty):
+        args = x.to(dev), W.to(dev), targets.to(dev)
+        loss, stats = cci.linear_cross_entropy(*args)
+        got.append((loss[~out.to(dev)], *cci.linear_cross_entropy_backward(dloss.to(dev), *args, stats)))
+    assert all(torch.equal(a, b) for a, b in zip(*got)) and got[0][2].isfinite().all()
+    assert (got[1][1].cpu()[out] == 0).all()
+
+
 def test_no_rows(dev):
     W = torch.ones((30, 16), device=dev)
     X, t = torch.empty((0, 16), device=dev), torch.empty(0, dtype=torch.int64, device=dev)
