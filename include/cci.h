@@ -610,7 +610,8 @@ cci_status cci_token_logprobs_backward(const void *logits, cci_dtype dtype, int6
  *   stats[n] = (max z, log sum exp(z - max), log of that sum over what is not listed,
  *               tail: sum q, else: log sum exp(t_j / T));  where |max z| is 64 or more and its rounding loses
  *               something of max x, the first two are max x and the logarithm with its sign set
- * An index of -1 lists nothing, whatever its t; a row that lists nothing has loss 0 and no gradient.  t_j may
+ * An index of -1 lists nothing, whatever its t; a row that lists nothing has loss 0 and no gradient,
+ * whatever its logits (stats 0, 0, 0 where they have no sum).  t_j may
  * be -inf (q_j = 0, and listed).  A listed logit of -inf with q_j > 0 makes the loss inf.  Where no unlisted logit is
  * above -inf, the rest takes no part (q_rest counts as 0).  NaN or +inf in a row makes its loss NaN.  Any other
  * index outside [0, V), or one that a row lists twice, sets CCI_ERR_INDEX in dev_status and makes the row's loss, and
@@ -639,7 +640,7 @@ cci_status cci_distillation_loss(const void *logits, cci_dtype dtype, int64_t N,
  * cci_distillation_loss_backward -- the gradient of cci_distillation_loss to the logits:
  *   dlogits[n][v] = dloss[n] / T * (Q p_v - q_v)            for the listed, Q = sum q + q_rest
  *                   dloss[n] / T * (Q p_v - q_rest r_v)     for others, r_v = p_v / p_rest (tail 0: Q p_v)
- * Rows of -inf alone and rows that list nothing get 0.
+ * Rows of -inf alone, rows that list nothing and rows whose dloss is 0 get 0.
  *
  *   dloss      device fp32 [N]; logits, top_idx, top_logp, k, temperature, tail as in the forward call
  *   stats      as it wrote them

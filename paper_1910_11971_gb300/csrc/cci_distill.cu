@@ -114,6 +114,7 @@ __device__ __forceinline__ Sums joined(Sums a, Sums b, float c)
 // sum or its normaliser's logarithm, as in stats; and - sum q_j (x_j - top) / T with the sum of those q_j
 struct Listed {
     float top, others, given, norm, off, share;
+    bool nothing;  // no index but -1
 };
 
 // a lane's part of a row's list: indices (-1: none), the teacher's values
@@ -148,20 +149,23 @@ __device__ __forceinline__ Listed listed_of(const Args &a, const int (&at)[kOwn]
     }
     top = row::warp_max(top);
     best = row::warp_max(best);
-    Listed r{top, 0.f, 0.f, 0.f, 0.f, 0.f};
+    Listed r{top, 0.f, 0.f, 0.f, 0.f, 0.f, false};
     const float from = ref_of(top), best_from = ref_of(best);
     int largest = 0;  // how many are
+    bool some = false;
 #pragma unroll
     for (int i = 0; i < kOwn; ++i) {
         q[i] = at[i] < 0 ? 0.f : (a.tail ? expf(q[i]) : expf((q[i] - best_from) / a.T));
         z[i] = (z[i] - from) / a.T;
         r.given += q[i];
+        some = some || at[i] != -1;
         if (z[i] == 0.f)
             ++largest;
         else if (at[i] >= 0)
             r.others += expf(z[i]);
     }
     largest = __reduce_add_sync(0xffffffffu, largest);
+    r.nothing = !__any_sync(0xffffffffu, some);
     r.given = row::warp_sum(r.given);
     r.others = row::warp_sum(r.others) + (largest > 1 ? static_cast<float>(largest - 1) : 0.f);
     const float unit = a.tail || r.given == 0.f ? 1.f : 1.f / r.given;
@@ -318,7 +322,11 @@ __device__ __forceinline__ void finish(const Args &a, int64_t n, const Sums &sum
         if (left > 0.f) loss += left * (listed < rest ? log1pf(listed / rest) : log_s - log_rest);
     }
     if (bad) report(a.status, CCI_ERR_INDEX);
-    a.loss[n] = bad ? nan_f() : loss;
+    a.loss[n] = bad ? nan_f() : (mine.nothing ? 0.f : loss);
+    if (mine.nothing && !bad && !(sum < -neg_inf())) {  // a pad row's logits may be anything: its gradient is 0 by these
+        reinterpret_cast<float4 *>(a.stats)[n] = make_float4(0.f, 0.f, 0.f, mine.norm);
+        return;
+    }
     // The gradient takes differences from the maximum.  Where the rounding of m / T says too little of it (a masked row's, say),
     // it is left as it is, and the logarithm, which is 0 at least, has its sign set
     const float high = m / a.T;
@@ -625,11 +633,12 @@ __global__ void __launch_bounds__(256) gradient_kernel(const Args a)
     const int hi = lo + a.steps * 256 * kU < V ? lo + a.steps * 256 * kU : V;
     const float unit = 1.f / a.T, c = kLog2e / a.T;
     row::Raw<T, 8> next[kU];
+    bool none = false;  // of what is not listed: -inf for it, whatever the logits
     auto load = [&](int e0) {
 #pragma unroll
         for (int u = 0; u < kU; ++u) {
             const int e = e0 + 8 * (32 * u + lane);
-            next[u] = load_group(x, e < V ? e : V, V);
+            next[u] = load_group(x, e < V && !none ? e : V, V);
         }
     };
     load(lo);
@@ -648,7 +657,7 @@ __global__ void __launch_bounds__(256) gradient_kernel(const Args a)
     }
     const float4 st = reinterpret_cast<const float4 *>(a.stats)[n];
     const float weight = a.dloss[n] / a.T, log_s = fabsf(st.y), log_rest = st.z;
-    const float m = ref_of(signbit(st.y) ? st.x : st.x * a.T);
+    float m = ref_of(signbit(st.y) ? st.x : st.x * a.T);
     float whole, left = 0.f;        // Q, q_rest
     float best = 0.f, norm = st.w;  // of the teacher's values: q_j = exp((t_j - best) / T - norm)
     if (a.tail) {
@@ -672,15 +681,19 @@ __global__ void __launch_bounds__(256) gradient_kernel(const Args a)
         if (at[i] >= 0) {
             const float q = a.tail ? expf(own[i]) : (whole == 0.f ? 0.f : expf((own[i] - best) * unit - norm));
             const float p = expf((z[i] - m) * unit - log_s);
-            own[i] = st.x == neg_inf() ? 0.f : (p * whole - q) * weight;
+            own[i] = st.x == neg_inf() || weight == 0.f ? 0.f : (p * whole - q) * weight;
         }
     }
     // off the list: coef exp(z - m - shift).  With a tail, relative to the sum over the unlisted
     const bool some = a.tail && log_rest != neg_inf();
     const float shift = some ? log_rest : log_s;
-    const float coef = (some ? whole * expf(log_rest - log_s) - left : whole) * weight;
+    float coef = (some ? whole * expf(log_rest - log_s) - left : whole) * weight, minus = -shift * kLog2e;
+    none = weight == 0.f || coef == 0.f;
+    if (none) {
+        coef = minus = m = 0.f;
+        load(lo);
+    }
     const unsigned long long c2 = pack2(c, c), neg = pack2(-m, -m), coef2 = pack2(coef, coef);
-    const float minus = -shift * kLog2e;
     const bool words = shift_of(dx) == s;
     __syncwarp();
     for (int e0 = lo; e0 < hi; e0 += 256 * kU) {

@@ -290,6 +290,29 @@ def test_nan_and_inf_keep_to_their_rows(dev):
     assert dx[0].isnan().all() and dx[3].isnan().all() and dx[1:3].isfinite().all()
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("tail", [False, True])
+@pytest.mark.parametrize("N,V", [(9, 1000), (9, 20000), (300, 5000), (4000, 3000)])
+def test_pad_rows_may_hold_anything(dev, N, V, tail, dtype):
+    """Rows that list nothing, and rows without a gradient."""
+    _, x, idx, value, dloss = inputs(N, V, 6, dtype, 14, 1.0, tail)
+    pad, off = torch.arange(N) % 4 == 1, torch.arange(N) % 4 == 2
+    idx[pad], dloss[off] = -1, 0.0
+    clean = torch.where((pad | off)[:, None], 0.0, x.float()).to(x.dtype)
+    dirty = clean.clone()
+    dirty[pad | off] = torch.tensor([1.0, float("nan"), INF, -INF, 2.0]).repeat(V // 5).to(x.dtype)
+    dirty[5] = INF
+    got = []
+    for logits in (clean, dirty):
+        d = logits.to(dev), idx.to(dev), value.to(dev)
+        status = cci.new_status(dev)
+        loss, stats = cci.distillation_loss(*d, tail=tail, status=status)
+        assert int(status.item()) == 0
+        got.append((loss[~off.to(dev)], cci.distillation_loss_backward(dloss.to(dev), *d, stats, tail=tail)))
+    assert torch.equal(got[0][0], got[1][0]) and torch.equal(got[0][1], got[1][1]) and got[0][1].isfinite().all()
+    assert (got[1][1].cpu()[pad | off] == 0).all()
+
+
 def test_teacher_values_of_minus_inf(dev):
     """They are listed, with q = 0: with a tail their logits are not among the rest."""
     N, V, k = 4, 700, 6
