@@ -100,6 +100,19 @@ __device__ __forceinline__ uint32_t e4m3x4(float a, float b, float c, float d)
 // subnormal in fp32 themselves
 __device__ __forceinline__ float scale_of(float most) { return max_nan(most / kE4m3Max, kLeastScale); }
 
+// N values by their scale, each as the division rounds it.  The reciprocal is held in two fp32 numbers, the second what the first
+// lacks of it (a double-length quotient: Dekker, "A floating-point technique for extending the available precision", 1971), so that
+// one rounding is left, of a quotient 2^-30 off at most: a value at the middle of two codes stays there, which the product with the first
+// alone moves now and then.  One operation a value more than that; divisions took 4000 x 8192 bf16 from 38.4 us to 44.6
+template <int N>
+__device__ __forceinline__ void by_scale(float (&y)[N], float scale)
+{
+    // of an infinite scale the second is 0, too
+    const float high = 1.f / scale, low = fmaf(-high, fminf(scale, 3.402823466e38f), 1.f) * high;
+#pragma unroll
+    for (int j = 0; j < N; ++j) y[j] = fmaf(y[j], high, y[j] * low);
+}
+
 template <typename T, int V, int NV, int TPR, bool SUM, bool FP8>
 __global__ void __launch_bounds__(block_threads(TPR), residents(TPR)) rms_kernel(const Forward p)
 {
@@ -193,11 +206,11 @@ __global__ void __launch_bounds__(block_threads(TPR), residents(TPR)) rms_kernel
                     scale = scale_of(m);
                     if (c < D && (t & 15) == 0) p.scales[n * p.groups + c / 128] = scale;
                 }
-                const float inv = 1.f / scale;
+                by_scale<V>(f[i], scale);
                 if (c < D) {
                     uint2 b;
-                    b.x = e4m3x4(f[i][0] * inv, f[i][1] * inv, f[i][2] * inv, f[i][3] * inv);
-                    b.y = e4m3x4(f[i][4] * inv, f[i][5] * inv, f[i][6] * inv, f[i][7] * inv);
+                    b.x = e4m3x4(f[i][0], f[i][1], f[i][2], f[i][3]);
+                    b.y = e4m3x4(f[i][4], f[i][5], f[i][6], f[i][7]);
                     *reinterpret_cast<uint2 *>(q + c) = b;
                 }
             }
@@ -263,9 +276,9 @@ __global__ void __launch_bounds__(1024) rms_long_kernel(const Forward p)
                 scale = scale_of(most);
                 if ((t & 31) == 0) p.scales[n * p.groups + g] = scale;
             }
-            const float inv = 1.f / scale;
+            by_scale<4>(y, scale);
             if (c0 < D) {
-                *reinterpret_cast<uint32_t *>(q + c0) = e4m3x4(y[0] * inv, y[1] * inv, y[2] * inv, y[3] * inv);
+                *reinterpret_cast<uint32_t *>(q + c0) = e4m3x4(y[0], y[1], y[2], y[3]);
 #pragma unroll
                 for (int j = 0; j < 4; ++j)
                     if (h) row::store<T, 1>(h + c0 + j, v + j);
