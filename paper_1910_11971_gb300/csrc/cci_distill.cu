@@ -380,7 +380,7 @@ __global__ void __launch_bounds__(256, 4) short_kernel(const Args a, int bytes)
     if (lane == 0) finish(a, n, sums, mine, c, bad);
 }
 
-// ---- few longer rows: a cluster each (8 x 131072 fp32, k = 32: 6.9 us, 9.0 by the two launches below, and one launch
+// ---- few longer rows: a cluster each (8 x 131072 fp32, k = 32: 7.5 us, 9.0 by the two launches below, and one launch
 // less to queue).  `bytes`: groups of a block ----
 constexpr int kMaxParts = 8;
 
@@ -394,6 +394,8 @@ __global__ void __launch_bounds__(256) cluster_kernel(const Args a, int bytes)
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int64_t n = blockIdx.x / a.parts;
     const int part = static_cast<int>(blockIdx.x % a.parts);
+    // the wait for this arrival, before the store into the first block, sees that every block of the cluster runs
+    if (a.parts > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
     const T *x = static_cast<const T *>(a.x) + n * a.ldx;
     const float c = kLog2e / a.T;
     const int s = shift_of(x), all = (a.V + s + 7) / 8;
@@ -436,6 +438,7 @@ __global__ void __launch_bounds__(256) cluster_kernel(const Args a, int bytes)
     __syncthreads();
     if (warp == 0) sums = warp_joined(lane < 8 ? warps[lane] : Sums{neg_inf(), 0.f}, c);
     if (a.parts > 1) {
+        asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
         cg::cluster_group cluster = cg::this_cluster();
         if (threadIdx.x == 0) *cluster.map_shared_rank(&parts[part], 0) = make_float4(sums.m, sums.s, bad ? 1.f : 0.f, 0.f);
         cluster.sync();
