@@ -309,7 +309,10 @@ __device__ __forceinline__ Sums warp_joined(Sums a, float c)
 __device__ __forceinline__ void finish(const Args &a, int64_t n, const Sums &sums, const Listed &mine, float c, bool bad)
 {
     const float m = fmaxf(sums.m, mine.top), from = ref_of(m);
-    const float rest = sums.s == 0.f ? 0.f : sums.s * ex2((sums.m - from) * c);
+    float rest = sums.s == 0.f ? 0.f : sums.s * ex2((sums.m - from) * c);
+    // The largest's own is 1, which its approximate exponentials (of Walk) miss by some 2^-24 for many maxima: where the others add less,
+    // the logarithm below would come out below 0, and its sign says how the maximum is held.  NaN stays
+    if (sums.m == m && m != neg_inf() && rest < 1.f) rest = 1.f;
     const bool some = mine.top != neg_inf();
     const float listed = some ? (1.f + mine.others) * ex2((mine.top - from) * c) : mine.others, sum = rest + listed;
     const bool empty = m == neg_inf() && sum == 0.f;
@@ -328,7 +331,7 @@ __device__ __forceinline__ void finish(const Args &a, int64_t n, const Sums &sum
         return;
     }
     // The gradient takes differences from the maximum.  Where the rounding of m / T says too little of it (a masked row's, say),
-    // it is left as it is, and the logarithm, which is 0 at least, has its sign set
+    // it is left as it is, and the logarithm, which is 0 at least (of 1 and more, by either way above), has its sign set
     const float high = m / a.T;
     const bool as_is = fabsf(high) >= kFar && high * a.T != m;
     reinterpret_cast<float4 *>(a.stats)[n] =
