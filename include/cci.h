@@ -609,7 +609,9 @@ cci_status cci_token_logprobs_backward(const void *logits, cci_dtype dtype, int6
  * by T^2: the gradient's dloss is the place for that.
  *   stats[n] = (max z, log sum exp(z - max), log of that sum over what is not listed,
  *               tail: sum q, else: log sum exp(t_j / T));  where |max z| is 64 or more and its rounding loses
- *               something of max x, the first two are max x and the logarithm with its sign set
+ *               something of max x, the first two are max x and the logarithm with its sign set; with a tail, where
+ *               the third is -64 or less, the last two are the largest x of what is not listed, and the log of
+ *               the sum of exp(z - its z) with its sign set
  * An index of -1 lists nothing, whatever its t; a row that lists nothing has loss 0 and no gradient,
  * whatever its logits (stats 0, 0, 0 where they have no sum).  t_j may
  * be -inf (q_j = 0, and listed).  A listed logit of -inf with q_j > 0 makes the loss inf.  Where no unlisted logit is

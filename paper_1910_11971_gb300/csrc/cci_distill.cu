@@ -318,10 +318,14 @@ __device__ __forceinline__ void finish(const Args &a, int64_t n, const Sums &sum
     const bool empty = m == neg_inf() && sum == 0.f;
     // A sure student's loss is what others add to the 1 of a listed token, a small rest's what the listed add to it: neither
     // is left to the rounding of a sum that is mostly something else.  No term below is negative: nothing cancels
-    const float log_s = empty ? 0.f : (some && mine.top >= sums.m ? log1pf(mine.others + rest) : logf(sum)), log_rest = logf(rest);
+    const float log_s = empty ? 0.f : (some && mine.top >= sums.m ? log1pf(mine.others + rest) : logf(sum));
+    // far below the listed, the rest's share is no number of 32 bits, or one of few digits, but its logarithm is
+    const bool others = sums.s != 0.f;
+    const float down = (sums.m - from) / a.T, log_own = logf(sums.s < 1.f ? 1.f : sums.s);
+    const float log_rest = !others ? neg_inf() : (down > -kFar ? logf(rest) : log_own + down);
     float loss = mine.off + (mine.share == 0.f ? 0.f : mine.share * (log_s - (ref_of(mine.top) - from) / a.T));
     if (a.tail) {
-        const float left = rest == 0.f ? 0.f : fmaxf(1.f - mine.given, 0.f);
+        const float left = others ? fmaxf(1.f - mine.given, 0.f) : 0.f;
         if (left > 0.f) loss += left * (listed < rest ? log1pf(listed / rest) : log_s - log_rest);
     }
     if (bad) report(a.status, CCI_ERR_INDEX);
@@ -334,8 +338,11 @@ __device__ __forceinline__ void finish(const Args &a, int64_t n, const Sums &sum
     // it is left as it is, and the logarithm, which is 0 at least (of 1 and more, by either way above), has its sign set
     const float high = m / a.T;
     const bool as_is = fabsf(high) >= kFar && high * a.T != m;
-    reinterpret_cast<float4 *>(a.stats)[n] =
-        make_float4(bad ? nan_f() : (as_is ? m : high), as_is ? -log_s : log_s, log_rest, mine.norm);
+    // Nor does the rounding of log_rest say enough of a rest that lies as far below: the largest of it as it is, and in the
+    // place of the teacher's sum, which is at least 0 and taken from the list again, the logarithm of its own sum with the sign set
+    const bool apart = a.tail && others && log_rest <= -kFar;
+    reinterpret_cast<float4 *>(a.stats)[n] = make_float4(bad ? nan_f() : (as_is ? m : high), as_is ? -log_s : log_s,
+                                                         apart ? sums.m : log_rest, apart ? -log_own : mine.norm);
 }
 
 // ---- short rows, or many: a warp each.  The argument: bytes of a row's bits ----
@@ -663,12 +670,20 @@ __global__ void __launch_bounds__(256) gradient_kernel(const Args a)
     }
     const float4 st = reinterpret_cast<const float4 *>(a.stats)[n];
     const float weight = a.dloss[n] / a.T, log_s = fabsf(st.y), log_rest = st.z;
-    float m = ref_of(signbit(st.y) ? st.x : st.x * a.T);
+    const float m = ref_of(signbit(st.y) ? st.x : st.x * a.T);
+    const bool apart = a.tail && signbit(st.w), some = a.tail && (apart || log_rest != neg_inf());
     float whole, left = 0.f;        // Q, q_rest
     float best = 0.f, norm = st.w;  // of the teacher's values: q_j = exp((t_j - best) / T - norm)
     if (a.tail) {
-        left = log_rest == neg_inf() ? 0.f : fmaxf(1.f - st.w, 0.f);
-        whole = st.w + left;
+        float given = st.w;
+        if (apart) {
+            given = 0.f;
+            for (int j = lane; j < a.k; j += 32)
+                if (a.idx[n * a.k + j] >= 0) given += expf(a.value[n * a.k + j]);
+            given = row::warp_sum(given);
+        }
+        if (some) left = fmaxf(1.f - given, 0.f);
+        whole = given + left;
     } else {
         if (fabsf(norm) >= kFar) {
             best = neg_inf();
@@ -690,16 +705,17 @@ __global__ void __launch_bounds__(256) gradient_kernel(const Args a)
             own[i] = st.x == neg_inf() || weight == 0.f ? 0.f : (p * whole - q) * weight;
         }
     }
-    // off the list: coef exp(z - m - shift).  With a tail, relative to the sum over the unlisted
-    const bool some = a.tail && log_rest != neg_inf();
-    const float shift = some ? log_rest : log_s;
-    float coef = (some ? whole * expf(log_rest - log_s) - left : whole) * weight, minus = -shift * kLog2e;
+    // off the list: coef exp((x - base) / T - shift).  With a tail, relative to the sum over the unlisted
+    float base = apart ? log_rest : m;
+    const float shift = apart ? fabsf(st.w) : (some ? log_rest : log_s);
+    const float log_p = (apart ? (base - m) / a.T + shift : log_rest) - log_s;  // of the rest
+    float coef = (some ? whole * expf(log_p) - left : whole) * weight, minus = -shift * kLog2e;
     none = weight == 0.f || coef == 0.f;
     if (none) {
-        coef = minus = m = 0.f;
+        coef = minus = base = 0.f;
         load(lo);
     }
-    const unsigned long long c2 = pack2(c, c), neg = pack2(-m, -m), coef2 = pack2(coef, coef);
+    const unsigned long long c2 = pack2(c, c), neg = pack2(-base, -base), coef2 = pack2(coef, coef);
     const bool words = shift_of(dx) == s;
     __syncwarp();
     for (int e0 = lo; e0 < hi; e0 += 256 * kU) {
