@@ -329,7 +329,9 @@ __device__ __forceinline__ void finish(const Args &a, int64_t n, const Sums &sum
         if (left > 0.f) loss += left * (listed < rest ? log1pf(listed / rest) : log_s - log_rest);
     }
     if (bad) report(a.status, CCI_ERR_INDEX);
-    a.loss[n] = bad ? nan_f() : (mine.nothing ? 0.f : loss);
+    // a sum that is NaN (of such logits, of +inf, or of a wrong list, as sums_kernel hands it on) is the loss' too, where the teacher gives
+    // nothing any weight as well
+    a.loss[n] = bad ? nan_f() : (mine.nothing ? 0.f : (sum != sum ? sum : loss));
     if (mine.nothing && !bad && !(sum < -neg_inf())) {  // a pad row's logits may be anything: its gradient is 0 by these
         reinterpret_cast<float4 *>(a.stats)[n] = make_float4(0.f, 0.f, 0.f, mine.norm);
         return;

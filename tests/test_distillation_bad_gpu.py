@@ -1,0 +1,65 @@
+"""Rows of distillation whose list is wrong, or whose logits are no numbers, where the teacher gives nothing any weight: their loss
+is NaN all the same, in each of the kernels, and the rows beside them are as they were."""
+import pytest
+import torch
+
+import paper_1910_11971_gb300 as cci
+
+INF, NAN = float("inf"), float("nan")
+INDEX = 10  # CCI_ERR_INDEX
+
+pytestmark = pytest.mark.gpu
+
+SIZES = [(40, 900), (9, 20000), (300, 5000)]  # a warp, a cluster a row; rows that share blocks
+
+
+@pytest.fixture(scope="module")
+def dev():
+    return torch.device("cuda:0")
+
+
+def lists(N, V, kind):
+    """idx, value, the wrong rows: every third."""
+    g = torch.Generator().manual_seed(V)
+    k = 1 if kind == "one" else 4
+    idx = torch.stack([torch.randperm(V, generator=g)[:k] for _ in range(N)]).to(torch.int32)
+    value = torch.log(torch.full((N, k), 0.2))
+    bad = torch.arange(N) % 3 == 1
+    if kind == "one":
+        idx[bad, 0] = -2
+    elif kind == "pads":          # another number than -1 for what is not there
+        idx[bad] = -100
+    elif kind == "past":
+        idx[bad, 2] = V
+        idx[bad, :2], idx[bad, 3] = -1, -1
+    else:                         # listed twice, of no weight
+        idx[bad, 3] = idx[bad, 1]
+        value[bad] = -INF
+    return idx, value, bad
+
+
+@pytest.mark.parametrize("tail", [False, True])
+@pytest.mark.parametrize("kind", ["one", "pads", "past", "twice"])
+@pytest.mark.parametrize("N,V", SIZES)
+def test_wrong_lists(dev, N, V, kind, tail):
+    x = torch.randn((N, V), generator=torch.Generator().manual_seed(1)).to(dev)
+    idx, value, bad = lists(N, V, kind)
+    status = cci.new_status(dev)
+    loss, _ = cci.distillation_loss(x, idx.to(dev), value.to(dev), tail=tail, status=status)
+    assert cci.read_status(status) == INDEX
+    assert (loss.cpu().isnan() == bad).all()
+    good = torch.where(bad[:, None], -1, idx).to(torch.int32)
+    same, _ = cci.distillation_loss(x, good.to(dev), value.to(dev), tail=tail)
+    assert torch.equal(loss.cpu()[~bad], same.cpu()[~bad])
+
+
+@pytest.mark.parametrize("what", [NAN, INF])
+@pytest.mark.parametrize("N,V", SIZES)
+def test_no_numbers_where_nothing_has_weight(dev, N, V, what):
+    x = torch.randn((N, V), generator=torch.Generator().manual_seed(2))
+    idx = torch.arange(3, dtype=torch.int32).repeat(N, 1)
+    value = torch.full((N, 3), -INF)
+    bad = torch.arange(N) % 3 == 1
+    x[bad, V // 2] = what
+    loss, _ = cci.distillation_loss(x.to(dev), idx.to(dev), value.to(dev))
+    assert (loss.cpu().isnan() == bad).all() and (loss.cpu()[~bad] == 0).all()
