@@ -699,12 +699,13 @@ __global__ void __launch_bounds__(256) gradient_kernel(const Args a)
         }
         whole = norm == neg_inf() ? 0.f : 1.f;  // nothing listed
     }
+    const bool lost = st.x != st.x || st.y != st.y;  // a wrong list, logits that are no numbers
 #pragma unroll
     for (int i = 0; i < kOwn; ++i) {
         if (at[i] >= 0) {
             const float q = a.tail ? expf(own[i]) : (whole == 0.f ? 0.f : expf((own[i] - best) * unit - norm));
             const float p = expf((z[i] - m) * unit - log_s);
-            own[i] = st.x == neg_inf() || weight == 0.f ? 0.f : (p * whole - q) * weight;
+            own[i] = weight == 0.f || (st.x == neg_inf() && !lost) ? 0.f : (p * whole - q) * (lost ? nan_f() : weight);
         }
     }
     // off the list: coef exp((x - base) / T - shift).  With a tail, relative to the sum over the unlisted
@@ -712,6 +713,7 @@ __global__ void __launch_bounds__(256) gradient_kernel(const Args a)
     const float shift = apart ? fabsf(st.w) : (some ? log_rest : log_s);
     const float log_p = (apart ? (base - m) / a.T + shift : log_rest) - log_s;  // of the rest
     float coef = (some ? whole * expf(log_p) - left : whole) * weight, minus = -shift * kLog2e;
+    if (lost) coef = nan_f();
     none = weight == 0.f || coef == 0.f;
     if (none) {
         coef = minus = base = 0.f;

@@ -63,3 +63,23 @@ def test_no_numbers_where_nothing_has_weight(dev, N, V, what):
     x[bad, V // 2] = what
     loss, _ = cci.distillation_loss(x.to(dev), idx.to(dev), value.to(dev))
     assert (loss.cpu().isnan() == bad).all() and (loss.cpu()[~bad] == 0).all()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("tail", [False, True])
+@pytest.mark.parametrize("kind", ["one", "pads", "past", "twice"])
+@pytest.mark.parametrize("N,V", SIZES)
+def test_gradients_of_wrong_lists(dev, N, V, kind, tail, dtype):
+    """NaN all along the row, unless its loss has no gradient; the other rows' as without."""
+    x = torch.randn((N, V), generator=torch.Generator().manual_seed(1)).to(dtype)
+    idx, value, bad = lists(N, V, kind)
+    x[1], x = -INF, x.to(dev)  # nothing but a wrong list
+    dloss = torch.where(torch.arange(N) % 6 == 4, 0.0, 1.0)
+    got = []
+    for at in (idx, torch.where(bad[:, None], -1, idx).to(torch.int32)):
+        args = x, at.to(dev), value.to(dev)
+        _, stats = cci.distillation_loss(*args, tail=tail)
+        got.append(cci.distillation_loss_backward(dloss.to(dev), *args, stats, tail=tail).cpu())
+    lost = bad & (dloss != 0)
+    assert got[0][lost].isnan().all() and (got[0][bad & ~lost] == 0).all()
+    assert torch.equal(got[0][~bad], got[1][~bad]) and got[1].isfinite().all()
