@@ -660,10 +660,12 @@ __global__ void __launch_bounds__(256) gradient_kernel(const Args a)
     // the listed logits among these, read before any of them is written (dx may be x), and what the teacher says of them
     int at[kOwn];
     float z[kOwn], own[kOwn];
+    bool listed = false;  // anything at all: a pad row has no gradient, whatever its loss has
 #pragma unroll
     for (int i = 0; i < kOwn; ++i) {
         const int j = lane + i * 32;
         at[i] = j < a.k ? a.idx[n * a.k + j] : -1;
+        listed = listed || at[i] != -1;
         if (at[i] < lo || at[i] >= hi) at[i] = -1;
         if (at[i] >= 0) {
             z[i] = row::to_f32(x[at[i]]);
@@ -714,7 +716,7 @@ __global__ void __launch_bounds__(256) gradient_kernel(const Args a)
     const float log_p = (apart ? (base - m) / a.T + shift : log_rest) - log_s;  // of the rest
     float coef = (some ? whole * expf(log_p) - left : whole) * weight, minus = -shift * kLog2e;
     if (lost) coef = nan_f();
-    none = weight == 0.f || coef == 0.f;
+    none = weight == 0.f || coef == 0.f || !__any_sync(0xffffffffu, listed);
     if (none) {
         coef = minus = base = 0.f;
         load(lo);

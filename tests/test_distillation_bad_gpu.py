@@ -83,3 +83,19 @@ def test_gradients_of_wrong_lists(dev, N, V, kind, tail, dtype):
     lost = bad & (dloss != 0)
     assert got[0][lost].isnan().all() and (got[0][bad & ~lost] == 0).all()
     assert torch.equal(got[0][~bad], got[1][~bad]) and got[1].isfinite().all()
+
+
+@pytest.mark.parametrize("tail", [False, True])
+@pytest.mark.parametrize("N,V", SIZES)
+def test_pad_rows_have_no_gradient_whatever_their_loss_has(dev, N, V, tail):
+    """Rows that list nothing, beside an incoming gradient of NaN or inf for them."""
+    x = torch.randn((N, V), generator=torch.Generator().manual_seed(3)).to(dev)
+    idx = torch.arange(4, dtype=torch.int32).repeat(N, 1)
+    pad = torch.arange(N) % 3 == 1
+    idx[pad] = -1
+    value = torch.log(torch.full((N, 4), 0.2))
+    args = x, idx.to(dev), value.to(dev)
+    _, stats = cci.distillation_loss(*args, tail=tail)
+    for what in (NAN, INF, 1.0):
+        dx = cci.distillation_loss_backward(torch.where(pad, what, 1.0).to(dev), *args, stats, tail=tail).cpu()
+        assert (dx[pad] == 0).all() and dx[~pad].isfinite().all()
