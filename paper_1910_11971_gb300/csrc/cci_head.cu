@@ -37,7 +37,9 @@ using gated::term_planes;
 using gated::tile_desc;
 
 // stages that the tensor core adds up by itself, of a tile's n: about eight of many, up to eleven of up to 33, where the output
-// warps are what a tile waits for (4096 x 2048 x 131072 bf16 both passes: 5235 us with eight, 5084 so)
+// warps are what a tile waits for (4096 x 2048 x 131072 bf16 both passes: 5235 us with eight, 5084 so; 4096 tokens by 32768, forward:
+// 1280 wide 194 and 171, 1408 212 and 192, 1792 275 and 248, 2112 309 and 302; widths between 1408 and 1792, and from 2176 on, are cut alike by
+// both)
 inline int chunk_of(int n)
 {
     const int chunks = n <= 33 ? (n + 10) / 11 : (n + 4) / 8;
