@@ -642,7 +642,7 @@ cci_status cci_distillation_loss(const void *logits, cci_dtype dtype, int64_t N,
  * cci_distillation_loss_backward -- the gradient of cci_distillation_loss to the logits:
  *   dlogits[n][v] = dloss[n] / T * (Q p_v - q_v)            for the listed, Q = sum q + q_rest
  *                   dloss[n] / T * (Q p_v - q_rest r_v)     for others, r_v = p_v / p_rest (tail 0: Q p_v)
- * Rows of -inf alone, rows that list nothing and rows whose dloss is 0 get 0.
+ * Rows of -inf alone, rows that list nothing, whatever their dloss, and rows whose dloss is 0 get 0.
  *
  *   dloss      device fp32 [N]; logits, top_idx, top_logp, k, temperature, tail as in the forward call
  *   stats      as it wrote them
@@ -749,7 +749,7 @@ cci_status cci_gated_linear_backward(const void *dH, const void *X, cci_dtype dt
  *   stats[n] = (m, log sum exp(z - m)), m the row's maximum (the gradient needs them)
  * with fp32 accumulators (bf16: products of the exact values; fp32: three bf16 planes of every
  * operand, as cci_gated_linear).  A target equal to `ignore_index` gives loss 0; any other target
- * outside [0, V) sets CCI_ERR_INDEX in dev_status and gives NaN.  NaN or infinite logits make their row's loss
+ * outside [0, V) sets CCI_ERR_INDEX in dev_status and gives NaN.  NaN or +inf logits make their row's loss
  * NaN.
  *
  *   X          device [N][D] of dtype
